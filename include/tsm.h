@@ -366,6 +366,85 @@ int tsm_resnet50_infer(const tsm_r50_desc* d, const void* clips, const float* pa
                        const float* bn_state, float* logits_out,
                        void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Gated linear recurrence over the frames of a clip: the operator along time for sequences that a shift of one frame
+ * does not reach across (long videos, features of whole clips, streams served frame by frame).
+ *   fwd:  a = sigmoid(g), h_t = a_t * h_{t-1} + (1 - a_t) * x_t, y_t = h_t rounded to dtype (the state itself is fp32)
+ *   bwd:  D_t = dy_t + a_{t+1} * D_{t+1} (behind the last frame: dh_last), dx_t = (1 - a_t) * D_t,
+ *         dg_t = D_t * (h_{t-1} - x_t) * a_t * (1 - a_t), dh0 = a_0 * D_0
+ * x, g, y, dy, dx, dg: [N,T,C,H,W] of dtype, dense.  Every value of a frame is a recurrence of its own, so the memory
+ * order of a frame does not matter: TSM_NTCHW and TSM_NTHWC tensors are taken alike, the states in the same order.
+ * h0, h_last, dh_last, dh0: fp32 [N,C,H,W], each may be NULL (h0, dh_last: zeros; h_last, dh0: not wanted).  h_last may
+ * be h0: a stream's state, carried in place from call to call (T = 1: one new frame).
+ * saved: caller-owned buffer of tsm_recur_saved_bytes(desc) bytes (0 up to 128 frames) in which the forward pass keeps
+ * what the backward pass needs; NULL in the forward pass where none follows.  The backward pass takes the h0 that the
+ * forward pass read.  Workspace: tsm_recur_workspace_bytes(desc), 0 for most shapes; NULL is accepted then.
+ * Steps are joined as affine maps, in a fixed order.  Once a state of a column is infinite its later states are
+ * infinite or NaN, which of the two depends on how its steps were joined.  No output may overlap an input or another
+ * output (h_last == h0 aside): TSM_ERR_SHAPE.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    int N, T, C, H, W;
+    int dtype;
+} tsm_recur_desc;
+size_t tsm_recur_saved_bytes(const tsm_recur_desc* d);
+size_t tsm_recur_workspace_bytes(const tsm_recur_desc* d);
+int tsm_recur_fwd(const tsm_recur_desc* d, const void* x, const void* g, const float* h0, void* y, float* h_last,
+                  void* saved, void* ws, size_t ws_bytes, void* stream);
+int tsm_recur_bwd(const tsm_recur_desc* d, const void* x, const void* g, const float* h0, const void* saved,
+                  const void* dy, const float* dh_last, void* dx, void* dg, float* dh0,
+                  void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Layer norm over the channels of a pixel or of a frame's feature vector (a normalisation that, unlike the blocks'
+ * BatchNorm, does not look at the rest of the batch).
+ *   fwd:  mean = sum x / C, rstd = 1 / sqrt(sum (x - mean)^2 / C + eps), xhat = (x - mean) * rstd, y = gamma * xhat + beta
+ *   bwd:  v = gamma * dy, dx = rstd * (v - mean(v) - xhat * mean(v * xhat)),
+ *         dgamma = sum over rows of dy * xhat, dbeta = sum over rows of dy (overwritten, summed in a fixed order)
+ * x, y, dy, dx: `rows` dense rows of C values of dtype -- the pixels of a TSM_NTHWC tensor, or feature vectors.
+ * gamma, beta, dgamma, dbeta: fp32 [C].  mean, rstd: fp32 [rows], written by the forward pass (each may be NULL there)
+ * and read by the backward pass.  Any C.  No output may overlap an input or another output: TSM_ERR_SHAPE.
+ * Workspace (backward only): tsm_layernorm_workspace_bytes(desc).
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    int64_t rows;
+    int C;
+    int dtype;
+    float eps;
+} tsm_layernorm_desc;
+size_t tsm_layernorm_workspace_bytes(const tsm_layernorm_desc* d);
+int tsm_layernorm_fwd(const tsm_layernorm_desc* d, const void* x, const float* gamma, const float* beta, void* y,
+                      float* mean, float* rstd, void* stream);
+int tsm_layernorm_bwd(const tsm_layernorm_desc* d, const void* x, const void* dy, const float* gamma,
+                      const float* mean, const float* rstd, void* dx, float* dgamma, float* dbeta,
+                      void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Linear classifier with softmax cross entropy, for heads of any number of classes: the logits are never stored.
+ *   fwd:  s = x w^T + bias, lse[r] = log sum_v exp s[r,v], loss[r] = lse[r] - s[r,labels[r]]
+ *   bwd:  G[r,v] = dloss[r] * (exp(s[r,v] - lse[r]) - (v == labels[r])), dx = G w, dw = G^T x, dbias = column sums of G
+ * x [rows,features], w [classes,features] of dtype; bias fp32 [classes] or NULL; labels int32 [rows].  A row whose label
+ * is no class (negative, or classes and above) is left out: its loss and its rows of G are zero, and what x holds there
+ * (NaN, infinities) reaches neither dw nor dbias.  Its lse is written like any other.
+ * loss, lse: fp32 [rows], per row; the mean of a batch is the caller's (dloss[r] = 1 / number of rows with a label).
+ * dx, dw: the types of x and w, overwritten; dbias fp32; each may be NULL where it is not wanted, not all of them.
+ * The backward pass forms the logits again, in pieces of the classes; lse is the forward pass's.  In TSM_BF16 the
+ * entries of G are rounded to bf16 for the two products (dbias is summed before that), everything else is fp32.
+ * Logits of minus infinity (a bias that takes a class out) are classes without weight; where no class of a row is left
+ * its lse is minus infinity, and its loss and gradients are NaN.  No output may overlap an input or another output.
+ * Workspace of both calls: tsm_xent_workspace_bytes(desc).
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    int rows, features, classes;
+    int dtype;
+} tsm_xent_desc;
+size_t tsm_xent_workspace_bytes(const tsm_xent_desc* d);
+int tsm_xent_fwd(const tsm_xent_desc* d, const void* x, const void* w, const float* bias, const int32_t* labels,
+                 float* loss, float* lse, void* ws, size_t ws_bytes, void* stream);
+int tsm_xent_bwd(const tsm_xent_desc* d, const void* x, const void* w, const float* bias, const int32_t* labels,
+                 const float* lse, const float* dloss, void* dx, void* dw, float* dbias,
+                 void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,7 +26,10 @@ EXPORTS = ["tsm_last_error", "tsm_profile_begin", "tsm_profile_end", "tsm_mfma_p
            "tsm_block_fwd", "tsm_block_bwd", "tsm_block_infer_workspace_bytes", "tsm_block_infer", "tsm_resnet50_param_count", "tsm_resnet50_num_tensors",
            "tsm_resnet50_param_info", "tsm_resnet50_bn_state_count", "tsm_resnet50_workspace_bytes",
            "tsm_resnet50_step", "tsm_resnet50_workspace_tensor", "tsm_resnet50_infer_workspace_bytes", "tsm_resnet50_infer",
-           "tsm_resnet50_accum_step", "tsm_lr_schedule"]
+           "tsm_resnet50_accum_step", "tsm_lr_schedule",
+           "tsm_recur_saved_bytes", "tsm_recur_workspace_bytes", "tsm_recur_fwd", "tsm_recur_bwd",
+           "tsm_layernorm_workspace_bytes", "tsm_layernorm_fwd", "tsm_layernorm_bwd",
+           "tsm_xent_workspace_bytes", "tsm_xent_fwd", "tsm_xent_bwd"]
 
 
 class TsmError(RuntimeError):
@@ -67,6 +70,18 @@ class R50Desc(ctypes.Structure):
                 ("dtype", ctypes.c_int)]
 
 
+class RecurDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("N", "T", "C", "H", "W", "dtype")]
+
+
+class LayerNormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("C", ctypes.c_int), ("dtype", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+class XentDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "features", "classes", "dtype")]
+
+
 _LIB = None
 
 
@@ -91,7 +106,8 @@ def lib():
         sig("tsm_profile_end", ci, [ctypes.c_char_p, sz])
         sig("tsm_mfma_probe", ci, [ci, vp, ctypes.POINTER(ctypes.c_double), vp])
         for n in ("tsm_conv_workspace_bytes", "tsm_block_saved_bytes", "tsm_block_workspace_bytes", "tsm_block_infer_workspace_bytes",
-                  "tsm_resnet50_workspace_bytes", "tsm_resnet50_infer_workspace_bytes"):
+                  "tsm_resnet50_workspace_bytes", "tsm_resnet50_infer_workspace_bytes", "tsm_recur_saved_bytes",
+                  "tsm_recur_workspace_bytes", "tsm_layernorm_workspace_bytes", "tsm_xent_workspace_bytes"):
             sig(n, sz, [vp])
         sig("tsm_resnet50_param_count", ctypes.c_int64, [ci])
         sig("tsm_resnet50_num_tensors", ci, [])
@@ -112,6 +128,12 @@ def lib():
                                                   ctypes.POINTER(ci)])
         sig("tsm_resnet50_infer", ci, [vp, vp, vp, vp, vp, vp, sz, vp])
         sig("tsm_resnet50_accum_step", ci, [vp, vp, vp, vp, vp, vp, vp, vp, vp, ci, ci, vp, sz, vp])
+        sig("tsm_recur_fwd", ci, [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp])
+        sig("tsm_recur_bwd", ci, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp])
+        sig("tsm_layernorm_fwd", ci, [vp, vp, vp, vp, vp, vp, vp, vp])
+        sig("tsm_layernorm_bwd", ci, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp])
+        sig("tsm_xent_fwd", ci, [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp])
+        sig("tsm_xent_bwd", ci, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp])
         sig("tsm_lr_schedule", ctypes.c_double, [ctypes.c_double, ci, ci, ctypes.c_double, ctypes.c_double])
         _LIB = L
     return _LIB
@@ -322,3 +344,54 @@ def tsm_lr_schedule(epoch, total_batch, warm_batch=8, warmup_epochs=5.0, total_e
     if v < 0:
         _check(-2)
     return v
+
+
+def tsm_recur_saved_bytes(desc):
+    return int(lib().tsm_recur_saved_bytes(ctypes.addressof(desc)))
+
+
+def tsm_recur_workspace_bytes(desc):
+    return int(lib().tsm_recur_workspace_bytes(ctypes.addressof(desc)))
+
+
+def tsm_recur_fwd(desc, x, g, h0, y, h_last, saved, ws, stream=None):
+    p, n = _ws(ws)
+    _check(lib().tsm_recur_fwd(ctypes.addressof(desc), _ptr(x), _ptr(g), _ptr(h0), _ptr(y), _ptr(h_last), _ptr(saved), p, n,
+                               _stream(stream)))
+
+
+def tsm_recur_bwd(desc, x, g, h0, saved, dy, dh_last, dx, dg, dh0, ws, stream=None):
+    p, n = _ws(ws)
+    _check(lib().tsm_recur_bwd(ctypes.addressof(desc), _ptr(x), _ptr(g), _ptr(h0), _ptr(saved), _ptr(dy), _ptr(dh_last),
+                               _ptr(dx), _ptr(dg), _ptr(dh0), p, n, _stream(stream)))
+
+
+def tsm_layernorm_workspace_bytes(desc):
+    return int(lib().tsm_layernorm_workspace_bytes(ctypes.addressof(desc)))
+
+
+def tsm_layernorm_fwd(desc, x, gamma, beta, y, mean, rstd, stream=None):
+    _check(lib().tsm_layernorm_fwd(ctypes.addressof(desc), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd),
+                                   _stream(stream)))
+
+
+def tsm_layernorm_bwd(desc, x, dy, gamma, mean, rstd, dx, dgamma, dbeta, ws, stream=None):
+    p, n = _ws(ws)
+    _check(lib().tsm_layernorm_bwd(ctypes.addressof(desc), _ptr(x), _ptr(dy), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dx),
+                                   _ptr(dgamma), _ptr(dbeta), p, n, _stream(stream)))
+
+
+def tsm_xent_workspace_bytes(desc):
+    return int(lib().tsm_xent_workspace_bytes(ctypes.addressof(desc)))
+
+
+def tsm_xent_fwd(desc, x, w, bias, labels, loss, lse, ws, stream=None):
+    p, n = _ws(ws)
+    _check(lib().tsm_xent_fwd(ctypes.addressof(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), _ptr(loss), _ptr(lse), p, n,
+                              _stream(stream)))
+
+
+def tsm_xent_bwd(desc, x, w, bias, labels, lse, dloss, dx, dw, dbias, ws, stream=None):
+    p, n = _ws(ws)
+    _check(lib().tsm_xent_bwd(ctypes.addressof(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), _ptr(lse), _ptr(dloss),
+                              _ptr(dx), _ptr(dw), _ptr(dbias), p, n, _stream(stream)))

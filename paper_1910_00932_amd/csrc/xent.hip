@@ -1,0 +1,392 @@
+// Linear classifier with softmax cross entropy whose logits are never stored, and its gradients.
+//
+//   s = x w^T + b;  lse_r = log sum_v exp s_rv;  loss_r = lse_r - s_r,label  (0 for rows whose label is no class)
+//   G_rv = dloss_r (exp(s_rv - lse_r) - [v == label_r]);  dx = G w;  dw = G^T x;  db_v = sum_r G_rv
+//
+// Forward: tiles of s stay in registers; each leaves the maximum and the sum of exponentials of its columns per row (a softmax
+// joined over the tiles) and the label's logit.  Backward: s is formed again in pieces of the classes, a piece of G in the storage
+// type lives in the workspace for the two products that read it.  G is rounded once to the storage type, as the operands of the
+// matrix cores are; lse, the losses, db (from G before that rounding) and all sums are fp32.
+#include "internal.h"
+#include "args.h"
+#include "vec_any.h"
+
+namespace tsm {
+
+typedef float x_f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 x_bf16x8 __attribute__((ext_vector_type(8)));
+
+struct XentEpi {
+    // STATS
+    float2* part;            // [N tiles][M]: maximum and sum of exp(s - maximum) of a tile's columns
+    float* picked;           // [M]: the label's logit
+    // STATS and GRAD: columns are classes col0 + n of `classes`
+    const float* bias;
+    const int32_t* labels;
+    long col0, classes;
+    // GRAD
+    const float *lse, *dloss;
+    void* G;                 // [M][ldg], zero behind the last column
+    long ldg;
+    float* dbias_part;       // [M tiles][ldg], nullable
+    // OUT
+    const float* acc;        // fp32 [M][N] added to the result, nullable
+    float* out_f32;          // [splits][M][N], or
+    void* out;               // [M][N] in the storage type
+};
+
+struct XentArgs {
+    const void *A, *B;
+    long lda, ldb, M, N, K, ksplit;    // ksplit: K of one split (grid.z)
+    const int32_t* klabels;            // rows k of B whose label is no class of `classes` count as zero; nullable
+    XentEpi e;
+};
+
+enum { XE_STATS = 0, XE_GRAD = 1, XE_OUT = 2 };
+
+__device__ __forceinline__ bool is_class(int label, long classes) { return label >= 0 && label < classes; }
+
+// exp(v - m) with exp(-inf - -inf) = 0: a column without any weight
+__device__ __forceinline__ float exp_below(float v, float m) { return v == -__builtin_inff() && v == m ? 0.f : __expf(v - m); }
+// joins (m, s) with (m2, s2)
+__device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float s2) {
+    const float t = fmaxf(m, m2);
+    s = (m == t ? s : s * __expf(m - t)) + (m2 == t ? s2 : s2 * __expf(m2 - t));
+    m = t;
+}
+
+// ---- the plain tile: 64 x 64 results, the four wavefronts take every fourth step of K ---------------------------------
+// AK / BK: the operand has K consecutive in memory ([rows][K]), else its rows are K ([K][rows]).
+template <typename T, bool KC>
+__device__ __forceinline__ void plain_frag(const T* P, long ld, long row, long rows, long k, long K, const int32_t* klabels, long classes,
+                                           typename RawVec<T, 16 / sizeof(T)>::type& f) {
+    constexpr int VE = 16 / sizeof(T);
+    if constexpr (KC) {
+        f = raw_load<T, VE>(P + row * ld + k, row < rows ? (int)(K - k < VE ? K - k : VE) : 0);
+    } else {
+        f = typename RawVec<T, VE>::type{};
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+            if (row < rows && k + e < K && (!klabels || is_class(klabels[k + e], classes))) {
+                if constexpr (sizeof(T) == 2) f[e >> 1] |= (uint32_t)P[(k + e) * ld + row] << (16 * (e & 1));
+                else f[e] = __float_as_uint(P[(k + e) * ld + row]);
+            }
+        }
+    }
+}
+
+template <typename T, int MODE, bool AK, bool BK>
+__global__ void __launch_bounds__(256) xent_plain_kernel(XentArgs a) {
+    constexpr int VE = 16 / sizeof(T), KSTEP = 2 * VE;
+    __shared__ float red[4][64][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hi = lane >> 5, lo = lane & 31;
+    const long ntiles = (a.N + 63) / 64, total = ntiles * ((a.M + 63) / 64);
+    const long kb = blockIdx.z * a.ksplit, ke = kb + a.ksplit < a.K ? kb + a.ksplit : a.K;
+    const T *A = (const T*)a.A, *B = (const T*)a.B;
+    for (long tile = blockIdx.x; tile < total; tile += gridDim.x) {
+    const long mt = tile / ntiles, nt = tile % ntiles;
+    const long m0 = mt * 64, n0 = nt * 64;
+    x_f32x16 acc[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    for (long k0 = kb + wave * KSTEP; k0 < ke; k0 += 4 * KSTEP) {
+        typename RawVec<T, VE>::type fa[2], fb[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            plain_frag<T, AK>(A, a.lda, m0 + 32 * i + lo, a.M, k0 + hi * VE, ke, nullptr, 0, fa[i]);
+            plain_frag<T, BK>(B, a.ldb, n0 + 32 * i + lo, a.N, k0 + hi * VE, ke, a.klabels, a.e.classes, fb[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if constexpr (sizeof(T) == 2)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x_bf16x8, fa[i]), __builtin_bit_cast(x_bf16x8, fb[j]), acc[i][j], 0, 0, 0);
+                else
+#pragma unroll
+                    for (int e = 0; e < VE; ++e)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[i][e]), __uint_as_float(fb[j][e]), acc[i][j], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) red[wave][i * 32 + 8 * (r / 4) + 4 * hi + r % 4][j * 32 + lo] = acc[i][j][r];
+    __syncthreads();
+    // one row of the tile at a time per wavefront, a column per lane
+    const long n = n0 + lane;
+    const long v = a.e.col0 + n;
+    const bool in = n < a.N;
+    const float bias = MODE != XE_OUT && in && a.e.bias ? a.e.bias[v] : 0.f;
+    float dbias = 0.f;
+    for (int q = 0; q < 16; ++q) {
+        const int row = wave * 16 + q;
+        const long m = m0 + row;
+        if (m >= a.M) break;
+        float s = (red[0][row][lane] + red[1][row][lane]) + (red[2][row][lane] + red[3][row][lane]);
+        if constexpr (MODE == XE_STATS) {
+            s = in ? s + bias : -__builtin_inff();
+            if (in && a.e.labels[m] == v) a.e.picked[m] = s;
+            float mx = s;
+            for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+            float t = in ? exp_below(s, mx) : 0.f;
+            for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
+            if (lane == 0) a.e.part[nt * a.M + m] = make_float2(mx, t);
+        } else if constexpr (MODE == XE_GRAD) {
+            const int label = a.e.labels[m];
+            float g = 0.f;
+            if (in && is_class(label, a.e.classes)) {
+                const float p = __expf(s + bias - a.e.lse[m]);
+                g = a.e.dloss[m] * (label == v ? p - 1.f : p);
+            }
+            dbias += g;
+            if (n < a.e.ldg) ((T*)a.e.G)[m * a.e.ldg + n] = Elem<T>::st(g);
+        } else if (in) {
+            if (a.e.acc) s += a.e.acc[m * a.N + n];
+            if (a.e.out_f32) a.e.out_f32[(blockIdx.z * a.M + m) * a.N + n] = s;
+            else ((T*)a.e.out)[m * a.N + n] = Elem<T>::st(s);
+        }
+    }
+    if constexpr (MODE == XE_GRAD) {
+        if (a.e.dbias_part) {
+            __syncthreads();
+            red[0][wave][lane] = dbias;
+            __syncthreads();
+            if (wave == 0 && in) a.e.dbias_part[mt * a.e.ldg + n] = (red[0][0][lane] + red[0][1][lane]) + (red[0][2][lane] + red[0][3][lane]);
+        }
+    }
+    __syncthreads();
+    }
+}
+
+// lse and loss of a row from its tiles: one wavefront per row
+__global__ void __launch_bounds__(256) xent_finish_kernel(const float2* __restrict__ part, const float* __restrict__ picked,
+                                                          const int32_t* __restrict__ labels, float* __restrict__ loss, float* __restrict__ lse,
+                                                          long M, long ntiles, long classes) {
+    const int lane = threadIdx.x & 63;
+    for (long m = (long)blockIdx.x * 4 + (threadIdx.x >> 6); m < M; m += (long)gridDim.x * 4) {
+        float mx = -__builtin_inff(), s = 0.f;
+        for (long t = lane; t < ntiles; t += 64) {
+            const float2 p = part[t * M + m];
+            join_softmax(mx, s, p.x, p.y);
+        }
+        for (int o = 32; o > 0; o >>= 1) {
+            const float m2 = __shfl_xor(mx, o, 64), s2 = __shfl_xor(s, o, 64);
+            join_softmax(mx, s, m2, s2);
+        }
+        if (lane == 0) {
+            const float l = mx + logf(s);
+            lse[m] = l;
+            loss[m] = is_class(labels[m], classes) ? l - picked[m] : 0.f;
+        }
+    }
+}
+
+// out[c] = sum of the rows of part [rows][ld]
+__global__ void __launch_bounds__(256) xent_colsum_kernel(const float* __restrict__ part, long rows, long ld, long n, float* __restrict__ out) {
+    const long c = (long)blockIdx.x * 256 + threadIdx.x;
+    if (c >= n) return;
+    float s = 0.f;
+    for (long r = 0; r < rows; ++r) s += part[r * ld + c];
+    out[c] = s;
+}
+
+// out = sum of the splits' results, rounded once
+template <typename T>
+__global__ void __launch_bounds__(256) xent_join_kernel(const float* __restrict__ part, int splits, long n, T* __restrict__ out) {
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
+        float s = 0.f;
+        for (int z = 0; z < splits; ++z) s += part[z * n + i];
+        out[i] = Elem<T>::st(s);
+    }
+}
+
+// ---- host --------------------------------------------------------------------------------
+struct XentPlan {
+    long piece, pieces, ldg;      // classes of a piece of G, number of pieces, row pitch of G
+    long ntiles;                  // column tiles of the forward pass
+    long mtiles;                  // row tiles of G
+    int zdx, zdw;                 // splits of K of the two products
+    size_t fwd_bytes, bwd_bytes;
+    size_t o_part, o_picked, o_G, o_acc, o_dw, o_dbias;
+};
+
+static constexpr size_t XENT_G_BYTES = (size_t)512 << 20;   // of a piece of G, at most (a piece has 1024 classes at least)
+
+static int splits_of(long tiles, long K) {
+    long z = tiles < 512 ? 512 / tiles : 1;
+    const long most = K / 512 > 1 ? K / 512 : 1;
+    if (z > most) z = most;
+    return (int)(z > 64 ? 64 : z);
+}
+
+static XentPlan xent_plan(const tsm_xent_desc* d) {
+    XentPlan p{};
+    const long R = d->rows, D = d->features, V = d->classes, es = (long)dtype_size(d->dtype);
+    p.ntiles = (V + 63) / 64;
+    p.mtiles = (R + 63) / 64;
+    Arena f(nullptr, 0);
+    p.o_part = f.used; f.take((size_t)p.ntiles * R * 8);
+    p.o_picked = f.used; f.take((size_t)R * 4);
+    p.fwd_bytes = f.used;
+    long piece = (long)(XENT_G_BYTES / es) / R / 1024 * 1024;
+    if (piece < 1024) piece = 1024;
+    if (piece > V) piece = V;
+    p.piece = piece;
+    p.pieces = (V + piece - 1) / piece;
+    p.ldg = (piece + 7) / 8 * 8;
+    const long dt = (D + 63) / 64;
+    p.zdx = p.pieces > 1 ? 1 : splits_of(p.mtiles * dt, V);
+    p.zdw = splits_of((piece + 63) / 64 * dt, R);
+    Arena b(nullptr, 0);
+    p.o_G = b.used; b.take((size_t)R * p.ldg * es);
+    p.o_acc = b.used; b.take(p.pieces > 1 || p.zdx > 1 ? (size_t)p.zdx * R * D * 4 : 0);
+    p.o_dw = b.used; b.take(p.zdw > 1 ? (size_t)p.zdw * piece * D * 4 : 0);
+    p.o_dbias = b.used; b.take((size_t)p.mtiles * p.ldg * 4);
+    p.bwd_bytes = b.used;
+    return p;
+}
+
+static int xent_check(const tsm_xent_desc* d, const char* who) {
+    if (!d) return fail(TSM_ERR_NULLPTR, "%s: null descriptor", who);
+    if (d->dtype != TSM_F32 && d->dtype != TSM_BF16) return fail(TSM_ERR_DTYPE, "%s: unknown dtype %d", who, d->dtype);
+    if (d->rows <= 0 || d->features <= 0 || d->classes <= 0) return fail(TSM_ERR_SHAPE, "%s: non-positive dimension", who);
+    if ((double)d->rows * d->features > 1e14 || (double)d->classes * d->features > 1e14) return fail(TSM_ERR_SHAPE, "%s: tensor too large", who);
+    return TSM_OK;
+}
+
+static size_t xent_ws(const XentPlan& p) { return p.fwd_bytes > p.bwd_bytes ? p.fwd_bytes : p.bwd_bytes; }
+
+template <typename T, int MODE, bool AK, bool BK>
+static int xent_product(const XentArgs& a, int splits, const char* what, hipStream_t s) {
+    XentArgs b = a;
+    const long nt = (a.N + 63) / 64, mt = (a.M + 63) / 64;
+    b.ksplit = ((a.K + splits - 1) / splits + 63) / 64 * 64;
+    xent_plain_kernel<T, MODE, AK, BK><<<dim3((unsigned)(nt * mt < 65536 ? nt * mt : 65536), 1, (unsigned)splits), dim3(256), 0, s>>>(b);
+    return check_launch(what);
+}
+
+template <typename T>
+static int xent_join(const float* part, int splits, long n, void* out, const char* what, hipStream_t s) {
+    const long blocks = (n + 255) / 256;
+    xent_join_kernel<T><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s>>>(part, splits, n, (T*)out);
+    return check_launch(what);
+}
+
+template <typename T>
+static int xent_fwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, const void* w, const float* bias, const int32_t* labels, float* loss,
+                    float* lse, char* ws, hipStream_t s) {
+    XentArgs a{};
+    a.A = x; a.B = w;
+    a.lda = a.ldb = a.K = d->features;
+    a.M = d->rows; a.N = d->classes;
+    a.e.part = (float2*)(ws + p.o_part);
+    a.e.picked = (float*)(ws + p.o_picked);
+    a.e.bias = bias; a.e.labels = labels; a.e.classes = d->classes;
+    TSM_TRY((xent_product<T, XE_STATS, true, true>(a, 1, "xent_stats", s)));
+    const long blocks = (a.M + 3) / 4;
+    xent_finish_kernel<<<dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s>>>(a.e.part, a.e.picked, labels, loss, lse, a.M, p.ntiles, d->classes);
+    return check_launch("xent_finish");
+}
+
+template <typename T>
+static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, const void* w, const float* bias, const int32_t* labels,
+                    const float* lse, const float* dloss, void* dx, void* dw, float* dbias, char* ws, hipStream_t s) {
+    const long R = d->rows, D = d->features, V = d->classes;
+    void* G = ws + p.o_G;
+    float *acc = (float*)(ws + p.o_acc), *dwp = (float*)(ws + p.o_dw), *dbp = (float*)(ws + p.o_dbias);
+    for (long c = 0; c < p.pieces; ++c) {
+        const long v0 = c * p.piece, n = V - v0 < p.piece ? V - v0 : p.piece;
+        const T* wc = (const T*)w + v0 * D;
+        XentArgs a{};
+        a.A = x; a.B = wc;
+        a.lda = a.ldb = a.K = D;
+        a.M = R; a.N = n;
+        a.e.bias = bias; a.e.labels = labels; a.e.classes = V; a.e.col0 = v0;
+        a.e.lse = lse; a.e.dloss = dloss; a.e.G = G; a.e.ldg = p.ldg; a.e.dbias_part = dbias ? dbp : nullptr;
+        TSM_TRY((xent_product<T, XE_GRAD, true, true>(a, 1, "xent_grad", s)));
+        if (dbias) {
+            xent_colsum_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(dbp, p.mtiles, p.ldg, n, dbias + v0);
+            TSM_TRY(check_launch("xent_dbias"));
+        }
+        if (dx) {
+            XentArgs b{};
+            b.A = G; b.lda = p.ldg; b.B = wc; b.ldb = D;
+            b.M = R; b.N = D; b.K = n;
+            b.e.acc = c > 0 ? acc : nullptr;
+            if (p.zdx > 1 || c + 1 < p.pieces) b.e.out_f32 = acc;
+            else b.e.out = dx;
+            TSM_TRY((xent_product<T, XE_OUT, true, false>(b, p.zdx, "xent_dx", s)));
+            if (p.zdx > 1) TSM_TRY(xent_join<T>(acc, p.zdx, R * D, dx, "xent_dx_join", s));
+        }
+        if (dw) {
+            XentArgs b{};
+            b.A = G; b.lda = p.ldg; b.B = x; b.ldb = D;
+            b.M = n; b.N = D; b.K = R;
+            b.klabels = labels; b.e.classes = V;
+            T* out = (T*)dw + v0 * D;
+            if (p.zdw > 1) b.e.out_f32 = dwp;
+            else b.e.out = out;
+            TSM_TRY((xent_product<T, XE_OUT, false, false>(b, p.zdw, "xent_dw", s)));
+            if (p.zdw > 1) TSM_TRY(xent_join<T>(dwp, p.zdw, n * D, out, "xent_dw_join", s));
+        }
+    }
+    return TSM_OK;
+}
+
+}  // namespace tsm
+
+using namespace tsm;
+
+extern "C" {
+
+size_t tsm_xent_workspace_bytes(const tsm_xent_desc* d) {
+    return xent_check(d, "tsm_xent_workspace_bytes") == TSM_OK ? xent_ws(xent_plan(d)) : 0;
+}
+
+int tsm_xent_fwd(const tsm_xent_desc* d, const void* x, const void* w, const float* bias, const int32_t* labels, float* loss, float* lse, void* ws,
+                 size_t ws_bytes, void* stream) {
+    const char* who = "tsm_xent_fwd";
+    TSM_TRY(xent_check(d, who));
+    if (!x || !w || !labels || !loss || !lse) return fail(TSM_ERR_NULLPTR, "%s: null pointer", who);
+    const XentPlan p = xent_plan(d);
+    const size_t need = xent_ws(p);
+    if (ws_bytes < need) return fail(TSM_ERR_WORKSPACE, "%s: workspace %zu bytes, need %zu", who, ws_bytes, need);
+    if (!ws) return fail(TSM_ERR_NULLPTR, "%s: null workspace", who);
+    const size_t es = dtype_size(d->dtype), rb = (size_t)d->rows * 4;
+    const Span in[] = {{x, (size_t)d->rows * d->features * es, "x"}, {w, (size_t)d->classes * d->features * es, "w"},
+                       {bias, (size_t)d->classes * 4, "bias"}, {labels, rb, "labels"}};
+    const Span out[] = {{loss, rb, "loss"}, {lse, rb, "lse"}, {ws, need, "the workspace"}};
+    TSM_TRY(check_spans(who, in, 4, out, 3));
+    const hipStream_t s = (hipStream_t)stream;
+    return d->dtype == TSM_BF16 ? xent_fwd<bf16_t>(d, p, x, w, bias, labels, loss, lse, (char*)ws, s)
+                                : xent_fwd<float>(d, p, x, w, bias, labels, loss, lse, (char*)ws, s);
+}
+
+int tsm_xent_bwd(const tsm_xent_desc* d, const void* x, const void* w, const float* bias, const int32_t* labels, const float* lse,
+                 const float* dloss, void* dx, void* dw, float* dbias, void* ws, size_t ws_bytes, void* stream) {
+    const char* who = "tsm_xent_bwd";
+    TSM_TRY(xent_check(d, who));
+    if (!x || !w || !labels || !lse || !dloss) return fail(TSM_ERR_NULLPTR, "%s: null pointer", who);
+    if (!dx && !dw && !dbias) return fail(TSM_ERR_NULLPTR, "%s: no gradient asked for", who);
+    const XentPlan p = xent_plan(d);
+    const size_t need = xent_ws(p);
+    if (ws_bytes < need) return fail(TSM_ERR_WORKSPACE, "%s: workspace %zu bytes, need %zu", who, ws_bytes, need);
+    if (!ws) return fail(TSM_ERR_NULLPTR, "%s: null workspace", who);
+    const size_t es = dtype_size(d->dtype), rb = (size_t)d->rows * 4;
+    const size_t xb = (size_t)d->rows * d->features * es, wb = (size_t)d->classes * d->features * es, bb = (size_t)d->classes * 4;
+    const Span in[] = {{x, xb, "x"}, {w, wb, "w"}, {bias, bb, "bias"}, {labels, rb, "labels"}, {lse, rb, "lse"}, {dloss, rb, "dloss"}};
+    const Span out[] = {{dx, xb, "dx"}, {dw, wb, "dw"}, {dbias, bb, "dbias"}, {ws, need, "the workspace"}};
+    TSM_TRY(check_spans(who, in, 6, out, 4));
+    const hipStream_t s = (hipStream_t)stream;
+    return d->dtype == TSM_BF16 ? xent_bwd<bf16_t>(d, p, x, w, bias, labels, lse, dloss, dx, dw, dbias, (char*)ws, s)
+                                : xent_bwd<float>(d, p, x, w, bias, labels, lse, dloss, dx, dw, dbias, (char*)ws, s);
+}
+
+}  // extern "C"

@@ -1,0 +1,183 @@
+"""The gated recurrence over frames against its definition in 64 bits.
+
+Bounds.  A step rounds its gate (a, 1 - a: relative error at most 4 units of 2^-24), a product and a sum: at most 8 units of the
+largest value X a column holds (a state is a mean of inputs).  Errors pass on with factors of at most 1, so a state is off by at
+most F = 8 T units of X, joined in whatever order; a result is rounded once more.  The same holds for D with the recurrence
+of |dy| in place of the states."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import head_oracle as H
+from paper_1910_00932_amd import binding as B
+from head_util import CDT, HALF, U, Guarded, scratch, values, within
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [  # N, T, C, H, W -- what it is for
+    (1, 1, 1, 1, 1),          # one value
+    (1, 1, 48, 3, 3),         # one new frame of a stream
+    (2, 8, 64, 5, 5),         # the usual eight frames: one segment
+    (3, 7, 13, 3, 3),         # odd columns, rows at any alignment
+    (2, 9, 17, 1, 3),         # the first length of four segments
+    (1, 32, 66, 1, 1),        # ... and the last
+    (2, 33, 5, 1, 1),         # the first of many segments
+    (1, 128, 10, 1, 1), (1, 129, 10, 1, 1),     # with and without a saved state
+    (5, 200, 130, 5, 5),      # 16 segments, the last tile partly filled
+    (2, 256, 34, 1, 1), (2, 257, 34, 1, 1),     # ends of a tile of 32 segments
+    (1, 1500, 67, 1, 1),      # spans of the time axis, ragged in both
+    (3, 700, 9, 7, 1),
+]
+
+
+def _run(shape, dtype, state, gate_shift=1.0, x=None, g=None):
+    N, T, C, Hh, W = shape
+    M = C * Hh * W
+    d = B.RecurDesc(N=N, T=T, C=C, H=Hh, W=W, dtype=CDT[dtype])
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    xd, xn = values((N, T, M), 0, dtype) if x is None else x
+    gd, gn = values((N, T, M), 1, dtype, shift=gate_shift) if g is None else g
+    dyd, dyn = values((N, T, M), 2, dtype)
+    h0d, h0n = values((N, M), 3, "f32") if state else (None, None)
+    dld, dln = values((N, M), 4, "f32") if state else (None, None)
+    y, hl = Guarded((N, T, M), dt), Guarded((N, M), torch.float32)
+    saved, ws = scratch(B.tsm_recur_saved_bytes(d)), scratch(B.tsm_recur_workspace_bytes(d))
+    B.tsm_recur_fwd(d, xd, gd, h0d, y.t, hl.t, saved, ws)
+    dx, dg, dh0 = Guarded((N, T, M), dt), Guarded((N, T, M), dt), Guarded((N, M), torch.float32)
+    B.tsm_recur_bwd(d, xd, gd, h0d, saved, dyd, dld, dx.t, dg.t, dh0.t, ws)
+    torch.cuda.synchronize()
+    return (xn, gn, h0n, dyn, dln), [v.np() for v in (y, hl, dx, dg, dh0)]
+
+
+@pytest.mark.parametrize("state", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_forward_and_backward(shape, dtype, state):
+    T = shape[1]
+    (x, g, h0, dy, dl), (y, hl, dx, dg, dh0) = _run(shape, dtype, state)
+    h = H.recur_fwd(x, g, h0)
+    rdx, rdg, rdh0 = H.recur_bwd(x, g, h0, dy, dl)
+    X = max(np.abs(x).max(), 0 if h0 is None else np.abs(h0).max())
+    F = 8 * T * U * X
+    within(y, h, F + HALF[dtype] * np.abs(h), "y")
+    within(hl, h[:, -1], F, "h_last")
+    a = H.sigmoid(g)
+    Dabs = np.abs(dy).copy()                       # the recurrence of |dy|
+    e = np.zeros_like(Dabs[:, 0]) if dl is None else np.abs(dl)
+    for t in reversed(range(T)):
+        Dabs[:, t] += e
+        e = a[:, t] * Dabs[:, t]
+    E = 8 * T * U * Dabs.max()
+    within(dx, rdx, E + HALF[dtype] * np.abs(rdx), "dx")
+    within(dg, rdg, E * X + Dabs * F + 8 * U * Dabs * X + HALF[dtype] * np.abs(rdg), "dg")
+    within(dh0, rdh0, E, "dh0")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gates_at_their_ends(dtype):
+    """Gates that keep all, take all, and values far out, in one column after the other."""
+    shape = (1, 40, 12, 1, 1)
+    xd, xn = values((1, 40, 12), 5, dtype)
+    g = np.tile(np.array([np.inf, -np.inf, 200.0, -200.0, 60.0, -60.0, 0.0, 15.0, -15.0, 1e-3, 30.0, -30.0], np.float32), (1, 40, 1))
+    gt = torch.from_numpy(g).to(xd.dtype)
+    (x, gn, h0, dy, dl), (y, hl, dx, dg, dh0) = _run(shape, dtype, True, x=(xd, xn), g=(gt.cuda(), gt.double().numpy()))
+    h = H.recur_fwd(x, gn, h0)
+    X = max(np.abs(x).max(), np.abs(h0).max())
+    within(y, h, 8 * 40 * U * X + HALF[dtype] * np.abs(h), "y")
+    rdx, rdg, rdh0 = H.recur_bwd(x, gn, h0, dy, dl)
+    S = np.abs(dy).sum(1).max() + np.abs(dl).max()
+    within(dh0, rdh0, 8 * 40 * U * S, "dh0")
+    within(dx, rdx, 8 * 40 * U * S + HALF[dtype] * np.abs(rdx), "dx")
+    within(dg, rdg, 3 * 8 * 40 * U * S * X + HALF[dtype] * np.abs(rdg), "dg")
+
+
+def test_a_bad_value_stays_in_its_column():
+    xd, xn = values((2, 150, 24), 6, "f32")
+    gd, gn = values((2, 150, 24), 7, "f32")
+    xd[0, 70, 5] = float("nan")
+    xn[0, 70, 5] = np.nan
+    (x, g, h0, dy, dl), (y, hl, dx, dg, dh0) = _run((2, 150, 24, 1, 1), "f32", False, x=(xd, xn), g=(gd, gn))
+    h = H.recur_fwd(x, g)
+    within(y, h, 8 * 150 * U * np.nanmax(np.abs(x)), "y")
+    assert np.isfinite(y[0, :70, 5]).all() and np.isnan(y[0, 70:, 5]).all()
+    assert np.isfinite(dx).all() and np.isnan(dg[0, 70:, 5]).all() and np.isfinite(dg[0, :70, 5]).all()
+
+
+@pytest.mark.parametrize("shape", [(2, 12, 40, 3, 3), (1, 700, 20, 1, 1)])
+def test_clip_by_clip_and_frame_by_frame(shape):
+    """A clip served in pieces, the state carried in place (h_last is h0), gives what one call gives."""
+    N, T, C, Hh, W = shape
+    M = C * Hh * W
+    xd, _ = values((N, T, M), 0, "f32")
+    gd, _ = values((N, T, M), 1, "f32", shift=1.0)
+    whole = Guarded((N, T, M), torch.float32)
+    d = B.RecurDesc(N=N, T=T, C=C, H=Hh, W=W, dtype=B.TSM_F32)
+    state0, _ = values((N, M), 3, "f32")
+    last = state0.clone()
+    ws = scratch(B.tsm_recur_workspace_bytes(d))
+    B.tsm_recur_fwd(d, xd, gd, last, whole.t, last, None, ws)            # in place, also where the time axis is split
+    state = state0.clone()
+    cuts = [0, 1, 2, T // 2, T]
+    for a, b in zip(cuts, cuts[1:]):
+        dp = B.RecurDesc(N=N, T=b - a, C=C, H=Hh, W=W, dtype=B.TSM_F32)
+        y = torch.empty((N, b - a, M), device="cuda")
+        B.tsm_recur_fwd(dp, xd[:, a:b].contiguous(), gd[:, a:b].contiguous(), state, y, state, None, scratch(B.tsm_recur_workspace_bytes(dp)))
+        within(y.double().cpu().numpy(), whole.np()[:, a:b], 2 * 8 * T * U * 5, "piece %d:%d" % (a, b))
+    within(state.double().cpu().numpy(), last.double().cpu().numpy(), 2 * 8 * T * U * 5, "state")
+
+
+def test_same_bits_twice_and_on_another_stream():
+    shape = (2, 900, 50, 1, 1)
+    first = _run(shape, "bf16", True)[1]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        second = _run(shape, "bf16", True)[1]
+    s.synchronize()
+    for a, b in zip(first, second):
+        assert np.array_equal(a, b)
+
+
+def test_states_and_saved_are_optional():
+    N, T, M = 2, 300, 20
+    d = B.RecurDesc(N=N, T=T, C=M, H=1, W=1, dtype=B.TSM_F32)
+    xd, x = values((N, T, M), 0, "f32")
+    gd, g = values((N, T, M), 1, "f32")
+    dyd, dy = values((N, T, M), 2, "f32")
+    y = Guarded((N, T, M), torch.float32)
+    ws = scratch(B.tsm_recur_workspace_bytes(d))
+    B.tsm_recur_fwd(d, xd, gd, None, y.t, None, None, ws)
+    within(y.np(), H.recur_fwd(x, g), 8 * T * U * 5, "y")
+    saved = scratch(B.tsm_recur_saved_bytes(d))
+    B.tsm_recur_fwd(d, xd, gd, None, y.t, None, saved, ws)
+    dx, dg = Guarded((N, T, M), torch.float32), Guarded((N, T, M), torch.float32)
+    B.tsm_recur_bwd(d, xd, gd, None, saved, dyd, None, dx.t, dg.t, None, ws)
+    rdx, rdg, _ = H.recur_bwd(x, g, None, dy)
+    within(dx.np(), rdx, 8 * T * U * 50, "dx")
+    within(dg.np(), rdg, 8 * T * U * 400, "dg")
+
+
+def test_gradient_is_that_of_the_kernels_own_forward():
+    """Differences of the library's forward pass along one direction: central, fp32.  The loss is a sum of n products of values
+    of order 1; its rounding error is at most about sqrt(n) * 2^-22, over 2e-2, and the third-order term 1e-4 of the slope's scale."""
+    N, T, M = 1, 150, 8
+    d = B.RecurDesc(N=N, T=T, C=M, H=1, W=1, dtype=B.TSM_F32)
+    xd, _ = values((N, T, M), 0, "f32")
+    gd, _ = values((N, T, M), 1, "f32")
+    dyd, dy = values((N, T, M), 2, "f32")
+    ux, _ = values((N, T, M), 8, "f32")
+    ug, _ = values((N, T, M), 9, "f32")
+    ws, saved = scratch(B.tsm_recur_workspace_bytes(d)), scratch(B.tsm_recur_saved_bytes(d))
+
+    def loss(x, g):
+        y = torch.empty_like(x)
+        B.tsm_recur_fwd(d, x, g, None, y, None, saved, ws)
+        return float((y.double() * dyd.double()).sum())
+    h = 1e-2
+    slope = (loss(xd + h * ux, gd + h * ug) - loss(xd - h * ux, gd - h * ug)) / (2 * h)
+    loss(xd, gd)
+    dx, dg = torch.empty_like(xd), torch.empty_like(xd)
+    B.tsm_recur_bwd(d, xd, gd, None, saved, dyd, None, dx, dg, None, ws)
+    want = float((dx.double() * ux.double()).sum() + (dg.double() * ug.double()).sum())
+    scale = float(np.sqrt((dx.double() ** 2).sum().item() + (dg.double() ** 2).sum().item()))
+    assert abs(slope - want) < 1e-2 * scale, (slope, want, scale)

@@ -1,0 +1,235 @@
+"""The linear classifier with softmax cross entropy against its definition in 64 bits.
+
+Bounds.  A logit is a sum of D products (exact in fp32 for bf16 operands) accumulated in fp32 in some order: off by at most
+d = (4 sqrt(D) + 16) units of 2^-24 of S = sum |x||w| + |b| (four standard deviations of D roundings).  lse is off by the largest
+such error, 16 units for the exponentials' and the logarithm's own, and (4 sqrt(V) + 16) for the sum over the classes; p by twice that
+relative to p.  In bf16 an entry of G is rounded once more (half a unit of 2^-7), and so is a result.  fp32 and bf16 hold no normal
+number below 2^-126: what is smaller may become zero."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import head_oracle as H
+from paper_1910_00932_amd import binding as B
+from head_util import CDT, HALF, TDT, U, Guarded, scratch, values, within
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [  # rows, features, classes
+    (1, 1, 1), (1, 2048, 400), (4, 64, 2), (3, 5, 7), (64, 128, 400), (65, 72, 129), (130, 96, 255), (256, 64, 256), (257, 200, 257),
+    (300, 33, 513), (31, 1000, 1000), (520, 264, 770), (16, 320, 5000), (1030, 40, 300), (700, 256, 1500), (8, 520, 20000), (2, 100, 70001),
+    (2500, 24, 16), (5000, 136, 40),
+]
+
+
+def _labels(rows, classes, seed, ignored):
+    rng = np.random.default_rng(seed)
+    lab = rng.integers(0, classes, rows).astype(np.int32)
+    if ignored:
+        drop = rng.random(rows) < 0.3
+        lab[drop] = rng.choice(np.array([-1, -100, classes, 2 ** 31 - 1], np.int64), drop.sum()).astype(np.int32)
+    return lab
+
+
+def _run(rows, D, V, dtype, bias, labels, x=None, w=None, want=("dx", "dw", "dbias"), scale=2.0):
+    d = B.XentDesc(rows=rows, features=D, classes=V, dtype=CDT[dtype])
+    xd, xn = values((rows, D), 0, dtype) if x is None else x
+    wd, wn = values((V, D), 1, dtype, scale=scale / np.sqrt(D)) if w is None else w
+    bd, bn = (None, None) if bias is None else bias
+    up, upn = values((rows,), 3, "f32")
+    lab = torch.from_numpy(labels).cuda()
+    ws = scratch(B.tsm_xent_workspace_bytes(d))
+    loss, lse = Guarded((rows,), torch.float32), Guarded((rows,), torch.float32)
+    B.tsm_xent_fwd(d, xd, wd, bd, lab, loss.t, lse.t, ws)
+    dx, dw, db = Guarded((rows, D), TDT[dtype]), Guarded((V, D), TDT[dtype]), Guarded((V,), torch.float32)
+    B.tsm_xent_bwd(d, xd, wd, bd, lab, lse.t, up, dx.t if "dx" in want else None, dw.t if "dw" in want else None,
+                   db.t if "dbias" in want else None, ws)
+    torch.cuda.synchronize()
+    return (xn, wn, bn, upn), [v.np() for v in (loss, lse, dx, dw, db)]
+
+
+def _check(inputs, outs, labels, dtype):
+    x, w, b, up = inputs
+    loss, lse, dx, dw, db = outs
+    (R, D), V = x.shape, w.shape[0]
+    used = ((labels >= 0) & (labels < V))[:, None]
+    S = (np.abs(x) @ np.abs(w).T).max(1) + (0 if b is None else np.abs(b[np.isfinite(b)]).max())
+    d = (4 * np.sqrt(D) + 16) * U * S
+    el = d + (4 * np.sqrt(V) + 32) * U + 16 * U * S
+    rloss, rlse = H.xent_fwd(x, w, b, labels)
+    within(lse, rlse, el, "lse")
+    within(loss, rloss, d + el, "loss")
+    G = H.xent_grad(x, w, b, labels, up)
+    p = np.where(used, np.abs(up)[:, None] * np.exp(x @ w.T + (0 if b is None else b) - rlse[:, None]), 0)
+    half = HALF[dtype]
+    TINY = 2.0 ** -126
+    eG = TINY + p * (2 * (d + el)[:, None] + 8 * U) + (np.abs(G) * half if dtype == "bf16" else 4 * U * np.abs(G))
+    rdx, rdw, rdb = H.xent_bwd(x, w, b, labels, up)
+    aw, ax = np.abs(w), np.where(used, np.abs(x), 0)
+    if dx is not None:
+        within(dx, rdx, eG @ aw + (4 * np.sqrt(V) + 16) * U * (np.abs(G) @ aw) + half * np.abs(rdx) + TINY, "dx")
+    within(dw, rdw, eG.T @ ax + (4 * np.sqrt(R) + 16) * U * (np.abs(G).T @ ax) + half * np.abs(rdw) + TINY, "dw")
+    eb = TINY + p * (2 * (d + el)[:, None] + 8 * U) + 4 * U * np.abs(G)
+    within(db, rdb, eb.sum(0) + (4 * np.sqrt(R) + 16) * U * np.abs(G).sum(0), "dbias")
+
+
+@pytest.mark.parametrize("biased,ignored", [(False, False), (True, True)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_forward_and_backward(shape, dtype, biased, ignored):
+    R, D, V = shape
+    labels = _labels(R, V, 4, ignored)
+    inputs, outs = _run(R, D, V, dtype, values((V,), 2, "f32") if biased else None, labels)
+    _check(inputs, outs, labels, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_row_has_a_label(dtype):
+    labels = np.full(70, -1, np.int32)
+    _, (loss, lse, dx, dw, db) = _run(70, 48, 90, dtype, None, labels)
+    assert (loss == 0).all() and np.isfinite(lse).all() and (dx == 0).all() and (dw == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(70, 64, 90), (300, 136, 700)])
+def test_bad_values_in_rows_without_a_label(dtype, shape):
+    """What rows without a label hold reaches none of the weights' gradients and no other row."""
+    R, D, V = shape
+    labels = _labels(R, V, 4, True)
+    out = ~((labels >= 0) & (labels < V))
+    xd, xn = values((R, D), 0, dtype)
+    clean = _run(R, D, V, dtype, None, labels, x=(xd, xn))
+    bad = xd.clone()
+    bad[torch.from_numpy(np.nonzero(out)[0][::2]).cuda()] = float("nan")
+    bad[torch.from_numpy(np.nonzero(out)[0][1::2]).cuda()] = float("inf")
+    _, dirty = _run(R, D, V, dtype, None, labels, x=(bad, None))
+    for k in (3, 4):
+        assert np.array_equal(dirty[k], clean[1][k])
+    for k in (0, 1, 2):
+        assert np.array_equal(dirty[k][~out], clean[1][k][~out])
+    assert (dirty[2][out] == 0).all() and (dirty[0][out] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_classes_taken_out_by_the_bias(dtype):
+    """Biases of minus infinity, tiles of them, and of the type's lowest value; a label among them has an infinite loss."""
+    R, D, V = 90, 64, 700
+    labels = _labels(R, V, 4, False)
+    labels[labels < 300] += 300
+    labels[5] = 10
+    b = np.zeros(V, np.float32)
+    b[:300] = -np.inf
+    b[640:650] = np.finfo(np.float32).min
+    labels[(labels >= 640) & (labels < 650)] = 600
+    bt = torch.from_numpy(b)
+    inputs, outs = _run(R, D, V, dtype, (bt.cuda(), b.astype(np.float64)), labels)
+    assert outs[0][5] == np.inf and np.isfinite(np.delete(outs[0], 5)).all()
+    x, w, _, up = inputs
+    keep = b > -1e30                                   # (the lowest value and minus infinity weigh nothing alike)
+    flat = np.where(keep, 0.0, -1e4)
+    rloss, rlse = H.xent_fwd(x, w, flat, labels)
+    within(outs[1], rlse, 1e-4, "lse")
+    G = H.xent_grad(x, w, flat, labels, up)
+    tol = 2.0 ** -7 if dtype == "bf16" else 1e-4       # entries of G off by 2^-8, sums of them and the results rounded alike
+    within(outs[2], G @ w, tol * (np.abs(G) @ np.abs(w)) + 1e-6, "dx")
+    within(outs[3], G.T @ x, tol * (np.abs(G).T @ np.abs(x)) + 1e-6, "dw")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_class_is_left(dtype):
+    R, D, V = 20, 32, 150
+    b = torch.full((V,), float("-inf"))
+    _, (loss, lse, dx, dw, db) = _run(R, D, V, dtype, (b.cuda(), None), _labels(R, V, 4, False))
+    assert np.isneginf(lse).all() and np.isnan(loss).all() and np.isnan(dx).all()
+
+
+def test_large_logits():
+    """Logits of some +-1500: only their differences matter."""
+    labels = _labels(40, 300, 4, False)
+    inputs, outs = _run(40, 64, 300, "bf16", None, labels, scale=400.0)
+    _check(inputs, outs, labels, "bf16")
+
+
+@pytest.mark.parametrize("want", [("dx",), ("dw",), ("dbias",)])
+def test_one_gradient_at_a_time(want):
+    labels = _labels(100, 300, 4, True)
+    both = _run(100, 72, 300, "bf16", None, labels)[1]
+    one = _run(100, 72, 300, "bf16", None, labels, want=want)[1]
+    for k, name in enumerate(("dx", "dw", "dbias")):
+        if name in want:
+            assert np.array_equal(one[2 + k], both[2 + k])
+        else:
+            assert np.isnan(one[2 + k]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_same_bits_twice_and_on_another_stream(dtype):
+    labels = _labels(600, 900, 4, True)
+    first = _run(600, 200, 900, dtype, None, labels)[1]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        second = _run(600, 200, 900, dtype, None, labels)[1]
+    s.synchronize()
+    for a, b in zip(first, second):
+        assert np.array_equal(a, b)
+
+
+def test_gradient_is_that_of_the_kernels_own_forward():
+    """Central differences of the library's losses in fp32 along one direction: losses of order 1 off by 1e-6 each, over 2e-2."""
+    R, D, V = 50, 64, 200
+    d = B.XentDesc(rows=R, features=D, classes=V, dtype=B.TSM_F32)
+    labels = torch.from_numpy(_labels(R, V, 4, True)).cuda()
+    xd, _ = values((R, D), 0, "f32")
+    wd, _ = values((V, D), 1, "f32", scale=0.2)
+    bd, _ = values((V,), 2, "f32")
+    up, _ = values((R,), 3, "f32")
+    dirs = [values(t.shape, 10 + i, "f32")[0] for i, t in enumerate((xd, wd, bd))]
+    dirs[1] *= 0.1
+    ws = scratch(B.tsm_xent_workspace_bytes(d))
+    lse = torch.empty(R, device="cuda")
+
+    def loss(x, w, b):
+        out = torch.empty(R, device="cuda")
+        B.tsm_xent_fwd(d, x, w, b, labels, out, lse, ws)
+        return float((out.double() * up.double()).sum())
+    h = 1e-2
+    slope = (loss(*[t + h * u for t, u in zip((xd, wd, bd), dirs)]) - loss(*[t - h * u for t, u in zip((xd, wd, bd), dirs)])) / (2 * h)
+    loss(xd, wd, bd)
+    grads = [torch.empty_like(t) for t in (xd, wd, bd)]
+    B.tsm_xent_bwd(d, xd, wd, bd, labels, lse, up, *grads, ws)
+    want = sum(float((g.double() * u.double()).sum()) for g, u in zip(grads, dirs))
+    scale = float(np.sqrt(sum((g.double() ** 2).sum().item() * (u.double() ** 2).mean().item() for g, u in zip(grads, dirs))))
+    assert abs(slope - want) < 1e-2 * scale, (slope, want, scale)
+
+
+def test_several_pieces_of_the_classes():
+    """More classes than one piece of G holds at this many rows: three pieces, the last one ragged."""
+    R, D, V = 40000, 16, 14000
+    d = B.XentDesc(rows=R, features=D, classes=V, dtype=B.TSM_BF16)
+    labels = _labels(R, V, 4, True)
+    xd, _ = values((R, D), 0, "bf16")
+    wd, _ = values((V, D), 1, "bf16", scale=0.5)
+    up, _ = values((R,), 3, "f32")
+    lab = torch.from_numpy(labels).cuda()
+    ws = scratch(B.tsm_xent_workspace_bytes(d))
+    assert ws.numel() < R * V * 2
+    loss, lse = Guarded((R,), torch.float32), Guarded((R,), torch.float32)
+    B.tsm_xent_fwd(d, xd, wd, None, lab, loss.t, lse.t, ws)
+    dx, dw = Guarded((R, D), torch.bfloat16), Guarded((V, D), torch.bfloat16)
+    B.tsm_xent_bwd(d, xd, wd, None, lab, lse.t, up, dx.t, dw.t, None, ws)
+    x, w = xd.float(), wd.float()
+    s = x @ w.t()                                     # fp32 on the GPU: D is 16, its own error is below 2^-20
+    ok = ((lab >= 0) & (lab < V))
+    at = torch.where(ok, lab, torch.zeros_like(lab)).long()
+    rlse = torch.logsumexp(s, 1)
+    within(lse.np(), rlse.double().cpu().numpy(), 1e-5, "lse")
+    rows = torch.arange(R, device="cuda")
+    within(loss.np(), torch.where(ok, rlse - s[rows, at], torch.zeros_like(rlse)).double().cpu().numpy(), 2e-5, "loss")
+    s.sub_(rlse[:, None]).exp_()
+    s[rows, at] -= 1
+    s.mul_(torch.where(ok, up, torch.zeros_like(up))[:, None])
+    mag = s.abs()
+    for got, want, size in ((dx, s @ w, mag @ w.abs()), (dw, s.t() @ x, mag.t() @ x.abs())):
+        want, size = want.double().cpu().numpy(), size.double().cpu().numpy()
+        within(got.np(), want, (2.0 ** -8 + 1e-4) * size + 2.0 ** -8 * np.abs(want), "gradient")
