@@ -165,6 +165,333 @@ __global__ void __launch_bounds__(256) xent_plain_kernel(XentArgs a) {
     }
 }
 
+// ---- the main tile: bf16, BM x BN results, eight wavefronts that share the operands through LDS -------------------------
+// Operands come 64 steps of K at a time, straight from memory into one of two LDS stages while the other is multiplied.  An
+// operand with consecutive K lies there as rows of 128 bytes whose eight 16-byte pieces are permuted by the row (piece ^ (row/2)%8),
+// so that the 32 rows of a fragment read spread over all banks; one whose rows are K lies there as it does in memory, its
+// 32-byte granules permuted by K, and fragments are read through the transposing LDS read, four K of 16 columns at a time.
+static constexpr int XBK = 64;
+static constexpr uint32_t X_OOB = 0x80000000u;     // beyond every buffer: such lanes of a load leave zeros
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t x_rsrc(const void* base) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x00020000);
+}
+__device__ __forceinline__ void x_load_lds16(__amdgpu_buffer_rsrc_t r, unsigned char* at, uint32_t voff, int soff) {
+#if defined(__HIP_DEVICE_COMPILE__)   // (the host pass of the compiler knows no such address space)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)at, 16, (int)voff, soff, 0, 0);
+#endif
+}
+template <int VM> __device__ __forceinline__ void x_wait() {     // at most VM memory operations and no LDS access outstanding
+    __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | (0 << 8) | ((VM >> 4) << 14));
+}
+__device__ __forceinline__ void x_barrier() {
+    asm volatile("" ::: "memory");   // (a fence would also wait for every load into LDS in flight)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+typedef short x_s16x4 __attribute__((ext_vector_type(4)));
+typedef short x_s16x8 __attribute__((ext_vector_type(8)));
+
+// One operand of a tile: ROWS rows of the result's side, KC: K consecutive in memory.
+template <int ROWS, bool KC, int NT>
+struct XOperand {
+    static constexpr int BYTES = ROWS * XBK * 2;
+    static constexpr int PIECES = BYTES / (NT * 16);          // per thread and step
+    static constexpr int RPP = KC ? NT / 8 : NT / (ROWS / 8); // rows of the LDS image per pass
+    static constexpr int PITCH = KC ? XBK * 2 : ROWS * 2;     // its bytes
+    static constexpr int GMASK = ROWS / 16 - 1;               // granules of 16 columns
+    uint32_t off[PIECES];         // byte offset in the step's window of this thread's pieces
+    int kfirst;                   // KC: K of the piece, else K of the thread's row in a pass
+    const char* base;             // of the step's window
+    long step;                    // bytes from one step to the next
+
+    __device__ __forceinline__ static int swz(int k) { return ((((k & 3) << 1) | (((k >> 3) & 1) << 3))) & GMASK; }
+
+    // row0: first row of the tile, rows: of the matrix; k0: first K.
+    __device__ __forceinline__ void init(const bf16_t* p, long ld, long row0, long rows, long k0, int tid) {
+        if constexpr (KC) {
+            const int r = tid / 8;
+            const int kv = (tid % 8) ^ ((r >> 1) & 7);
+            kfirst = kv * 8;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                off[i] = row0 + i * RPP + r < rows ? (uint32_t)((i * RPP + r) * ld * 2 + kv * 16) : X_OOB;
+            base = (const char*)(p + row0 * ld + k0);
+            step = XBK * 2;
+        } else {
+            const int k = tid / (ROWS / 8), slot = tid % (ROWS / 8);
+            kfirst = k;
+            const int col = (((slot >> 1) ^ swz(k)) << 4) + (slot & 1) * 8;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) off[i] = row0 + col < rows ? (uint32_t)((i * RPP + k) * ld * 2 + col * 2) : X_OOB;
+            base = (const char*)(p + k0 * ld + row0);
+            step = XBK * 2 * ld;
+        }
+    }
+    // Piece i of the step at the window: left = K from its start to the end; mask: bit k clear for rows k that count as zero.
+    __device__ __forceinline__ void load(unsigned char* stage, int i, long left, uint64_t mask, int wave_u) const {
+        const int k = KC ? kfirst : i * RPP + kfirst;
+        const bool in = k < left && (KC || (mask >> k) & 1);
+        x_load_lds16(x_rsrc(base), stage + i * (NT * 16) + wave_u * 1024, in ? off[i] : X_OOB, 0);
+    }
+    // address of the fragment of rows row0.. (a multiple of 32) in slice 0 of K; slice ks is at frag_at(..., ks)
+    __device__ __forceinline__ static x_bf16x8 frag(const unsigned char* stage, int row0, int ks, int lane) {
+        if constexpr (KC) {
+            const int r = lane & 31, hi = lane >> 5;
+            return *(const x_bf16x8*)(stage + (row0 + r) * PITCH + (((2 * ks + hi) ^ ((r >> 1) & 7)) * 16));
+        } else {
+            const int c = lane & 3, e = (lane >> 2) & 3, mblk = (lane >> 4) & 1, kg = lane >> 5;
+            const int g = (row0 / 16 + mblk) ^ swz(8 * kg + e);
+            const unsigned char* p = stage + (16 * ks + 8 * kg + e) * PITCH + g * 32 + c * 8;
+            const x_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) x_s16x4*)p);
+            const x_s16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) x_s16x4*)(p + 4 * PITCH));
+            return __builtin_bit_cast(x_bf16x8, (x_s16x8)__builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+template <int MODE, int BM, int BN, int WM, int WN, bool AK, bool BK>
+__global__ void __launch_bounds__(WM * WN * 64) xent_tile_kernel(XentArgs a, const uint64_t* __restrict__ kmask) {
+    constexpr int NT = WM * WN * 64, MI = BM / (WM * 32), NJ = BN / (WN * 32), KS = XBK / 16;
+    typedef XOperand<BM, AK, NT> OpA;
+    typedef XOperand<BN, BK, NT> OpB;
+    constexpr int STAGE = OpA::BYTES + OpB::BYTES;
+    constexpr int NP = OpA::PIECES + OpB::PIECES;
+    constexpr float L2E = 1.44269502f;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5, lo = lane & 31;
+    const int wave_u = __builtin_amdgcn_readfirstlane(wave);
+    const int wm = wave_u / WN, wn = wave_u % WN;
+
+    // Tiles: eight row tiles at a time, column by column; every XCD takes a stretch of that order, so that the tiles it works
+    // on at one time share their operands in its L2.
+    const long mtiles = (a.M + BM - 1) / BM, ntiles = (a.N + BN - 1) / BN, total = mtiles * ntiles;
+    long tile = blockIdx.x;
+    {
+        const long per = total / 8, more = total % 8, x = tile % 8, at = tile / 8;
+        tile = x * per + (x < more ? x : more) + at;
+    }
+    const long band = tile / (8 * ntiles), rest = tile - band * 8 * ntiles;
+    const long high = mtiles - band * 8 < 8 ? mtiles - band * 8 : 8;
+    const long mt = band * 8 + rest % high, nt = rest / high;
+    const long m0 = mt * BM, n0 = nt * BN;
+    const long kb = blockIdx.z * a.ksplit, ke = kb + a.ksplit < a.K ? kb + a.ksplit : a.K;
+
+    OpA pa;
+    OpB pb;
+    pa.init((const bf16_t*)a.A, a.lda, m0, a.M, kb, tid);
+    pb.init((const bf16_t*)a.B, a.ldb, n0, a.N, kb, tid);
+    const int steps = (int)((ke - kb + XBK - 1) / XBK);
+    long left = ke - kb;
+    const uint64_t* mp = kmask ? kmask + kb / 64 : nullptr;
+    auto load_piece = [&](int stage, int q, uint64_t mask) {
+        unsigned char* st = smem + stage * STAGE;
+        if (q < OpA::PIECES) pa.load(st, q, left, ~0ull, wave_u);
+        else pb.load(st + OpA::BYTES, q - OpA::PIECES, left, mask, wave_u);
+    };
+    uint64_t mask = mp && left > 0 ? mp[0] : ~0ull;
+#pragma unroll
+    for (int q = 0; q < NP; ++q) load_piece(0, q, mask);
+
+    x_f32x16 acc[MI][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+    // One barrier per step, in front of its last group of products: behind it the next step is complete and this stage is free.
+    x_bf16x8 af[2][MI], bf[2][NJ];
+    auto frags = [&](int stage, int ks, int to) {
+        const unsigned char* st = smem + stage * STAGE;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) af[to][i] = OpA::frag(st, wm * (BM / WM) + i * 32, ks, lane);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) bf[to][j] = OpB::frag(st + OpA::BYTES, wn * (BN / WN) + j * 32, ks, lane);
+    };
+    x_wait<0>();
+    x_barrier();
+    frags(0, 0, 0);
+    for (int kc = 0; kc < steps; ++kc) {
+        const int cur = kc & 1, nxt = cur ^ 1;
+        const bool more = kc + 1 < steps;
+        if (more) {
+            pa.base += pa.step;
+            pb.base += pb.step;
+            left -= XBK;
+            if (mp) mask = *++mp;
+        }
+        constexpr int PPK = (NP + KS - 2) / (KS - 1);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            if (ks + 1 < KS) {
+                frags(cur, ks + 1, (ks + 1) & 1);
+            } else {
+                x_wait<0>();
+                x_barrier();
+                if (more) frags(nxt, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)      // the result's columns run along registers, its rows along lanes
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[ks & 1][j], af[ks & 1][i], acc[i][j], 0, 0, 0);
+            if (more)
+#pragma unroll
+                for (int q = ks * PPK; q < (ks + 1) * PPK && q < NP; ++q) load_piece(nxt, q, mask);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
+    // ---- epilogue: this lane has row mrow(i), columns ncol(j, r) = .. + r % 4, four at a time
+    auto mrow = [&](int i) { return m0 + wm * (BM / WM) + i * 32 + lo; };
+    const long nw = n0 + wn * (BN / WN);
+    if constexpr (MODE != XE_OUT) {
+        const float* bias = a.e.bias ? a.e.bias + a.e.col0 : nullptr;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const long n = nw + j * 32 + 8 * q + 4 * hi;
+                float b[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) b[t] = bias && n + t < a.N ? bias[n + t] : 0.f;
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) acc[i][j][4 * q + t] = n + t < a.N ? acc[i][j][4 * q + t] + b[t] : -__builtin_inff();
+            }
+    }
+    if constexpr (MODE == XE_STATS) {
+        float2* s_part = (float2*)smem;            // [WN][BM]   (nobody reads the stages any more: the last barrier is behind)
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const long m = mrow(i);
+            const long ln = m < a.M ? (long)a.e.labels[m] - a.e.col0 - nw : -1;    // the label among the wavefront's columns
+            if (__any(ln >= 0 && ln < BN / WN && nw + ln < a.N)) {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (ln == j * 32 + 8 * (r / 4) + 4 * hi + r % 4 && nw + ln < a.N) a.e.picked[m] = acc[i][j][r];
+            }
+            float mx = -__builtin_inff();
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float from = mx == -__builtin_inff() ? 0.f : mx;       // (a row of minus infinities sums to zero)
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[i][j][r] - from) * L2E);
+            s += __shfl_xor(s, 32, 64);
+            if (hi == 0) s_part[wn * BM + wm * (BM / WM) + i * 32 + lo] = make_float2(mx, s);
+        }
+        __syncthreads();
+        for (int r = tid; r < BM; r += NT)
+            if (m0 + r < a.M) {
+                float2 p = s_part[r];
+#pragma unroll
+                for (int w = 1; w < WN; ++w) join_softmax(p.x, p.y, s_part[w * BM + r].x, s_part[w * BM + r].y);
+                a.e.part[nt * a.M + m0 + r] = p;
+            }
+    } else if constexpr (MODE == XE_GRAD) {
+        constexpr int LDC = BN + 8;                // [BM][LDC] bf16, then stored row by row
+        bf16_t* s_out = (bf16_t*)smem;
+        float colsum[NJ][16];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) colsum[j][r] = 0.f;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const long m = mrow(i);
+            const int label = m < a.M ? a.e.labels[m] : -1;
+            const bool use = is_class(label, a.e.classes);
+            const float up = use ? a.e.dloss[m] : 0.f, lse = use ? a.e.lse[m] : 0.f;
+            const long ln = use ? (long)label - a.e.col0 - nw : -1;
+            const bool here = __any(ln >= 0 && ln < BN / WN);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float g[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        float p = __builtin_amdgcn_exp2f((acc[i][j][4 * q + t] - lse) * L2E);
+                        if (here && ln == j * 32 + 8 * q + 4 * hi + t) p -= 1.f;
+                        const bool in = use && nw + j * 32 + 8 * q + 4 * hi + t < a.N;
+                        g[t] = in ? up * p : 0.f;
+                        colsum[j][4 * q + t] += g[t];
+                    }
+                    *(uint2*)(s_out + (wm * (BM / WM) + i * 32 + lo) * LDC + wn * (BN / WN) + j * 32 + 8 * q + 4 * hi) =
+                        make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
+                }
+        }
+        __syncthreads();
+        constexpr int CV = BN / 8;
+        for (int q = tid; q < BM * CV; q += NT) {
+            const int r = q / CV, c = (q % CV) * 8;
+            if (m0 + r < a.M && n0 + c < a.e.ldg) *(any_u32x4*)((bf16_t*)a.e.G + (m0 + r) * a.e.ldg + n0 + c) = *(const any_u32x4*)(s_out + r * LDC + c);
+        }
+        if (a.e.dbias_part) {
+            // sums over the wavefront's rows, then over the wavefronts
+            __syncthreads();
+            float* s_sum = (float*)smem;           // [WM][BN]
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    float t = colsum[j][r];
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
+                    if (lo == 0) s_sum[wm * BN + wn * (BN / WN) + j * 32 + 8 * (r / 4) + 4 * hi + r % 4] = t;
+                }
+            __syncthreads();
+            for (int c = tid; c < BN; c += NT)
+                if (n0 + c < a.N) {
+                    float t = s_sum[c];
+#pragma unroll
+                    for (int w = 1; w < WM; ++w) t += s_sum[w * BN + c];
+                    a.e.dbias_part[mt * a.e.ldg + n0 + c] = t;
+                }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const long m = mrow(i);
+            if (m >= a.M) continue;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const long n = nw + j * 32 + 8 * q + 4 * hi;       // (N is a multiple of 8)
+                    if (n >= a.N) continue;
+                    float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                    if (a.e.acc) {
+                        const float4 o = *(const float4*)(a.e.acc + m * a.N + n);
+                        v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+                    }
+                    if (a.e.out_f32) *(float4*)(a.e.out_f32 + (blockIdx.z * a.M + m) * a.N + n) = v;
+                    else *(uint2*)((bf16_t*)a.e.out + m * a.N + n) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+                }
+        }
+    }
+}
+
+// bit r of word r / 64: row r has a label
+__global__ void __launch_bounds__(256) xent_mask_kernel(const int32_t* __restrict__ labels, long rows, long classes, uint64_t* __restrict__ mask) {
+    for (long r = (long)blockIdx.x * 256 + threadIdx.x; r < (rows + 63) / 64 * 64; r += (long)gridDim.x * 256) {
+        const uint64_t b = __ballot(r < rows && is_class(labels[r], classes));
+        if ((threadIdx.x & 63) == 0) mask[r / 64] = b;
+    }
+}
+
 // lse and loss of a row from its tiles: one wavefront per row
 __global__ void __launch_bounds__(256) xent_finish_kernel(const float2* __restrict__ part, const float* __restrict__ picked,
                                                           const int32_t* __restrict__ labels, float* __restrict__ loss, float* __restrict__ lse,
@@ -214,13 +541,16 @@ struct XentPlan {
     long mtiles;                  // row tiles of G
     int zdx, zdw;                 // splits of K of the two products
     size_t fwd_bytes, bwd_bytes;
-    size_t o_part, o_picked, o_G, o_acc, o_dw, o_dbias;
+    size_t o_part, o_picked, o_G, o_acc, o_dw, o_dbias, o_mask;
+    bool main;                    // on the main tiles
 };
 
 static constexpr size_t XENT_G_BYTES = (size_t)512 << 20;   // of a piece of G, at most (a piece has 1024 classes at least)
 
-static int splits_of(long tiles, long K) {
-    long z = tiles < 512 ? 512 / tiles : 1;
+static constexpr int X_BM = 256, X_BN = 256, X_WM = 2, X_WN = 4;
+
+static int splits_of(long tiles, long K, long fill) {
+    long z = tiles < fill ? fill / tiles : 1;
     const long most = K / 512 > 1 ? K / 512 : 1;
     if (z > most) z = most;
     return (int)(z > 64 ? 64 : z);
@@ -229,26 +559,30 @@ static int splits_of(long tiles, long K) {
 static XentPlan xent_plan(const tsm_xent_desc* d) {
     XentPlan p{};
     const long R = d->rows, D = d->features, V = d->classes, es = (long)dtype_size(d->dtype);
-    p.ntiles = (V + 63) / 64;
-    p.mtiles = (R + 63) / 64;
+    p.main = d->dtype == TSM_BF16 && D % 8 == 0 && D <= (1 << 21);
+    const long bm = p.main ? X_BM : 64, bn = p.main ? X_BN : 64, fill = p.main ? 256 : 512;
+    p.ntiles = (V + bn - 1) / bn;
+    p.mtiles = (R + bm - 1) / bm;
     Arena f(nullptr, 0);
     p.o_part = f.used; f.take((size_t)p.ntiles * R * 8);
     p.o_picked = f.used; f.take((size_t)R * 4);
     p.fwd_bytes = f.used;
     long piece = (long)(XENT_G_BYTES / es) / R / 1024 * 1024;
     if (piece < 1024) piece = 1024;
+    if (piece > (1 << 21)) piece = 1 << 21;      // (offsets inside a tile of G stay below 2 GiB)
     if (piece > V) piece = V;
     p.piece = piece;
     p.pieces = (V + piece - 1) / piece;
     p.ldg = (piece + 7) / 8 * 8;
-    const long dt = (D + 63) / 64;
-    p.zdx = p.pieces > 1 ? 1 : splits_of(p.mtiles * dt, V);
-    p.zdw = splits_of((piece + 63) / 64 * dt, R);
+    const long dt = (D + bn - 1) / bn;
+    p.zdx = p.pieces > 1 ? 1 : splits_of(p.mtiles * dt, V, fill);
+    p.zdw = splits_of((piece + bm - 1) / bm * dt, R, fill);
     Arena b(nullptr, 0);
     p.o_G = b.used; b.take((size_t)R * p.ldg * es);
     p.o_acc = b.used; b.take(p.pieces > 1 || p.zdx > 1 ? (size_t)p.zdx * R * D * 4 : 0);
     p.o_dw = b.used; b.take(p.zdw > 1 ? (size_t)p.zdw * piece * D * 4 : 0);
     p.o_dbias = b.used; b.take((size_t)p.mtiles * p.ldg * 4);
+    p.o_mask = b.used; b.take((size_t)(R + 63) / 64 * 8);
     p.bwd_bytes = b.used;
     return p;
 }
@@ -264,8 +598,24 @@ static int xent_check(const tsm_xent_desc* d, const char* who) {
 static size_t xent_ws(const XentPlan& p) { return p.fwd_bytes > p.bwd_bytes ? p.fwd_bytes : p.bwd_bytes; }
 
 template <typename T, int MODE, bool AK, bool BK>
-static int xent_product(const XentArgs& a, int splits, const char* what, hipStream_t s) {
+static int xent_product(const XentArgs& a, const XentPlan& p, int splits, const uint64_t* kmask, const char* what, hipStream_t s) {
     XentArgs b = a;
+    if constexpr (sizeof(T) == 2) {
+        if (p.main) {
+            const long tiles = ((a.N + X_BN - 1) / X_BN) * ((a.M + X_BM - 1) / X_BM);
+            const size_t smem = MODE == XE_GRAD ? (size_t)X_BM * (X_BN + 8) * 2 : (size_t)2 * (X_BM + X_BN) * XBK * 2;
+            auto kernel = xent_tile_kernel<MODE, X_BM, X_BN, X_WM, X_WN, AK, BK>;
+            static bool configured = false;
+            if (!configured) {
+                if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
+                    return fail(TSM_ERR_LAUNCH, "%s: cannot raise dynamic LDS limit", what);
+                configured = true;
+            }
+            b.ksplit = ((a.K + splits - 1) / splits + 63) / 64 * 64;
+            kernel<<<dim3((unsigned)tiles, 1, (unsigned)splits), dim3(X_WM * X_WN * 64), smem, s>>>(b, kmask);
+            return check_launch(what);
+        }
+    }
     const long nt = (a.N + 63) / 64, mt = (a.M + 63) / 64;
     b.ksplit = ((a.K + splits - 1) / splits + 63) / 64 * 64;
     xent_plain_kernel<T, MODE, AK, BK><<<dim3((unsigned)(nt * mt < 65536 ? nt * mt : 65536), 1, (unsigned)splits), dim3(256), 0, s>>>(b);
@@ -289,7 +639,7 @@ static int xent_fwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
     a.e.part = (float2*)(ws + p.o_part);
     a.e.picked = (float*)(ws + p.o_picked);
     a.e.bias = bias; a.e.labels = labels; a.e.classes = d->classes;
-    TSM_TRY((xent_product<T, XE_STATS, true, true>(a, 1, "xent_stats", s)));
+    TSM_TRY((xent_product<T, XE_STATS, true, true>(a, p, 1, nullptr, "xent_stats", s)));
     const long blocks = (a.M + 3) / 4;
     xent_finish_kernel<<<dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s>>>(a.e.part, a.e.picked, labels, loss, lse, a.M, p.ntiles, d->classes);
     return check_launch("xent_finish");
@@ -301,6 +651,13 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
     const long R = d->rows, D = d->features, V = d->classes;
     void* G = ws + p.o_G;
     float *acc = (float*)(ws + p.o_acc), *dwp = (float*)(ws + p.o_dw), *dbp = (float*)(ws + p.o_dbias);
+    uint64_t* mask = nullptr;
+    if (dw && p.main) {
+        mask = (uint64_t*)(ws + p.o_mask);
+        const long blocks = (R + 255) / 256;
+        xent_mask_kernel<<<dim3((unsigned)(blocks < 1024 ? blocks : 1024)), dim3(256), 0, s>>>(labels, R, V, mask);
+        TSM_TRY(check_launch("xent_mask"));
+    }
     for (long c = 0; c < p.pieces; ++c) {
         const long v0 = c * p.piece, n = V - v0 < p.piece ? V - v0 : p.piece;
         const T* wc = (const T*)w + v0 * D;
@@ -310,7 +667,7 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
         a.M = R; a.N = n;
         a.e.bias = bias; a.e.labels = labels; a.e.classes = V; a.e.col0 = v0;
         a.e.lse = lse; a.e.dloss = dloss; a.e.G = G; a.e.ldg = p.ldg; a.e.dbias_part = dbias ? dbp : nullptr;
-        TSM_TRY((xent_product<T, XE_GRAD, true, true>(a, 1, "xent_grad", s)));
+        TSM_TRY((xent_product<T, XE_GRAD, true, true>(a, p, 1, nullptr, "xent_grad", s)));
         if (dbias) {
             xent_colsum_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(dbp, p.mtiles, p.ldg, n, dbias + v0);
             TSM_TRY(check_launch("xent_dbias"));
@@ -322,7 +679,7 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
             b.e.acc = c > 0 ? acc : nullptr;
             if (p.zdx > 1 || c + 1 < p.pieces) b.e.out_f32 = acc;
             else b.e.out = dx;
-            TSM_TRY((xent_product<T, XE_OUT, true, false>(b, p.zdx, "xent_dx", s)));
+            TSM_TRY((xent_product<T, XE_OUT, true, false>(b, p, p.zdx, nullptr, "xent_dx", s)));
             if (p.zdx > 1) TSM_TRY(xent_join<T>(acc, p.zdx, R * D, dx, "xent_dx_join", s));
         }
         if (dw) {
@@ -333,7 +690,7 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
             T* out = (T*)dw + v0 * D;
             if (p.zdw > 1) b.e.out_f32 = dwp;
             else b.e.out = out;
-            TSM_TRY((xent_product<T, XE_OUT, false, false>(b, p.zdw, "xent_dw", s)));
+            TSM_TRY((xent_product<T, XE_OUT, false, false>(b, p, p.zdw, mask, "xent_dw", s)));
             if (p.zdw > 1) TSM_TRY(xent_join<T>(dwp, p.zdw, n * D, out, "xent_dw_join", s));
         }
     }
