@@ -26,9 +26,10 @@ struct XentEpi {
     long col0, classes;
     // GRAD
     const float *lse, *dloss;
-    void* G;                 // [M][ldg], zero behind the last column
+    void* G;                 // [M][ldg], zero behind the last column; the main tiles': blocks (X_GROWS), ldg elements per row tile
     long ldg;
-    float* dbias_part;       // [M tiles][ldg], nullable
+    float* dbias_part;       // [M tiles][lddb], nullable
+    long lddb;
     // OUT
     const float* acc;        // fp32 [M][N] added to the result, nullable
     float* out_f32;          // [splits][M][N], or
@@ -158,7 +159,7 @@ __global__ void __launch_bounds__(256) xent_plain_kernel(XentArgs a) {
             __syncthreads();
             red[0][wave][lane] = dbias;
             __syncthreads();
-            if (wave == 0 && in) a.e.dbias_part[mt * a.e.ldg + n] = (red[0][0][lane] + red[0][1][lane]) + (red[0][2][lane] + red[0][3][lane]);
+            if (wave == 0 && in) a.e.dbias_part[mt * a.e.lddb + n] = (red[0][0][lane] + red[0][1][lane]) + (red[0][2][lane] + red[0][3][lane]);
         }
     }
     __syncthreads();
@@ -171,6 +172,7 @@ __global__ void __launch_bounds__(256) xent_plain_kernel(XentArgs a) {
 // so that the 32 rows of a fragment read spread over all banks; one whose rows are K lies there as it does in memory, its
 // 32-byte granules permuted by K, and fragments are read through the transposing LDS read, four K of 16 columns at a time.
 static constexpr int XBK = 64;
+static constexpr int X_GTILE = 256;                // rows of a block of G, and columns of the tiles that write them
 static constexpr uint32_t X_OOB = 0x80000000u;     // beyond every buffer: such lanes of a load leave zeros
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t x_rsrc(const void* base) {
@@ -192,9 +194,14 @@ __device__ __forceinline__ void x_barrier() {
 typedef short x_s16x4 __attribute__((ext_vector_type(4)));
 typedef short x_s16x8 __attribute__((ext_vector_type(8)));
 
-// One operand of a tile: ROWS rows of the result's side, KC: K consecutive in memory.
-template <int ROWS, bool KC, int NT>
+// How an operand lies in memory.  The blocks of G: [row tile][64 columns][256 rows], 32 KB each, so that a step of either product
+// reads stretches of 8 KB and more, where rows of G as such would be a 64 KB apart.
+enum { X_ROWS = 0, X_COLS = 1, X_GROWS = 2, X_GCOLS = 3 };     // [rows][K], [K][rows], G with its columns as K, with its rows as K
+
+// One operand of a tile: ROWS rows of the result's side.
+template <int ROWS, int KIND, int NT>
 struct XOperand {
+    static constexpr bool KC = KIND == X_ROWS || KIND == X_GROWS;     // K consecutive in LDS
     static constexpr int BYTES = ROWS * XBK * 2;
     static constexpr int PIECES = BYTES / (NT * 16);          // per thread and step
     static constexpr int RPP = KC ? NT / 8 : NT / (ROWS / 8); // rows of the LDS image per pass
@@ -204,37 +211,58 @@ struct XOperand {
     int kfirst;                   // KC: K of the piece, else K of the thread's row in a pass
     const char* base;             // of the step's window
     long step;                    // bytes from one step to the next
+    int quarter;                  // X_GCOLS: steps into a row tile
 
     __device__ __forceinline__ static int swz(int k) { return ((((k & 3) << 1) | (((k >> 3) & 1) << 3))) & GMASK; }
 
-    // row0: first row of the tile, rows: of the matrix; k0: first K.
+    // row0: first row of the tile, rows: of the matrix; k0: first K.  ld: elements from row to row, for G from one row tile to the next.
     __device__ __forceinline__ void init(const bf16_t* p, long ld, long row0, long rows, long k0, int tid) {
+        quarter = 0;
         if constexpr (KC) {
             const int r = tid / 8;
             const int kv = (tid % 8) ^ ((r >> 1) & 7);
             kfirst = kv * 8;
+            const long pitch = KIND == X_GROWS ? XBK : ld;
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
-                off[i] = row0 + i * RPP + r < rows ? (uint32_t)((i * RPP + r) * ld * 2 + kv * 16) : X_OOB;
-            base = (const char*)(p + row0 * ld + k0);
-            step = XBK * 2;
+                off[i] = row0 + i * RPP + r < rows ? (uint32_t)((i * RPP + r) * pitch * 2 + kv * 16) : X_OOB;
+            base = KIND == X_GROWS ? (const char*)(p + row0 / ROWS * ld + k0 * ROWS) : (const char*)(p + row0 * ld + k0);
+            step = KIND == X_GROWS ? ROWS * XBK * 2 : XBK * 2;
         } else {
             const int k = tid / (ROWS / 8), slot = tid % (ROWS / 8);
             kfirst = k;
             const int col = (((slot >> 1) ^ swz(k)) << 4) + (slot & 1) * 8;
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) off[i] = row0 + col < rows ? (uint32_t)((i * RPP + k) * ld * 2 + col * 2) : X_OOB;
-            base = (const char*)(p + k0 * ld + row0);
-            step = XBK * 2 * ld;
+            for (int i = 0; i < PIECES; ++i) {
+                const long at = KIND == X_GCOLS ? col / XBK * (X_GTILE * XBK) + (i * RPP + k) * XBK + col % XBK : (i * RPP + k) * ld + col;
+                off[i] = row0 + col < rows ? (uint32_t)(at * 2) : X_OOB;
+            }
+            if constexpr (KIND == X_GCOLS) {
+                quarter = (int)(k0 % X_GTILE / XBK);
+                base = (const char*)(p + k0 / X_GTILE * ld + row0 * X_GTILE + k0 % X_GTILE * XBK);
+                step = (ld - (X_GTILE - XBK) * XBK) * 2;       // into the next row tile
+            } else {
+                base = (const char*)(p + k0 * ld + row0);
+                step = XBK * 2 * ld;
+            }
+        }
+    }
+    __device__ __forceinline__ void advance() {
+        if constexpr (KIND == X_GCOLS) {
+            const bool last = quarter == X_GTILE / XBK - 1;
+            base += last ? step : (long)XBK * XBK * 2;
+            quarter = last ? 0 : quarter + 1;
+        } else {
+            base += step;
         }
     }
     // Piece i of the step at the window: left = K from its start to the end; mask: bit k clear for rows k that count as zero.
-    __device__ __forceinline__ void load(unsigned char* stage, int i, long left, uint64_t mask, int wave_u) const {
+    __device__ __forceinline__ void load(unsigned char* stage, int i, int left, uint64_t mask, int wave_u) const {
         const int k = KC ? kfirst : i * RPP + kfirst;
         const bool in = k < left && (KC || (mask >> k) & 1);
         x_load_lds16(x_rsrc(base), stage + i * (NT * 16) + wave_u * 1024, in ? off[i] : X_OOB, 0);
     }
-    // address of the fragment of rows row0.. (a multiple of 32) in slice 0 of K; slice ks is at frag_at(..., ks)
+    // the 32 rows from row0 (a multiple of 32), K slice ks
     __device__ __forceinline__ static x_bf16x8 frag(const unsigned char* stage, int row0, int ks, int lane) {
         if constexpr (KC) {
             const int r = lane & 31, hi = lane >> 5;
@@ -250,11 +278,12 @@ struct XOperand {
     }
 };
 
-template <int MODE, int BM, int BN, int WM, int WN, bool AK, bool BK>
+// DB: the column sums of G are wanted.
+template <int MODE, int BM, int BN, int WM, int WN, int AKIND, int BKIND, bool DB>
 __global__ void __launch_bounds__(WM * WN * 64) xent_tile_kernel(XentArgs a, const uint64_t* __restrict__ kmask) {
     constexpr int NT = WM * WN * 64, MI = BM / (WM * 32), NJ = BN / (WN * 32), KS = XBK / 16;
-    typedef XOperand<BM, AK, NT> OpA;
-    typedef XOperand<BN, BK, NT> OpB;
+    typedef XOperand<BM, AKIND, NT> OpA;
+    typedef XOperand<BN, BKIND, NT> OpB;
     constexpr int STAGE = OpA::BYTES + OpB::BYTES;
     constexpr int NP = OpA::PIECES + OpB::PIECES;
     constexpr float L2E = 1.44269502f;
@@ -282,17 +311,17 @@ __global__ void __launch_bounds__(WM * WN * 64) xent_tile_kernel(XentArgs a, con
     pa.init((const bf16_t*)a.A, a.lda, m0, a.M, kb, tid);
     pb.init((const bf16_t*)a.B, a.ldb, n0, a.N, kb, tid);
     const int steps = (int)((ke - kb + XBK - 1) / XBK);
-    long left = ke - kb;
     const uint64_t* mp = kmask ? kmask + kb / 64 : nullptr;
-    auto load_piece = [&](int stage, int q, uint64_t mask) {
+    auto load_step = [&](int stage, int kc) {
         unsigned char* st = smem + stage * STAGE;
-        if (q < OpA::PIECES) pa.load(st, q, left, ~0ull, wave_u);
-        else pb.load(st + OpA::BYTES, q - OpA::PIECES, left, mask, wave_u);
-    };
-    uint64_t mask = mp && left > 0 ? mp[0] : ~0ull;
+        const long l = ke - kb - (long)kc * XBK;
+        const int left = l < XBK ? (int)l : XBK;
+        const uint64_t mask = mp ? mp[kc] : ~0ull;
 #pragma unroll
-    for (int q = 0; q < NP; ++q) load_piece(0, q, mask);
-
+        for (int q = 0; q < OpA::PIECES; ++q) pa.load(st, q, left, ~0ull, wave_u);
+#pragma unroll
+        for (int q = 0; q < OpB::PIECES; ++q) pb.load(st + OpA::BYTES, q, left, mask, wave_u);
+    };
     x_f32x16 acc[MI][NJ];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -302,6 +331,9 @@ __global__ void __launch_bounds__(WM * WN * 64) xent_tile_kernel(XentArgs a, con
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
     // One barrier per step, in front of its last group of products: behind it the next step is complete and this stage is free.
+    // A step's loads are issued in one go at the start of the step before: spread over its groups the last of them came late
+    // (17.6 and 19.5 ms for the largest listed pass); stages of 32 K, up to four steps ahead, gain nothing (18.0 ms), four wavefronts of
+    // 128 x 128 instead of eight of 128 x 64 lose (20.4 ms).
     x_bf16x8 af[2][MI], bf[2][NJ];
     auto frags = [&](int stage, int ks, int to) {
         const unsigned char* st = smem + stage * STAGE;
@@ -310,19 +342,20 @@ __global__ void __launch_bounds__(WM * WN * 64) xent_tile_kernel(XentArgs a, con
 #pragma unroll
         for (int j = 0; j < NJ; ++j) bf[to][j] = OpB::frag(st + OpA::BYTES, wn * (BN / WN) + j * 32, ks, lane);
     };
-    x_wait<0>();
-    x_barrier();
-    frags(0, 0, 0);
+    if (steps > 0) {
+        load_step(0, 0);
+        x_wait<0>();
+        x_barrier();
+        frags(0, 0, 0);
+    }
     for (int kc = 0; kc < steps; ++kc) {
         const int cur = kc & 1, nxt = cur ^ 1;
         const bool more = kc + 1 < steps;
         if (more) {
-            pa.base += pa.step;
-            pb.base += pb.step;
-            left -= XBK;
-            if (mp) mask = *++mp;
+            pa.advance();
+            pb.advance();
+            load_step(nxt, kc + 1);
         }
-        constexpr int PPK = (NP + KS - 2) / (KS - 1);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             if (ks + 1 < KS) {
@@ -332,16 +365,11 @@ __global__ void __launch_bounds__(WM * WN * 64) xent_tile_kernel(XentArgs a, con
                 x_barrier();
                 if (more) frags(nxt, 0, 0);
             }
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
                 for (int j = 0; j < NJ; ++j)      // the result's columns run along registers, its rows along lanes
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[ks & 1][j], af[ks & 1][i], acc[i][j], 0, 0, 0);
-            if (more)
-#pragma unroll
-                for (int q = ks * PPK; q < (ks + 1) * PPK && q < NP; ++q) load_piece(nxt, q, mask);
-            __builtin_amdgcn_sched_barrier(0);
         }
     }
 
@@ -403,11 +431,12 @@ __global__ void __launch_bounds__(WM * WN * 64) xent_tile_kernel(XentArgs a, con
     } else if constexpr (MODE == XE_GRAD) {
         constexpr int LDC = BN + 8;                // [BM][LDC] bf16, then stored row by row
         bf16_t* s_out = (bf16_t*)smem;
-        float colsum[NJ][16];
+        float colsum[DB ? NJ : 1][16];
+        if constexpr (DB)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+            for (int j = 0; j < NJ; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) colsum[j][r] = 0.f;
+                for (int r = 0; r < 16; ++r) colsum[j][r] = 0.f;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const long m = mrow(i);
@@ -427,19 +456,18 @@ __global__ void __launch_bounds__(WM * WN * 64) xent_tile_kernel(XentArgs a, con
                         if (here && ln == j * 32 + 8 * q + 4 * hi + t) p -= 1.f;
                         const bool in = use && nw + j * 32 + 8 * q + 4 * hi + t < a.N;
                         g[t] = in ? up * p : 0.f;
-                        colsum[j][4 * q + t] += g[t];
+                        if constexpr (DB) colsum[j][4 * q + t] += g[t];
                     }
                     *(uint2*)(s_out + (wm * (BM / WM) + i * 32 + lo) * LDC + wn * (BN / WN) + j * 32 + 8 * q + 4 * hi) =
                         make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
                 }
         }
         __syncthreads();
-        constexpr int CV = BN / 8;
-        for (int q = tid; q < BM * CV; q += NT) {
-            const int r = q / CV, c = (q % CV) * 8;
-            if (m0 + r < a.M && n0 + c < a.e.ldg) *(any_u32x4*)((bf16_t*)a.e.G + (m0 + r) * a.e.ldg + n0 + c) = *(const any_u32x4*)(s_out + r * LDC + c);
-        }
-        if (a.e.dbias_part) {
+        // (the tile's four blocks of G follow one another)
+        static_assert(MODE != XE_GRAD || (BM == X_GTILE && BN == X_GTILE), "G's blocks");
+        any_u32x4* G = (any_u32x4*)((bf16_t*)a.e.G + mt * a.e.ldg + n0 * X_GTILE);
+        for (int q = tid; q < BM * BN / 8; q += NT) G[q] = *(const any_u32x4*)(s_out + q / 8 % BM * LDC + q / (8 * BM) * XBK + q % 8 * 8);
+        if constexpr (DB) {
             // sums over the wavefront's rows, then over the wavefronts
             __syncthreads();
             float* s_sum = (float*)smem;           // [WM][BN]
@@ -458,7 +486,7 @@ __global__ void __launch_bounds__(WM * WN * 64) xent_tile_kernel(XentArgs a, con
                     float t = s_sum[c];
 #pragma unroll
                     for (int w = 1; w < WM; ++w) t += s_sum[w * BN + c];
-                    a.e.dbias_part[mt * a.e.ldg + n0 + c] = t;
+                    a.e.dbias_part[mt * a.e.lddb + n0 + c] = t;
                 }
         }
     } else {
@@ -536,7 +564,8 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float* __restrict_
 
 // ---- host --------------------------------------------------------------------------------
 struct XentPlan {
-    long piece, pieces, ldg;      // classes of a piece of G, number of pieces, row pitch of G
+    long piece, pieces;           // classes of a piece of G, number of pieces
+    long ldg, lddb;               // elements from row (main: row tile) to row of G, of the partial sums of db
     long ntiles;                  // column tiles of the forward pass
     long mtiles;                  // row tiles of G
     int zdx, zdw;                 // splits of K of the two products
@@ -569,19 +598,19 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     p.fwd_bytes = f.used;
     long piece = (long)(XENT_G_BYTES / es) / R / 1024 * 1024;
     if (piece < 1024) piece = 1024;
-    if (piece > (1 << 21)) piece = 1 << 21;      // (offsets inside a tile of G stay below 2 GiB)
     if (piece > V) piece = V;
     p.piece = piece;
     p.pieces = (V + piece - 1) / piece;
-    p.ldg = (piece + 7) / 8 * 8;
+    p.lddb = (piece + 7) / 8 * 8;
+    p.ldg = p.main ? (piece + X_GTILE - 1) / X_GTILE * X_GTILE * X_GTILE : p.lddb;
     const long dt = (D + bn - 1) / bn;
     p.zdx = p.pieces > 1 ? 1 : splits_of(p.mtiles * dt, V, fill);
     p.zdw = splits_of((piece + bm - 1) / bm * dt, R, fill);
     Arena b(nullptr, 0);
-    p.o_G = b.used; b.take((size_t)R * p.ldg * es);
+    p.o_G = b.used; b.take((size_t)(p.main ? p.mtiles : R) * p.ldg * es);
     p.o_acc = b.used; b.take(p.pieces > 1 || p.zdx > 1 ? (size_t)p.zdx * R * D * 4 : 0);
     p.o_dw = b.used; b.take(p.zdw > 1 ? (size_t)p.zdw * piece * D * 4 : 0);
-    p.o_dbias = b.used; b.take((size_t)p.mtiles * p.ldg * 4);
+    p.o_dbias = b.used; b.take((size_t)p.mtiles * p.lddb * 4);
     p.o_mask = b.used; b.take((size_t)(R + 63) / 64 * 8);
     p.bwd_bytes = b.used;
     return p;
@@ -597,14 +626,14 @@ static int xent_check(const tsm_xent_desc* d, const char* who) {
 
 static size_t xent_ws(const XentPlan& p) { return p.fwd_bytes > p.bwd_bytes ? p.fwd_bytes : p.bwd_bytes; }
 
-template <typename T, int MODE, bool AK, bool BK>
+template <typename T, int MODE, bool AK, bool BK, bool DB = false>
 static int xent_product(const XentArgs& a, const XentPlan& p, int splits, const uint64_t* kmask, const char* what, hipStream_t s) {
     XentArgs b = a;
     if constexpr (sizeof(T) == 2) {
         if (p.main) {
             const long tiles = ((a.N + X_BN - 1) / X_BN) * ((a.M + X_BM - 1) / X_BM);
             const size_t smem = MODE == XE_GRAD ? (size_t)X_BM * (X_BN + 8) * 2 : (size_t)2 * (X_BM + X_BN) * XBK * 2;
-            auto kernel = xent_tile_kernel<MODE, X_BM, X_BN, X_WM, X_WN, AK, BK>;
+            auto kernel = xent_tile_kernel<MODE, X_BM, X_BN, X_WM, X_WN, MODE != XE_OUT ? X_ROWS : AK ? X_GROWS : X_GCOLS, BK ? X_ROWS : X_COLS, DB>;
             static bool configured = false;
             if (!configured) {
                 if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
@@ -667,9 +696,11 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
         a.M = R; a.N = n;
         a.e.bias = bias; a.e.labels = labels; a.e.classes = V; a.e.col0 = v0;
         a.e.lse = lse; a.e.dloss = dloss; a.e.G = G; a.e.ldg = p.ldg; a.e.dbias_part = dbias ? dbp : nullptr;
-        TSM_TRY((xent_product<T, XE_GRAD, true, true>(a, p, 1, nullptr, "xent_grad", s)));
+        a.e.lddb = p.lddb;
+        if (dbias) TSM_TRY((xent_product<T, XE_GRAD, true, true, true>(a, p, 1, nullptr, "xent_grad", s)));
+        else TSM_TRY((xent_product<T, XE_GRAD, true, true>(a, p, 1, nullptr, "xent_grad", s)));
         if (dbias) {
-            xent_colsum_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(dbp, p.mtiles, p.ldg, n, dbias + v0);
+            xent_colsum_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(dbp, p.mtiles, p.lddb, n, dbias + v0);
             TSM_TRY(check_launch("xent_dbias"));
         }
         if (dx) {
