@@ -7,6 +7,7 @@
 // joined over the tiles) and the label's logit.  Backward: s is formed again in pieces of the classes, a piece of G in the storage
 // type lives in the workspace for the two products that read it.  G is rounded once to the storage type, as the operands of the
 // matrix cores are; lse, the losses, db (from G before that rounding) and all sums are fp32.
+#include <type_traits>
 #include "internal.h"
 #include "args.h"
 #include "vec_any.h"
@@ -186,6 +187,9 @@ __device__ __forceinline__ void x_load_lds16(__amdgpu_buffer_rsrc_t r, unsigned 
 template <int VM> __device__ __forceinline__ void x_wait() {     // at most VM memory operations and no LDS access outstanding
     __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | (0 << 8) | ((VM >> 4) << 14));
 }
+__device__ __forceinline__ void x_wait_lds() {                    // no LDS access outstanding
+    __builtin_amdgcn_s_waitcnt(0xf | (7 << 4) | (0 << 8) | (3 << 14));
+}
 __device__ __forceinline__ void x_barrier() {
     asm volatile("" ::: "memory");   // (a fence would also wait for every load into LDS in flight)
     __builtin_amdgcn_s_barrier();
@@ -262,254 +266,369 @@ struct XOperand {
         const bool in = k < left && (KC || (mask >> k) & 1);
         x_load_lds16(x_rsrc(base), stage + i * (NT * 16) + wave_u * 1024, in ? off[i] : X_OOB, 0);
     }
-    // the 32 rows from row0 (a multiple of 32), K slice ks
-    __device__ __forceinline__ static x_bf16x8 frag(const unsigned char* stage, int row0, int ks, int lane) {
+    // Where a lane reads the fragment of the 32 rows from row0 (a multiple of 32), K consecutive: of slice ks, else of slice 0.
+    __device__ __forceinline__ static uint32_t frag_at(int row0, int ks, int lane) {
         if constexpr (KC) {
             const int r = lane & 31, hi = lane >> 5;
-            return *(const x_bf16x8*)(stage + (row0 + r) * PITCH + (((2 * ks + hi) ^ ((r >> 1) & 7)) * 16));
+            return (row0 + r) * PITCH + (((2 * ks + hi) ^ ((r >> 1) & 7)) * 16);
         } else {
             const int c = lane & 3, e = (lane >> 2) & 3, mblk = (lane >> 4) & 1, kg = lane >> 5;
-            const int g = (row0 / 16 + mblk) ^ swz(8 * kg + e);
-            const unsigned char* p = stage + (16 * ks + 8 * kg + e) * PITCH + g * 32 + c * 8;
-            const x_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) x_s16x4*)p);
-            const x_s16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) x_s16x4*)(p + 4 * PITCH));
-            return __builtin_bit_cast(x_bf16x8, (x_s16x8)__builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+            return (8 * kg + e) * PITCH + ((row0 / 16 + mblk) ^ swz(8 * kg + e)) * 32 + c * 8;
         }
     }
 };
 
+// The fragments of a K slice, four of A and two of B, read and waited for in one block: as separate reads the compiler, which
+// cannot tell the stage being read from the one that loads are on their way to, waits for those loads first.
+__device__ __forceinline__ x_bf16x8 x_join(x_s16x4 lo, x_s16x4 up) {
+    return __builtin_bit_cast(x_bf16x8, (x_s16x8)__builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// both with consecutive K: one address each, fragments 32 rows apart
+__device__ __forceinline__ void read_frags(uint32_t a, uint32_t b, x_bf16x8 (&fa)[4], x_bf16x8 (&fb)[2]) {
+    asm volatile("ds_read_b128 %0, %6\n ds_read_b128 %4, %7\n ds_read_b128 %1, %6 offset:4096\n ds_read_b128 %5, %7 offset:4096\n"
+                 "ds_read_b128 %2, %6 offset:8192\n ds_read_b128 %3, %6 offset:12288\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(fa[0]), "=&v"(fa[1]), "=&v"(fa[2]), "=&v"(fa[3]), "=&v"(fb[0]), "=&v"(fb[1])
+                 : "v"(a), "v"(b) : "memory");
+}
+// B through the transposing read: one address per fragmnt, slice OFF, its K 4 to 7 at OFF2
+template <int OFF, int OFF2>
+__device__ __forceinline__ void read_frags(uint32_t a, const uint32_t (&b)[2], x_bf16x8 (&fa)[4], x_bf16x8 (&fb)[2]) {
+    x_s16x4 l0, l1, u0, u1;
+    asm volatile("ds_read_b128 %0, %8\n ds_read_b64_tr_b16 %4, %9 offset:%11\n ds_read_b64_tr_b16 %5, %9 offset:%12\n"
+                 "ds_read_b128 %1, %8 offset:4096\n ds_read_b64_tr_b16 %6, %10 offset:%11\n ds_read_b64_tr_b16 %7, %10 offset:%12\n"
+                 "ds_read_b128 %2, %8 offset:8192\n ds_read_b128 %3, %8 offset:12288\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(fa[0]), "=&v"(fa[1]), "=&v"(fa[2]), "=&v"(fa[3]), "=&v"(l0), "=&v"(u0), "=&v"(l1), "=&v"(u1)
+                 : "v"(a), "v"(b[0]), "v"(b[1]), "n"(OFF), "n"(OFF2) : "memory");
+    fb[0] = x_join(l0, u0);
+    fb[1] = x_join(l1, u1);
+}
+// both through it
+template <int OFF, int OFF2>
+__device__ __forceinline__ void read_frags(const uint32_t (&a)[4], const uint32_t (&b)[2], x_bf16x8 (&fa)[4], x_bf16x8 (&fb)[2]) {
+    x_s16x4 l[6], u[6];
+    asm volatile("ds_read_b64_tr_b16 %0, %12 offset:%18\n ds_read_b64_tr_b16 %1, %12 offset:%19\n ds_read_b64_tr_b16 %8, %16 offset:%18\n"
+                 "ds_read_b64_tr_b16 %9, %16 offset:%19\n ds_read_b64_tr_b16 %2, %13 offset:%18\n ds_read_b64_tr_b16 %3, %13 offset:%19\n"
+                 "ds_read_b64_tr_b16 %10, %17 offset:%18\n ds_read_b64_tr_b16 %11, %17 offset:%19\n ds_read_b64_tr_b16 %4, %14 offset:%18\n"
+                 "ds_read_b64_tr_b16 %5, %14 offset:%19\n ds_read_b64_tr_b16 %6, %15 offset:%18\n ds_read_b64_tr_b16 %7, %15 offset:%19\n"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(l[0]), "=&v"(u[0]), "=&v"(l[1]), "=&v"(u[1]), "=&v"(l[2]), "=&v"(u[2]), "=&v"(l[3]), "=&v"(u[3]), "=&v"(l[4]), "=&v"(u[4]),
+                   "=&v"(l[5]), "=&v"(u[5])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b[0]), "v"(b[1]), "n"(OFF), "n"(OFF2) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fa[i] = x_join(l[i], u[i]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) fb[j] = x_join(l[4 + j], u[4 + j]);
+}
+
+// Two words that the two halves of a wavefront hold of adjacent column quads, x of quads 0 | 1, y of quads 2 | 3: afterwards the lower
+// half has quads 0, 1 and the upper half quads 2, 3.
+__device__ __forceinline__ void swap_halves(uint32_t& x, uint32_t& y) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(x, y, false, false));
+    x = r[0];
+    y = r[1];
+}
+
+// Sum over the 32 lanes of a half, in its last lane: within rows of 16 lanes by data-parallel moves, then across the two rows.
+template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
+    return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float sum32(float v) {
+    v = dpp_add<0xB1>(v);         // quad_perm 1 0 3 2
+    v = dpp_add<0x4E>(v);         // quad_perm 2 3 0 1
+    v = dpp_add<0x141>(v);        // row_half_mirror
+    v = dpp_add<0x140>(v);        // row_mirror
+    return v + __shfl_xor(v, 16, 64);
+}
+
+static constexpr int X_BM = 256, X_BN = 256, X_WM = 2, X_WN = 4, X_NT = X_WM * X_WN * 64, X_BLOCKS = 1 << 22;   // of one launch, at most
+static constexpr int X_STAGE = (X_BM + X_BN) * XBK * 2;
+static constexpr int X_SMEM = 2 * X_STAGE + X_WN * X_BM * 8 + X_BN * 4;   // two stages, row statistics, biases
+
+// One block per CU at a time.  (Persistent blocks that load a tile's first steps behind the epilogue of the tile before are no faster: the
+// epilogue is 3 of 58 us at 2048 features.)
 // DB: the column sums of G are wanted.
-template <int MODE, int BM, int BN, int WM, int WN, int AKIND, int BKIND, bool DB>
-__global__ void __launch_bounds__(WM * WN * 64) xent_tile_kernel(XentArgs a, const uint64_t* __restrict__ kmask) {
-    constexpr int NT = WM * WN * 64, MI = BM / (WM * 32), NJ = BN / (WN * 32), KS = XBK / 16;
+template <int MODE, int AKIND, int BKIND, bool DB>
+__global__ void __launch_bounds__(X_NT) xent_tile_kernel(XentArgs a, const uint64_t* __restrict__ kmask, long job0) {
+    constexpr int BM = X_BM, BN = X_BN, WM = X_WM, WN = X_WN, NT = X_NT, MI = BM / (WM * 32), NJ = BN / (WN * 32);
     typedef XOperand<BM, AKIND, NT> OpA;
     typedef XOperand<BN, BKIND, NT> OpB;
-    constexpr int STAGE = OpA::BYTES + OpB::BYTES;
     constexpr int NP = OpA::PIECES + OpB::PIECES;
     constexpr float L2E = 1.44269502f;
+    static_assert(MI == 4 && NJ == 2 && XBK == 64, "read_frags");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    float2* s_part = (float2*)(smem + 2 * X_STAGE);             // [WN][BM]; the column sums of G as floats [WM][BN]
+    float* s_bias = (float*)(smem + 2 * X_STAGE + WN * BM * 8); // [BN]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5, lo = lane & 31;
     const int wave_u = __builtin_amdgcn_readfirstlane(wave);
     const int wm = wave_u / WN, wn = wave_u % WN;
 
-    // Tiles: eight row tiles at a time, column by column; every XCD takes a stretch of that order, so that the tiles it works
-    // on at one time share their operands in its L2.
-    const long mtiles = (a.M + BM - 1) / BM, ntiles = (a.N + BN - 1) / BN, total = mtiles * ntiles;
-    long tile = blockIdx.x;
-    {
-        const long per = total / 8, more = total % 8, x = tile % 8, at = tile / 8;
-        tile = x * per + (x < more ? x : more) + at;
-    }
-    const long band = tile / (8 * ntiles), rest = tile - band * 8 * ntiles;
-    const long high = mtiles - band * 8 < 8 ? mtiles - band * 8 : 8;
-    const long mt = band * 8 + rest % high, nt = rest / high;
+    // Jobs: the tiles of every split of K, four row tiles at a time (eight where the classes run along columns), column by column.
+    // Every XCD takes a stretch of that order, so that the tiles it works on at one time share their operands in its L2 (bands
+    // of 2, 4, 8, 16, 32 row tiles: dw 4.23, 4.19, 4.42, 4.98, 5.24 ms of 8192 x 2048 x 131072, statistics 3.95, 3.89, 3.80, 3.90, 4.35).
+    constexpr int BAND = MODE == XE_OUT ? 4 : 8;
+    const long mtiles = (a.M + BM - 1) / BM, ntiles = (a.N + BN - 1) / BN, tiles = mtiles * ntiles;
+    const int njobs = gridDim.x;
+    const int xcd = blockIdx.x & 7;
+    const long job = job0 + xcd * (njobs / 8) + (xcd < njobs % 8 ? xcd : njobs % 8) + (blockIdx.x >> 3), tile = job % tiles, z = job / tiles;
+    const long band = tile / (BAND * ntiles), rest = tile - band * BAND * ntiles;
+    const long high = mtiles - band * BAND < BAND ? mtiles - band * BAND : BAND;
+    const long mt = band * BAND + rest % high, nt = rest / high;
     const long m0 = mt * BM, n0 = nt * BN;
-    const long kb = blockIdx.z * a.ksplit, ke = kb + a.ksplit < a.K ? kb + a.ksplit : a.K;
-
+    const long kb = z * a.ksplit, ke = kb + a.ksplit < a.K ? kb + a.ksplit : a.K;
+    const int steps = ke > kb ? (int)((ke - kb + XBK - 1) / XBK) : 0;
     OpA pa;
     OpB pb;
-    pa.init((const bf16_t*)a.A, a.lda, m0, a.M, kb, tid);
-    pb.init((const bf16_t*)a.B, a.ldb, n0, a.N, kb, tid);
-    const int steps = (int)((ke - kb + XBK - 1) / XBK);
-    const uint64_t* mp = kmask ? kmask + kb / 64 : nullptr;
-    auto load_step = [&](int stage, int kc) {
-        unsigned char* st = smem + stage * STAGE;
+    auto load_step = [&](int stage, int kc) {                   // the step at the operands' windows
+        unsigned char* st = smem + stage * X_STAGE;
         const long l = ke - kb - (long)kc * XBK;
         const int left = l < XBK ? (int)l : XBK;
-        const uint64_t mask = mp ? mp[kc] : ~0ull;
+        uint64_t mask = ~0ull;
+        if constexpr (AKIND == X_GCOLS) mask = ((const __attribute__((address_space(4))) uint64_t*)kmask)[kb / XBK + kc];
 #pragma unroll
         for (int q = 0; q < OpA::PIECES; ++q) pa.load(st, q, left, ~0ull, wave_u);
 #pragma unroll
         for (int q = 0; q < OpB::PIECES; ++q) pb.load(st + OpA::BYTES, q, left, mask, wave_u);
     };
-    x_f32x16 acc[MI][NJ];
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-
-    // One barrier per step, in front of its last group of products: behind it the next step is complete and this stage is free.
-    // A step's loads are issued in one go at the start of the step before: spread over its groups the last of them came late
-    // (17.6 and 19.5 ms for the largest listed pass); stages of 32 K, up to four steps ahead, gain nothing (18.0 ms), four wavefronts of
-    // 128 x 128 instead of eight of 128 x 64 lose (20.4 ms).
-    x_bf16x8 af[2][MI], bf[2][NJ];
-    auto frags = [&](int stage, int ks, int to) {
-        const unsigned char* st = smem + stage * STAGE;
-#pragma unroll
-        for (int i = 0; i < MI; ++i) af[to][i] = OpA::frag(st, wm * (BM / WM) + i * 32, ks, lane);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) bf[to][j] = OpB::frag(st + OpA::BYTES, wn * (BN / WN) + j * 32, ks, lane);
+    auto next_step = [&](int stage, int kc) {
+        pa.advance();
+        pb.advance();
+        load_step(stage, kc);
     };
-    if (steps > 0) {
-        load_step(0, 0);
-        x_wait<0>();
-        x_barrier();
-        frags(0, 0, 0);
-    }
-    for (int kc = 0; kc < steps; ++kc) {
-        const int cur = kc & 1, nxt = cur ^ 1;
-        const bool more = kc + 1 < steps;
-        if (more) {
-            pa.advance();
-            pb.advance();
-            load_step(nxt, kc + 1);
-        }
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)smem;
+    uint32_t aat[4], bat[4];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            if (ks + 1 < KS) {
-                frags(cur, ks + 1, (ks + 1) & 1);
+    for (int q = 0; q < 4; ++q) {
+        aat[q] = lds0 + (OpA::KC ? OpA::frag_at(wm * (BM / WM), q, lane) : OpA::frag_at(wm * (BM / WM) + q * 32, 0, lane));
+        if (OpB::KC || q < NJ) bat[q] = lds0 + OpA::BYTES + (OpB::KC ? OpB::frag_at(wn * (BN / WN), q, lane) : OpB::frag_at(wn * (BN / WN) + q * 32, 0, lane));
+    }
+    x_bf16x8 af[2][MI], bf[2][NJ];
+    auto read = [&](auto slice, int stage) {
+        constexpr int ks = decltype(slice)::value, f = ks & 1;
+        const uint32_t so = stage * X_STAGE;
+        if constexpr (OpA::KC && OpB::KC) {
+            read_frags(aat[ks] + so, bat[ks] + so, af[f], bf[f]);
+        } else {
+            const uint32_t b[2] = {bat[0] + so, bat[1] + so};
+            if constexpr (OpA::KC) {
+                read_frags<16 * ks * OpB::PITCH, (16 * ks + 4) * OpB::PITCH>(aat[ks] + so, b, af[f], bf[f]);
+            } else {
+                const uint32_t q[4] = {aat[0] + so, aat[1] + so, aat[2] + so, aat[3] + so};
+                read_frags<16 * ks * OpB::PITCH, (16 * ks + 4) * OpB::PITCH>(q, b, af[f], bf[f]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    x_f32x16 acc[MI][NJ];
+    auto multiply = [&](int f) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)      // the result's columns run along registers, its rows along lanes
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[f][j], af[f][i], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    typedef std::integral_constant<int, 0> S0;
+    typedef std::integral_constant<int, 1> S1;
+    typedef std::integral_constant<int, 2> S2;
+    typedef std::integral_constant<int, 3> S3;
+
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+        // One barrier per step, in front of its last group of products: behind it the next step is complete and this stage is
+        // free, and the loads of the step after next go to it, a whole step ahead of their barrier.  The reads of a slice wait on their
+        // own; of the two wavefronts of a SIMD one multiplies meanwhile.  ms of the largest listed pass: loads spread over the
+        // groups of the step before 19.5, at its start 17.6, behind its barrier 16.3, with the reads in one block each 15.5;
+        // stages of 32 K, up to four steps ahead, gained nothing (18.0 against 17.6), four wavefronts of 128 x 128 lose (20.4).
+        if (steps > 0) {
+            pa.init((const bf16_t*)a.A, a.lda, m0, a.M, kb, tid);
+            pb.init((const bf16_t*)a.B, a.ldb, n0, a.N, kb, tid);
+            load_step(0, 0);
+            if (steps > 1) {
+                next_step(1, 1);
+                x_wait<NP>();
             } else {
                 x_wait<0>();
-                x_barrier();
-                if (more) frags(nxt, 0, 0);
             }
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)      // the result's columns run along registers, its rows along lanes
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[ks & 1][j], af[ks & 1][i], acc[i][j], 0, 0, 0);
+            x_barrier();
+            read(S0{}, 0);
         }
-    }
+        for (int kc = 0; kc < steps; ++kc) {
+            const int cur = kc & 1, nxt = cur ^ 1;
+            multiply(0);
+            read(S1{}, cur);
+            multiply(1);
+            read(S2{}, cur);
+            multiply(0);
+            read(S3{}, cur);
+            x_wait<0>();
+            x_barrier();
+            multiply(1);
+            if (kc + 2 < steps) next_step(cur, kc + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            if (kc + 1 < steps) read(S0{}, nxt);
+        }
 
-    // ---- epilogue: this lane has row mrow(i), columns ncol(j, r) = .. + r % 4, four at a time
-    auto mrow = [&](int i) { return m0 + wm * (BM / WM) + i * 32 + lo; };
-    const long nw = n0 + wn * (BN / WN);
-    if constexpr (MODE != XE_OUT) {
-        const float* bias = a.e.bias ? a.e.bias + a.e.col0 : nullptr;
+        // ---- epilogue: rows mrow(i), columns nw + ncol(j, q) .. + 3
+        const int wrow = wm * (BM / WM) + lo;
+        auto mrow = [&](int i) { return m0 + wrow + i * 32; };
+        int label[MI];
+        float lse[MI], up[MI];
+        if constexpr (MODE != XE_OUT) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const long n = nw + j * 32 + 8 * q + 4 * hi;
-                float b[4];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) b[t] = bias && n + t < a.N ? bias[n + t] : 0.f;
-#pragma unroll
-                for (int i = 0; i < MI; ++i)
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) acc[i][j][4 * q + t] = n + t < a.N ? acc[i][j][4 * q + t] + b[t] : -__builtin_inff();
+            for (int i = 0; i < MI; ++i) {
+                const long m = mrow(i) < a.M ? mrow(i) : a.M - 1;
+                label[i] = a.e.labels[m];
+                if constexpr (MODE == XE_GRAD) {
+                    lse[i] = a.e.lse[m];
+                    up[i] = a.e.dloss[m];
+                }
             }
-    }
-    if constexpr (MODE == XE_STATS) {
-        float2* s_part = (float2*)smem;            // [WN][BM]   (nobody reads the stages any more: the last barrier is behind)
+            if (tid < BN) s_bias[tid] = a.e.bias && n0 + tid < a.N ? a.e.bias[a.e.col0 + n0 + tid] : 0.f;
+            __syncthreads();
+        }
+        const long nw = n0 + wn * (BN / WN);
+        const int cols = (int)(a.N - nw < BN / WN ? a.N - nw : BN / WN);     // of the wavefront's, those that there are
+        // where row i's label is among them, else below zero
+        auto label_col = [&](int i) {
+            const long ln = (long)label[i] - a.e.col0 - nw;
+            return mrow(i) < a.M && is_class(label[i], a.e.classes) && ln >= 0 && ln < cols ? (int)ln : -1;
+        };
+        auto ncol = [&](int j, int q) { return j * 32 + 8 * q + 4 * hi; };
+        if constexpr (MODE != XE_OUT) {
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const long m = mrow(i);
-            const long ln = m < a.M ? (long)a.e.labels[m] - a.e.col0 - nw : -1;    // the label among the wavefront's columns
-            if (__any(ln >= 0 && ln < BN / WN && nw + ln < a.N)) {
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float4 b = *(const float4*)(s_bias + wn * (BN / WN) + ncol(j, q));
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) {
+                        acc[i][j][4 * q] += b.x;
+                        acc[i][j][4 * q + 1] += b.y;
+                        acc[i][j][4 * q + 2] += b.z;
+                        acc[i][j][4 * q + 3] += b.w;
+                    }
+                }
+            if (n0 + BN > a.N) {                                // the last column tile: nothing behind the last class
 #pragma unroll
                 for (int j = 0; j < NJ; ++j)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (ln == j * 32 + 8 * (r / 4) + 4 * hi + r % 4 && nw + ln < a.N) a.e.picked[m] = acc[i][j][r];
+                        if (ncol(j, r / 4) + r % 4 >= cols)
+#pragma unroll
+                            for (int i = 0; i < MI; ++i) acc[i][j][r] = -__builtin_inff();
             }
-            float mx = -__builtin_inff();
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float from = mx == -__builtin_inff() ? 0.f : mx;       // (a row of minus infinities sums to zero)
-            float s = 0.f;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[i][j][r] - from) * L2E);
-            s += __shfl_xor(s, 32, 64);
-            if (hi == 0) s_part[wn * BM + wm * (BM / WM) + i * 32 + lo] = make_float2(mx, s);
         }
-        __syncthreads();
-        for (int r = tid; r < BM; r += NT)
-            if (m0 + r < a.M) {
-                float2 p = s_part[r];
+        if constexpr (MODE == XE_STATS) {
 #pragma unroll
-                for (int w = 1; w < WN; ++w) join_softmax(p.x, p.y, s_part[w * BM + r].x, s_part[w * BM + r].y);
-                a.e.part[nt * a.M + m0 + r] = p;
+            for (int i = 0; i < MI; ++i) {
+                __builtin_amdgcn_sched_barrier(0);               // one row at a time, within the registers
+                const long m = mrow(i);
+                const int ln = label_col(i);
+                if (__any(ln >= 0)) {
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (ln == ncol(j, r / 4) + r % 4) a.e.picked[m] = acc[i][j][r];
+                }
+                float mx = -__builtin_inff();
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
+                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                const float from = mx == -__builtin_inff() ? 0.f : mx;       // (a row of minus infinities sums to zero)
+                float s = 0.f;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[i][j][r] - from) * L2E);
+                s += __shfl_xor(s, 32, 64);
+                if (hi == 0) s_part[wn * BM + wrow + i * 32] = make_float2(mx, s);
             }
-    } else if constexpr (MODE == XE_GRAD) {
-        constexpr int LDC = BN + 8;                // [BM][LDC] bf16, then stored row by row
-        bf16_t* s_out = (bf16_t*)smem;
-        float colsum[DB ? NJ : 1][16];
-        if constexpr (DB)
+            x_wait_lds();
+            x_barrier();
+            if (tid < BM && m0 + tid < a.M) {
+                float2 p = s_part[tid];
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+                for (int w = 1; w < WN; ++w) join_softmax(p.x, p.y, s_part[w * BM + tid].x, s_part[w * BM + tid].y);
+                a.e.part[nt * a.M + m0 + tid] = p;
+            }
+        } else if constexpr (MODE == XE_GRAD) {
+            bf16_t* G = (bf16_t*)a.e.G + mt * a.e.ldg + nw * X_GTILE + wrow * XBK;      // the wavefront's block, this lane's row
+            static_assert(BM == X_GTILE && BN / WN == XBK, "a wavefront's columns are those of a block of G");
 #pragma unroll
-                for (int r = 0; r < 16; ++r) colsum[j][r] = 0.f;
+            for (int i = 0; i < MI; ++i) {
+                __builtin_amdgcn_sched_barrier(0);               // one row at a time, within the registers
+                const bool use = mrow(i) < a.M && is_class(label[i], a.e.classes);
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const long m = mrow(i);
-            const int label = m < a.M ? a.e.labels[m] : -1;
-            const bool use = is_class(label, a.e.classes);
-            const float up = use ? a.e.dloss[m] : 0.f, lse = use ? a.e.lse[m] : 0.f;
-            const long ln = use ? (long)label - a.e.col0 - nw : -1;
-            const bool here = __any(ln >= 0 && ln < BN / WN);
+                for (int j = 0; j < NJ; ++j)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+                    for (int r = 0; r < 16; ++r)                             // (zero behind the last class: s is minus infinity there)
+                        acc[i][j][r] = use ? up[i] * __builtin_amdgcn_exp2f((acc[i][j][r] - lse[i]) * L2E) : 0.f;
+                const int ln = label_col(i);
+                if (__any(ln >= 0)) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float g[4];
+                    for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        float p = __builtin_amdgcn_exp2f((acc[i][j][4 * q + t] - lse) * L2E);
-                        if (here && ln == j * 32 + 8 * q + 4 * hi + t) p -= 1.f;
-                        const bool in = use && nw + j * 32 + 8 * q + 4 * hi + t < a.N;
-                        g[t] = in ? up * p : 0.f;
-                        if constexpr (DB) colsum[j][4 * q + t] += g[t];
+                        for (int r = 0; r < 16; ++r)
+                            if (ln == ncol(j, r / 4) + r % 4) acc[i][j][r] -= up[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; q += 2) {
+                        uint32_t w0 = pack_bf16x2(acc[i][j][4 * q], acc[i][j][4 * q + 1]), w1 = pack_bf16x2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                        uint32_t w2 = pack_bf16x2(acc[i][j][4 * q + 4], acc[i][j][4 * q + 5]), w3 = pack_bf16x2(acc[i][j][4 * q + 6], acc[i][j][4 * q + 7]);
+                        swap_halves(w0, w2);
+                        swap_halves(w1, w3);
+                        *(any_u32x4*)(G + i * 32 * XBK + j * 32 + 8 * (q + hi)) = any_u32x4{w0, w1, w2, w3};
                     }
-                    *(uint2*)(s_out + (wm * (BM / WM) + i * 32 + lo) * LDC + wn * (BN / WN) + j * 32 + 8 * q + 4 * hi) =
-                        make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
-                }
-        }
-        __syncthreads();
-        // (the tile's four blocks of G follow one another)
-        static_assert(MODE != XE_GRAD || (BM == X_GTILE && BN == X_GTILE), "G's blocks");
-        any_u32x4* G = (any_u32x4*)((bf16_t*)a.e.G + mt * a.e.ldg + n0 * X_GTILE);
-        for (int q = tid; q < BM * BN / 8; q += NT) G[q] = *(const any_u32x4*)(s_out + q / 8 % BM * LDC + q / (8 * BM) * XBK + q % 8 * 8);
-        if constexpr (DB) {
-            // sums over the wavefront's rows, then over the wavefronts
-            __syncthreads();
-            float* s_sum = (float*)smem;           // [WM][BN]
+            if constexpr (DB) {
+                // sums over the wavefront's rows, then over the wavefronts
+                float* s_sum = (float*)s_part;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+                for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float t = colsum[j][r];
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
-                    if (lo == 0) s_sum[wm * BN + wn * (BN / WN) + j * 32 + 8 * (r / 4) + 4 * hi + r % 4] = t;
-                }
-            __syncthreads();
-            for (int c = tid; c < BN; c += NT)
-                if (n0 + c < a.N) {
-                    float t = s_sum[c];
-#pragma unroll
-                    for (int w = 1; w < WM; ++w) t += s_sum[w * BN + c];
-                    a.e.dbias_part[mt * a.e.lddb + n0 + c] = t;
-                }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const long m = mrow(i);
-            if (m >= a.M) continue;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const long n = nw + j * 32 + 8 * q + 4 * hi;       // (N is a multiple of 8)
-                    if (n >= a.N) continue;
-                    float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-                    if (a.e.acc) {
-                        const float4 o = *(const float4*)(a.e.acc + m * a.N + n);
-                        v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+                    for (int r = 0; r < 16; ++r) {
+                        const float t = sum32((acc[0][j][r] + acc[1][j][r]) + (acc[2][j][r] + acc[3][j][r]));
+                        if (lo == 31) s_sum[wm * BN + wn * (BN / WN) + ncol(j, r / 4) + r % 4] = t;
                     }
-                    if (a.e.out_f32) *(float4*)(a.e.out_f32 + (blockIdx.z * a.M + m) * a.N + n) = v;
-                    else *(uint2*)((bf16_t*)a.e.out + m * a.N + n) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-                }
+                x_wait_lds();
+                x_barrier();
+                if (tid < BN && n0 + tid < a.N) a.e.dbias_part[mt * a.e.lddb + n0 + tid] = s_sum[tid] + s_sum[BN + tid];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const long m = mrow(i);
+                if (m >= a.M) continue;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const long n = nw + ncol(j, q);       // (N is a multiple of 8)
+                        if (n >= a.N) continue;
+                        float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                        if (a.e.acc) {
+                            const float4 o = *(const float4*)(a.e.acc + m * a.N + n);
+                            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+                        }
+                        if (a.e.out_f32) *(float4*)(a.e.out_f32 + (z * a.M + m) * a.N + n) = v;
+                        else *(uint2*)((bf16_t*)a.e.out + m * a.N + n) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+                    }
+            }
         }
-    }
 }
 
 // bit r of word r / 64: row r has a label
@@ -576,8 +695,6 @@ struct XentPlan {
 
 static constexpr size_t XENT_G_BYTES = (size_t)512 << 20;   // of a piece of G, at most (a piece has 1024 classes at least)
 
-static constexpr int X_BM = 256, X_BN = 256, X_WM = 2, X_WN = 4;
-
 static int splits_of(long tiles, long K, long fill) {
     long z = tiles < fill ? fill / tiles : 1;
     const long most = K / 512 > 1 ? K / 512 : 1;
@@ -631,9 +748,8 @@ static int xent_product(const XentArgs& a, const XentPlan& p, int splits, const 
     XentArgs b = a;
     if constexpr (sizeof(T) == 2) {
         if (p.main) {
-            const long tiles = ((a.N + X_BN - 1) / X_BN) * ((a.M + X_BM - 1) / X_BM);
-            const size_t smem = MODE == XE_GRAD ? (size_t)X_BM * (X_BN + 8) * 2 : (size_t)2 * (X_BM + X_BN) * XBK * 2;
-            auto kernel = xent_tile_kernel<MODE, X_BM, X_BN, X_WM, X_WN, MODE != XE_OUT ? X_ROWS : AK ? X_GROWS : X_GCOLS, BK ? X_ROWS : X_COLS, DB>;
+            const long jobs = ((a.N + X_BN - 1) / X_BN) * ((a.M + X_BM - 1) / X_BM) * splits;
+            auto kernel = xent_tile_kernel<MODE, MODE != XE_OUT ? X_ROWS : AK ? X_GROWS : X_GCOLS, BK ? X_ROWS : X_COLS, DB>;
             static bool configured = false;
             if (!configured) {
                 if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
@@ -641,7 +757,8 @@ static int xent_product(const XentArgs& a, const XentPlan& p, int splits, const 
                 configured = true;
             }
             b.ksplit = ((a.K + splits - 1) / splits + 63) / 64 * 64;
-            kernel<<<dim3((unsigned)tiles, 1, (unsigned)splits), dim3(X_WM * X_WN * 64), smem, s>>>(b, kmask);
+            for (long j = 0; j < jobs; j += X_BLOCKS)
+                kernel<<<dim3((unsigned)(jobs - j < X_BLOCKS ? jobs - j : X_BLOCKS)), dim3(X_NT), X_SMEM, s>>>(b, kmask, j);
             return check_launch(what);
         }
     }
