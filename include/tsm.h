@@ -432,7 +432,7 @@ int tsm_layernorm_bwd(const tsm_layernorm_desc* d, const void* x, const void* dy
  * entries of G are rounded to bf16 for the two products (dbias is summed before that), everything else is fp32.
  * Logits of minus infinity (a bias that takes a class out) are classes without weight; where no class of a row is left
  * its lse is minus infinity, and its loss and gradients are NaN.  No output may overlap an input or another output.
- * Workspace of both calls: tsm_xent_workspace_bytes(desc).
+ * Workspace of both calls: tsm_xent_workspace_bytes(desc).  At most 2^21 features.
  * ---------------------------------------------------------------------- */
 typedef struct {
     int rows, features, classes;

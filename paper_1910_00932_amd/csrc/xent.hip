@@ -4,9 +4,13 @@
 //   G_rv = dloss_r (exp(s_rv - lse_r) - [v == label_r]);  dx = G w;  dw = G^T x;  db_v = sum_r G_rv
 //
 // Forward: tiles of s stay in registers; each leaves the maximum and the sum of exponentials of its columns per row (a softmax
-// joined over the tiles) and the label's logit.  Backward: s is formed again in pieces of the classes, a piece of G in the storage
-// type lives in the workspace for the two products that read it.  G is rounded once to the storage type, as the operands of the
-// matrix cores are; lse, the losses, db (from G before that rounding) and all sums are fp32.
+// joined over the tiles) and the label's logit.  Backward: s is formed again in pieces of the classes, a piece of G lives in the
+// workspace for the two products that read it.  Four products of rows x features x classes in all, on the bf16 matrix cores.
+//
+// bf16: G is rounded once, to the type of the matrix cores' operands; lse, the losses, db (from G before that rounding) and
+// all sums are fp32.  fp32: x, w and G are cut into three bf16 parts each, exactly (8 + 8 + 8 bits), and a product is the sum of the
+// six largest part products (the method of Henry, Tang and Heinecke, "Leveraging the bfloat16 artificial intelligence datatype for
+// higher-precision computations", 2019; what is left out is at most 2^-24 of it), one after the other along K, the small parts first.
 #include <type_traits>
 #include "internal.h"
 #include "args.h"
@@ -17,9 +21,10 @@ namespace tsm {
 typedef float x_f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 x_bf16x8 __attribute__((ext_vector_type(8)));
 
+
 struct XentEpi {
     // STATS
-    float2* part;            // [N tiles][M]: maximum and sum of exp(s - maximum) of a tile's columns
+    float2* part;            // [column tiles][M]: maximum and sum of exp(s - maximum) of a tile's columns
     float* picked;           // [M]: the label's logit
     // STATS and GRAD: columns are classes col0 + n of `classes`
     const float* bias;
@@ -27,23 +32,27 @@ struct XentEpi {
     long col0, classes;
     // GRAD
     const float *lse, *dloss;
-    void* G;                 // [M][ldg], zero behind the last column; the main tiles': blocks (X_GROWS), ldg elements per row tile
-    long ldg;
-    float* dbias_part;       // [M tiles][lddb], nullable
+    bf16_t* G;               // in blocks (X_GROWS): ldg elements per 256 rows, gplane from one part to the next
+    long ldg, gplane;
+    float* dbias_part;       // [row tiles][lddb]
     long lddb;
-    // OUT
-    const float* acc;        // fp32 [M][N] added to the result, nullable
+    uint64_t* mask;          // bit r % 64 of word r / 64: row r has a label; nullable
+    // OUT: [M][N]
+    const float* acc;        // fp32, added to the result, nullable
     float* out_f32;          // [splits][M][N], or
-    void* out;               // [M][N] in the storage type
+    bf16_t* out;
 };
 
 struct XentArgs {
-    const void *A, *B;
-    long lda, ldb, M, N, K, ksplit;    // ksplit: K of one split (grid.z)
-    const int32_t* klabels;            // rows k of B whose label is no class of `classes` count as zero; nullable
+    const bf16_t *A, *B;
+    long lda, ldb, aplane, bplane;     // elements from row to row (G: per 256 rows), from part to part
+    long M, N, K, ksplit;              // ksplit: K of one split, a multiple of 64
+    const uint64_t* kmask;             // OUT over the rows of G: rows of B that count as zero
+    long job0;
     XentEpi e;
 };
 
+enum { X_SMALL = 0, X_MID = 1, X_BIG = 2 };      // tiles of 64, 128, 256
 enum { XE_STATS = 0, XE_GRAD = 1, XE_OUT = 2 };
 
 __device__ __forceinline__ bool is_class(int label, long classes) { return label >= 0 && label < classes; }
@@ -57,119 +66,9 @@ __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float
     m = t;
 }
 
-// ---- the plain tile: 64 x 64 results, the four wavefronts take every fourth step of K ---------------------------------
-// AK / BK: the operand has K consecutive in memory ([rows][K]), else its rows are K ([K][rows]).
-template <typename T, bool KC>
-__device__ __forceinline__ void plain_frag(const T* P, long ld, long row, long rows, long k, long K, const int32_t* klabels, long classes,
-                                           typename RawVec<T, 16 / sizeof(T)>::type& f) {
-    constexpr int VE = 16 / sizeof(T);
-    if constexpr (KC) {
-        f = raw_load<T, VE>(P + row * ld + k, row < rows ? (int)(K - k < VE ? K - k : VE) : 0);
-    } else {
-        f = typename RawVec<T, VE>::type{};
-#pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            if (row < rows && k + e < K && (!klabels || is_class(klabels[k + e], classes))) {
-                if constexpr (sizeof(T) == 2) f[e >> 1] |= (uint32_t)P[(k + e) * ld + row] << (16 * (e & 1));
-                else f[e] = __float_as_uint(P[(k + e) * ld + row]);
-            }
-        }
-    }
-}
-
-template <typename T, int MODE, bool AK, bool BK>
-__global__ void __launch_bounds__(256) xent_plain_kernel(XentArgs a) {
-    constexpr int VE = 16 / sizeof(T), KSTEP = 2 * VE;
-    __shared__ float red[4][64][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hi = lane >> 5, lo = lane & 31;
-    const long ntiles = (a.N + 63) / 64, total = ntiles * ((a.M + 63) / 64);
-    const long kb = blockIdx.z * a.ksplit, ke = kb + a.ksplit < a.K ? kb + a.ksplit : a.K;
-    const T *A = (const T*)a.A, *B = (const T*)a.B;
-    for (long tile = blockIdx.x; tile < total; tile += gridDim.x) {
-    const long mt = tile / ntiles, nt = tile % ntiles;
-    const long m0 = mt * 64, n0 = nt * 64;
-    x_f32x16 acc[2][2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    for (long k0 = kb + wave * KSTEP; k0 < ke; k0 += 4 * KSTEP) {
-        typename RawVec<T, VE>::type fa[2], fb[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            plain_frag<T, AK>(A, a.lda, m0 + 32 * i + lo, a.M, k0 + hi * VE, ke, nullptr, 0, fa[i]);
-            plain_frag<T, BK>(B, a.ldb, n0 + 32 * i + lo, a.N, k0 + hi * VE, ke, a.klabels, a.e.classes, fb[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if constexpr (sizeof(T) == 2)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x_bf16x8, fa[i]), __builtin_bit_cast(x_bf16x8, fb[j]), acc[i][j], 0, 0, 0);
-                else
-#pragma unroll
-                    for (int e = 0; e < VE; ++e)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[i][e]), __uint_as_float(fb[j][e]), acc[i][j], 0, 0, 0);
-            }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) red[wave][i * 32 + 8 * (r / 4) + 4 * hi + r % 4][j * 32 + lo] = acc[i][j][r];
-    __syncthreads();
-    // one row of the tile at a time per wavefront, a column per lane
-    const long n = n0 + lane;
-    const long v = a.e.col0 + n;
-    const bool in = n < a.N;
-    const float bias = MODE != XE_OUT && in && a.e.bias ? a.e.bias[v] : 0.f;
-    float dbias = 0.f;
-    for (int q = 0; q < 16; ++q) {
-        const int row = wave * 16 + q;
-        const long m = m0 + row;
-        if (m >= a.M) break;
-        float s = (red[0][row][lane] + red[1][row][lane]) + (red[2][row][lane] + red[3][row][lane]);
-        if constexpr (MODE == XE_STATS) {
-            s = in ? s + bias : -__builtin_inff();
-            if (in && a.e.labels[m] == v) a.e.picked[m] = s;
-            float mx = s;
-            for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-            float t = in ? exp_below(s, mx) : 0.f;
-            for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
-            if (lane == 0) a.e.part[nt * a.M + m] = make_float2(mx, t);
-        } else if constexpr (MODE == XE_GRAD) {
-            const int label = a.e.labels[m];
-            float g = 0.f;
-            if (in && is_class(label, a.e.classes)) {
-                const float p = __expf(s + bias - a.e.lse[m]);
-                g = a.e.dloss[m] * (label == v ? p - 1.f : p);
-            }
-            dbias += g;
-            if (n < a.e.ldg) ((T*)a.e.G)[m * a.e.ldg + n] = Elem<T>::st(g);
-        } else if (in) {
-            if (a.e.acc) s += a.e.acc[m * a.N + n];
-            if (a.e.out_f32) a.e.out_f32[(blockIdx.z * a.M + m) * a.N + n] = s;
-            else ((T*)a.e.out)[m * a.N + n] = Elem<T>::st(s);
-        }
-    }
-    if constexpr (MODE == XE_GRAD) {
-        if (a.e.dbias_part) {
-            __syncthreads();
-            red[0][wave][lane] = dbias;
-            __syncthreads();
-            if (wave == 0 && in) a.e.dbias_part[mt * a.e.lddb + n] = (red[0][0][lane] + red[0][1][lane]) + (red[0][2][lane] + red[0][3][lane]);
-        }
-    }
-    __syncthreads();
-    }
-}
-
-// ---- the main tile: bf16, BM x BN results, eight wavefronts that share the operands through LDS -------------------------
-// Operands come 64 steps of K at a time, straight from memory into one of two LDS stages while the other is multiplied.  An
-// operand with consecutive K lies there as rows of 128 bytes whose eight 16-byte pieces are permuted by the row (piece ^ (row/2)%8),
+// ---- tiles: BM x BN results of wavefronts that share the operands through LDS ---------------------------------------------
+// Operands come 64 steps of K at a time, straight from memory into an LDS stage while another is multiplied.  An operand with
+// consecutive K lies there as rows of 128 bytes whose eight 16-byte pieces are permuted by the row (piece ^ (row/2)%8),
 // so that the 32 rows of a fragment read spread over all banks; one whose rows are K lies there as it does in memory, its
 // 32-byte granules permuted by K, and fragments are read through the transposing LDS read, four K of 16 columns at a time.
 static constexpr int XBK = 64;
@@ -198,11 +97,11 @@ __device__ __forceinline__ void x_barrier() {
 typedef short x_s16x4 __attribute__((ext_vector_type(4)));
 typedef short x_s16x8 __attribute__((ext_vector_type(8)));
 
-// How an operand lies in memory.  The blocks of G: [row tile][64 columns][256 rows], 32 KB each, so that a step of either product
-// reads stretches of 8 KB and more, where rows of G as such would be a 64 KB apart.
+// How an operand lies in memory.  The blocks of G: [256 rows][64 columns], 32 KB each, those of 256 rows after one another, so that a
+// step of either product reads stretches of 8 KB, where rows of G as such would lie 64 KB apart.
 enum { X_ROWS = 0, X_COLS = 1, X_GROWS = 2, X_GCOLS = 3 };     // [rows][K], [K][rows], G with its columns as K, with its rows as K
 
-// One operand of a tile: ROWS rows of the result's side.
+// One operand of a tile: ROWS rows of the result's side, loaded by NT threads.
 template <int ROWS, int KIND, int NT>
 struct XOperand {
     static constexpr bool KC = KIND == X_ROWS || KIND == X_GROWS;     // K consecutive in LDS
@@ -210,18 +109,20 @@ struct XOperand {
     static constexpr int PIECES = BYTES / (NT * 16);          // per thread and step
     static constexpr int RPP = KC ? NT / 8 : NT / (ROWS / 8); // rows of the LDS image per pass
     static constexpr int PITCH = KC ? XBK * 2 : ROWS * 2;     // its bytes
-    static constexpr int GMASK = ROWS / 16 - 1;               // granules of 16 columns
     uint32_t off[PIECES];         // byte offset in the step's window of this thread's pieces
     int kfirst;                   // KC: K of the piece, else K of the thread's row in a pass
-    const char* base;             // of the step's window
+    const char *base, *base0;     // of the step's window, of the first one of the first part
     long step;                    // bytes from one step to the next
-    int quarter;                  // X_GCOLS: steps into a row tile
+    int quarter, quarter0;        // X_GCOLS: steps into 256 rows
 
-    __device__ __forceinline__ static int swz(int k) { return ((((k & 3) << 1) | (((k >> 3) & 1) << 3))) & GMASK; }
+    // XOR of the granule number: four consecutive K and the two granules of a fragment fall on different banks
+    __device__ __forceinline__ static int swz(int k) {
+        return ROWS == 64 ? ((k >> 1) & 1) << 1 : ((((k & 3) << 1) | (((k >> 3) & 1) << 3))) & (ROWS / 16 - 1);
+    }
 
-    // row0: first row of the tile, rows: of the matrix; k0: first K.  ld: elements from row to row, for G from one row tile to the next.
+    // row0: first row of the tile, rows: of the matrix; k0: first K.
     __device__ __forceinline__ void init(const bf16_t* p, long ld, long row0, long rows, long k0, int tid) {
-        quarter = 0;
+        quarter0 = 0;
         if constexpr (KC) {
             const int r = tid / 8;
             const int kv = (tid % 8) ^ ((r >> 1) & 7);
@@ -230,8 +131,8 @@ struct XOperand {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
                 off[i] = row0 + i * RPP + r < rows ? (uint32_t)((i * RPP + r) * pitch * 2 + kv * 16) : X_OOB;
-            base = KIND == X_GROWS ? (const char*)(p + row0 / ROWS * ld + k0 * ROWS) : (const char*)(p + row0 * ld + k0);
-            step = KIND == X_GROWS ? ROWS * XBK * 2 : XBK * 2;
+            base0 = (const char*)(KIND == X_GROWS ? p + row0 / X_GTILE * ld + row0 % X_GTILE * XBK + k0 * X_GTILE : p + row0 * ld + k0);
+            step = KIND == X_GROWS ? X_GTILE * XBK * 2 : XBK * 2;
         } else {
             const int k = tid / (ROWS / 8), slot = tid % (ROWS / 8);
             kfirst = k;
@@ -242,14 +143,26 @@ struct XOperand {
                 off[i] = row0 + col < rows ? (uint32_t)(at * 2) : X_OOB;
             }
             if constexpr (KIND == X_GCOLS) {
-                quarter = (int)(k0 % X_GTILE / XBK);
-                base = (const char*)(p + k0 / X_GTILE * ld + row0 * X_GTILE + k0 % X_GTILE * XBK);
-                step = (ld - (X_GTILE - XBK) * XBK) * 2;       // into the next row tile
+                quarter0 = (int)(k0 % X_GTILE / XBK);
+                base0 = (const char*)(p + k0 / X_GTILE * ld + row0 * X_GTILE + k0 % X_GTILE * XBK);
+                step = (ld - (X_GTILE - XBK) * XBK) * 2;       // into the next 256 rows
             } else {
-                base = (const char*)(p + k0 * ld + row0);
+                base0 = (const char*)(p + k0 * ld + row0);
                 step = XBK * 2 * ld;
             }
         }
+        // (the same in all lanes, which the compiler has to know for a load's descriptor)
+        base0 = (const char*)uniform((uint64_t)base0);
+        step = (long)uniform((uint64_t)step);
+        quarter0 = __builtin_amdgcn_readfirstlane(quarter0);
+        restart(0);
+    }
+    __device__ __forceinline__ static uint64_t uniform(uint64_t v) {
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+    }
+    __device__ __forceinline__ void restart(long elements) {   // the first step again, of another part
+        base = base0 + elements * 2;
+        quarter = quarter0;
     }
     __device__ __forceinline__ void advance() {
         if constexpr (KIND == X_GCOLS) {
@@ -320,6 +233,72 @@ __device__ __forceinline__ void read_frags(const uint32_t (&a)[4], const uint32_
     for (int j = 0; j < 2; ++j) fb[j] = x_join(l[4 + j], u[4 + j]);
 }
 
+// the middle tiles' two and two
+__device__ __forceinline__ void read_frags(uint32_t a, uint32_t b, x_bf16x8 (&fa)[2], x_bf16x8 (&fb)[2]) {
+    asm volatile("ds_read_b128 %0, %4\n ds_read_b128 %2, %5\n ds_read_b128 %1, %4 offset:4096\n ds_read_b128 %3, %5 offset:4096\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(fa[0]), "=&v"(fa[1]), "=&v"(fb[0]), "=&v"(fb[1]) : "v"(a), "v"(b) : "memory");
+}
+template <int OFF, int OFF2>
+__device__ __forceinline__ void read_frags(uint32_t a, const uint32_t (&b)[2], x_bf16x8 (&fa)[2], x_bf16x8 (&fb)[2]) {
+    x_s16x4 l0, l1, u0, u1;
+    asm volatile("ds_read_b128 %0, %6\n ds_read_b64_tr_b16 %2, %7 offset:%9\n ds_read_b64_tr_b16 %3, %7 offset:%10\n"
+                 "ds_read_b128 %1, %6 offset:4096\n ds_read_b64_tr_b16 %4, %8 offset:%9\n ds_read_b64_tr_b16 %5, %8 offset:%10\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(fa[0]), "=&v"(fa[1]), "=&v"(l0), "=&v"(u0), "=&v"(l1), "=&v"(u1)
+                 : "v"(a), "v"(b[0]), "v"(b[1]), "n"(OFF), "n"(OFF2) : "memory");
+    fb[0] = x_join(l0, u0);
+    fb[1] = x_join(l1, u1);
+}
+template <int OFF, int OFF2>
+__device__ __forceinline__ void read_frags(const uint32_t (&a)[2], const uint32_t (&b)[2], x_bf16x8 (&fa)[2], x_bf16x8 (&fb)[2]) {
+    x_s16x4 l[4], u[4];
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n ds_read_b64_tr_b16 %1, %8 offset:%13\n ds_read_b64_tr_b16 %4, %10 offset:%12\n"
+                 "ds_read_b64_tr_b16 %5, %10 offset:%13\n ds_read_b64_tr_b16 %2, %9 offset:%12\n ds_read_b64_tr_b16 %3, %9 offset:%13\n"
+                 "ds_read_b64_tr_b16 %6, %11 offset:%12\n ds_read_b64_tr_b16 %7, %11 offset:%13\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(l[0]), "=&v"(u[0]), "=&v"(l[1]), "=&v"(u[1]), "=&v"(l[2]), "=&v"(u[2]), "=&v"(l[3]), "=&v"(u[3])
+                 : "v"(a[0]), "v"(a[1]), "v"(b[0]), "v"(b[1]), "n"(OFF), "n"(OFF2) : "memory");
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        fa[i] = x_join(l[i], u[i]);
+        fb[i] = x_join(l[2 + i], u[2 + i]);
+    }
+}
+// The small tiles' wavefronts have one fragment of each operand per slice: the four slices of a step in one block.
+__device__ __forceinline__ void read_step(const uint32_t (&a)[4], const uint32_t (&b)[4], x_bf16x8 (&fa)[4], x_bf16x8 (&fb)[4]) {
+    asm volatile("ds_read_b128 %0, %8\n ds_read_b128 %4, %12\n ds_read_b128 %1, %9\n ds_read_b128 %5, %13\n"
+                 "ds_read_b128 %2, %10\n ds_read_b128 %6, %14\n ds_read_b128 %3, %11\n ds_read_b128 %7, %15\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(fa[0]), "=&v"(fa[1]), "=&v"(fa[2]), "=&v"(fa[3]), "=&v"(fb[0]), "=&v"(fb[1]), "=&v"(fb[2]), "=&v"(fb[3])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]) : "memory");
+}
+// (PITCH of 128 bytes: slices 2048 bytes apart, K 4 to 7 at 512)
+__device__ __forceinline__ void read_step(const uint32_t (&a)[4], uint32_t b, x_bf16x8 (&fa)[4], x_bf16x8 (&fb)[4]) {
+    x_s16x4 l[4], u[4];
+    asm volatile("ds_read_b128 %0, %12\n ds_read_b64_tr_b16 %4, %16\n ds_read_b64_tr_b16 %5, %16 offset:512\n"
+                 "ds_read_b128 %1, %13\n ds_read_b64_tr_b16 %6, %16 offset:2048\n ds_read_b64_tr_b16 %7, %16 offset:2560\n"
+                 "ds_read_b128 %2, %14\n ds_read_b64_tr_b16 %8, %16 offset:4096\n ds_read_b64_tr_b16 %9, %16 offset:4608\n"
+                 "ds_read_b128 %3, %15\n ds_read_b64_tr_b16 %10, %16 offset:6144\n ds_read_b64_tr_b16 %11, %16 offset:6656\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(fa[0]), "=&v"(fa[1]), "=&v"(fa[2]), "=&v"(fa[3]), "=&v"(l[0]), "=&v"(u[0]), "=&v"(l[1]), "=&v"(u[1]), "=&v"(l[2]), "=&v"(u[2]),
+                   "=&v"(l[3]), "=&v"(u[3])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b) : "memory");
+#pragma unroll
+    for (int k = 0; k < 4; ++k) fb[k] = x_join(l[k], u[k]);
+}
+__device__ __forceinline__ void read_step(uint32_t a, uint32_t b, x_bf16x8 (&fa)[4], x_bf16x8 (&fb)[4]) {
+    x_s16x4 l[8], u[8];
+    asm volatile("ds_read_b64_tr_b16 %0, %16\n ds_read_b64_tr_b16 %1, %16 offset:512\n ds_read_b64_tr_b16 %8, %17\n ds_read_b64_tr_b16 %9, %17 offset:512\n"
+                 "ds_read_b64_tr_b16 %2, %16 offset:2048\n ds_read_b64_tr_b16 %3, %16 offset:2560\n ds_read_b64_tr_b16 %10, %17 offset:2048\n"
+                 "ds_read_b64_tr_b16 %11, %17 offset:2560\n ds_read_b64_tr_b16 %4, %16 offset:4096\n ds_read_b64_tr_b16 %5, %16 offset:4608\n"
+                 "ds_read_b64_tr_b16 %12, %17 offset:4096\n ds_read_b64_tr_b16 %13, %17 offset:4608\n ds_read_b64_tr_b16 %6, %16 offset:6144\n"
+                 "ds_read_b64_tr_b16 %7, %16 offset:6656\n ds_read_b64_tr_b16 %14, %17 offset:6144\n ds_read_b64_tr_b16 %15, %17 offset:6656\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(l[0]), "=&v"(u[0]), "=&v"(l[1]), "=&v"(u[1]), "=&v"(l[2]), "=&v"(u[2]), "=&v"(l[3]), "=&v"(u[3]), "=&v"(l[4]), "=&v"(u[4]),
+                   "=&v"(l[5]), "=&v"(u[5]), "=&v"(l[6]), "=&v"(u[6]), "=&v"(l[7]), "=&v"(u[7])
+                 : "v"(a), "v"(b) : "memory");
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        fa[k] = x_join(l[k], u[k]);
+        fb[k] = x_join(l[4 + k], u[4 + k]);
+    }
+}
+
 // Two words that the two halves of a wavefront hold of adjacent column quads, x of quads 0 | 1, y of quads 2 | 3: afterwards the lower
 // half has quads 0, 1 and the upper half quads 2, 3.
 __device__ __forceinline__ void swap_halves(uint32_t& x, uint32_t& y) {
@@ -341,24 +320,29 @@ __device__ __forceinline__ float sum32(float v) {
     return v + __shfl_xor(v, 16, 64);
 }
 
-static constexpr int X_BM = 256, X_BN = 256, X_WM = 2, X_WN = 4, X_NT = X_WM * X_WN * 64, X_BLOCKS = 1 << 22;   // of one launch, at most
-static constexpr int X_STAGE = (X_BM + X_BN) * XBK * 2;
-static constexpr int X_SMEM = 2 * X_STAGE + X_WN * X_BM * 8 + X_BN * 4;   // two stages, row statistics, biases
+// The two shapes of a tile.  The large one: eight wavefronts of 128 x 64, one block per CU, for whatever fills the chip with it.  The
+// small one: four of 32 x 32, two blocks per CU, loads three steps ahead, for the rest.
+struct XBig { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NS = 2; };
+struct XMid { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, NS = 2; };
+struct XSmall { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 4; };
+template <typename C> constexpr int x_stage() { return (C::BM + C::BN) * XBK * 2; }
+template <typename C> constexpr int x_smem() { return C::NS * x_stage<C>() + C::WN * C::BM * 8 + C::BN * 4; }   // stages, row statistics, biases
+static constexpr int X_LAUNCH = 1 << 22;   // blocks of one launch, at most
 
-// One block per CU at a time.  (Persistent blocks that load a tile's first steps behind the epilogue of the tile before are no faster: the
-// epilogue is 3 of 58 us at 2048 features.)
-// DB: the column sums of G are wanted.
-template <int MODE, int AKIND, int BKIND, bool DB>
-__global__ void __launch_bounds__(X_NT) xent_tile_kernel(XentArgs a, const uint64_t* __restrict__ kmask, long job0) {
-    constexpr int BM = X_BM, BN = X_BN, WM = X_WM, WN = X_WN, NT = X_NT, MI = BM / (WM * 32), NJ = BN / (WN * 32);
+// SPLIT: operands in three parts.  DB: the column sums of G are wanted.
+template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
+__global__ void __launch_bounds__(C::WM * C::WN * 64) xent_tile_kernel(XentArgs a) {
+    constexpr int BM = C::BM, BN = C::BN, WM = C::WM, WN = C::WN, NT = WM * WN * 64, MI = BM / (WM * 32), NJ = BN / (WN * 32);
+    constexpr bool BIG = NJ == 2;
+    static_assert((BIG && (MI == 4 || MI == 2)) || (MI == 1 && NJ == 1 && BN == 64), "read_frags, read_step");
+    constexpr int TM = BM / WM, TN = BN / WN, NS = C::NS, STAGE = x_stage<C>();
     typedef XOperand<BM, AKIND, NT> OpA;
     typedef XOperand<BN, BKIND, NT> OpB;
     constexpr int NP = OpA::PIECES + OpB::PIECES;
     constexpr float L2E = 1.44269502f;
-    static_assert(MI == 4 && NJ == 2 && XBK == 64, "read_frags");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    float2* s_part = (float2*)(smem + 2 * X_STAGE);             // [WN][BM]; the column sums of G as floats [WM][BN]
-    float* s_bias = (float*)(smem + 2 * X_STAGE + WN * BM * 8); // [BN]
+    float2* s_part = (float2*)(smem + NS * STAGE);              // [WN][BM]; the column sums of G as floats [WM][BN]
+    float* s_bias = (float*)(smem + NS * STAGE + WN * BM * 8);  // [BN]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5, lo = lane & 31;
     const int wave_u = __builtin_amdgcn_readfirstlane(wave);
     const int wm = wave_u / WN, wn = wave_u % WN;
@@ -370,97 +354,108 @@ __global__ void __launch_bounds__(X_NT) xent_tile_kernel(XentArgs a, const uint6
     const long mtiles = (a.M + BM - 1) / BM, ntiles = (a.N + BN - 1) / BN, tiles = mtiles * ntiles;
     const int njobs = gridDim.x;
     const int xcd = blockIdx.x & 7;
-    const long job = job0 + xcd * (njobs / 8) + (xcd < njobs % 8 ? xcd : njobs % 8) + (blockIdx.x >> 3), tile = job % tiles, z = job / tiles;
+    const long job = a.job0 + xcd * (njobs / 8) + (xcd < njobs % 8 ? xcd : njobs % 8) + (blockIdx.x >> 3), tile = job % tiles, z = job / tiles;
     const long band = tile / (BAND * ntiles), rest = tile - band * BAND * ntiles;
     const long high = mtiles - band * BAND < BAND ? mtiles - band * BAND : BAND;
     const long mt = band * BAND + rest % high, nt = rest / high;
     const long m0 = mt * BM, n0 = nt * BN;
     const long kb = z * a.ksplit, ke = kb + a.ksplit < a.K ? kb + a.ksplit : a.K;
-    const int steps = ke > kb ? (int)((ke - kb + XBK - 1) / XBK) : 0;
+    const int ksteps = ke > kb ? (int)((ke - kb + XBK - 1) / XBK) : 0, steps = ksteps * (SPLIT ? 6 : 1);
     OpA pa;
     OpB pb;
-    auto load_step = [&](int stage, int kc) {                   // the step at the operands' windows
-        unsigned char* st = smem + stage * X_STAGE;
+    int kc = 0, pair = 0;                                       // of the step at the operands' windows
+    auto load_step = [&](int stage) {
+        unsigned char* st = smem + stage * STAGE;
         const long l = ke - kb - (long)kc * XBK;
         const int left = l < XBK ? (int)l : XBK;
         uint64_t mask = ~0ull;
-        if constexpr (AKIND == X_GCOLS) mask = ((const __attribute__((address_space(4))) uint64_t*)kmask)[kb / XBK + kc];
+        if constexpr (AKIND == X_GCOLS) mask = ((const __attribute__((address_space(4))) uint64_t*)a.kmask)[kb / XBK + kc];
 #pragma unroll
         for (int q = 0; q < OpA::PIECES; ++q) pa.load(st, q, left, ~0ull, wave_u);
 #pragma unroll
         for (int q = 0; q < OpB::PIECES; ++q) pb.load(st + OpA::BYTES, q, left, mask, wave_u);
     };
-    auto next_step = [&](int stage, int kc) {
-        pa.advance();
-        pb.advance();
-        load_step(stage, kc);
+    auto next_step = [&](int stage) {
+        ++kc;
+        if (SPLIT && kc == ksteps) {                            // the next pair of parts: 2 0, 0 2, 1 1, 1 0, 0 1, 0 0
+            kc = 0;
+            ++pair;
+            pa.restart(a.aplane * ((0x001102 >> (4 * pair)) & 3));
+            pb.restart(a.bplane * ((0x010120 >> (4 * pair)) & 3));
+        } else {
+            pa.advance();
+            pb.advance();
+        }
+        load_step(stage);
     };
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)smem;
     uint32_t aat[4], bat[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        aat[q] = lds0 + (OpA::KC ? OpA::frag_at(wm * (BM / WM), q, lane) : OpA::frag_at(wm * (BM / WM) + q * 32, 0, lane));
-        if (OpB::KC || q < NJ) bat[q] = lds0 + OpA::BYTES + (OpB::KC ? OpB::frag_at(wn * (BN / WN), q, lane) : OpB::frag_at(wn * (BN / WN) + q * 32, 0, lane));
+        if (OpA::KC || q < MI) aat[q] = lds0 + (OpA::KC ? OpA::frag_at(wm * TM, q, lane) : OpA::frag_at(wm * TM + q * 32, 0, lane));
+        if (OpB::KC || q < NJ) bat[q] = lds0 + OpA::BYTES + (OpB::KC ? OpB::frag_at(wn * TN, q, lane) : OpB::frag_at(wn * TN + q * 32, 0, lane));
     }
-    x_bf16x8 af[2][MI], bf[2][NJ];
-    auto read = [&](auto slice, int stage) {
-        constexpr int ks = decltype(slice)::value, f = ks & 1;
-        const uint32_t so = stage * X_STAGE;
-        if constexpr (OpA::KC && OpB::KC) {
-            read_frags(aat[ks] + so, bat[ks] + so, af[f], bf[f]);
-        } else {
-            const uint32_t b[2] = {bat[0] + so, bat[1] + so};
-            if constexpr (OpA::KC) {
-                read_frags<16 * ks * OpB::PITCH, (16 * ks + 4) * OpB::PITCH>(aat[ks] + so, b, af[f], bf[f]);
-            } else {
-                const uint32_t q[4] = {aat[0] + so, aat[1] + so, aat[2] + so, aat[3] + so};
-                read_frags<16 * ks * OpB::PITCH, (16 * ks + 4) * OpB::PITCH>(q, b, af[f], bf[f]);
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-    };
     x_f32x16 acc[MI][NJ];
-    auto multiply = [&](int f) {
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)      // the result's columns run along registers, its rows along lanes
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[f][j], af[f][i], acc[i][j], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    typedef std::integral_constant<int, 0> S0;
-    typedef std::integral_constant<int, 1> S1;
-    typedef std::integral_constant<int, 2> S2;
-    typedef std::integral_constant<int, 3> S3;
-
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    if (steps > 0) {
+        pa.init(a.A, a.lda, m0, a.M, kb, tid);
+        pb.init(a.B, a.ldb, n0, a.N, kb, tid);
+        if constexpr (SPLIT) pa.restart(a.aplane * 2);
+        load_step(0);
+    }
+    if constexpr (BIG) {
+        x_bf16x8 af[2][MI], bf[2][NJ];
+        auto read = [&](auto slice, int stage) {
+            constexpr int ks = decltype(slice)::value, f = ks & 1;
+            const uint32_t so = stage * STAGE;
+            if constexpr (OpA::KC && OpB::KC) {
+                read_frags(aat[ks] + so, bat[ks] + so, af[f], bf[f]);
+            } else {
+                const uint32_t b[2] = {bat[0] + so, bat[1] + so};
+                if constexpr (OpA::KC) {
+                    read_frags<16 * ks * OpB::PITCH, (16 * ks + 4) * OpB::PITCH>(aat[ks] + so, b, af[f], bf[f]);
+                } else {
+                    uint32_t q[MI];
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+                    for (int i = 0; i < MI; ++i) q[i] = aat[i] + so;
+                    read_frags<16 * ks * OpB::PITCH, (16 * ks + 4) * OpB::PITCH>(q, b, af[f], bf[f]);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto multiply = [&](int f) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)      // the result's columns run along registers, its rows along lanes
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[f][j], af[f][i], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        typedef std::integral_constant<int, 0> S0;
+        typedef std::integral_constant<int, 1> S1;
+        typedef std::integral_constant<int, 2> S2;
+        typedef std::integral_constant<int, 3> S3;
         // One barrier per step, in front of its last group of products: behind it the next step is complete and this stage is
         // free, and the loads of the step after next go to it, a whole step ahead of their barrier.  The reads of a slice wait on their
         // own; of the two wavefronts of a SIMD one multiplies meanwhile.  ms of the largest listed pass: loads spread over the
         // groups of the step before 19.5, at its start 17.6, behind its barrier 16.3, with the reads in one block each 15.5;
-        // stages of 32 K, up to four steps ahead, gained nothing (18.0 against 17.6), four wavefronts of 128 x 128 lose (20.4).
+        // stages of 32 K, up to four steps ahead, gained nothing (18.0 against 17.6), four wavefronts of 128 x 128 lose (20.4).  Persistent
+        // blocks that load a tile's first steps behind the epilogue before are no faster (that epilogue is 3 of 58 us at 2048 features).
+        if (steps > 1) next_step(1);
         if (steps > 0) {
-            pa.init((const bf16_t*)a.A, a.lda, m0, a.M, kb, tid);
-            pb.init((const bf16_t*)a.B, a.ldb, n0, a.N, kb, tid);
-            load_step(0, 0);
-            if (steps > 1) {
-                next_step(1, 1);
-                x_wait<NP>();
-            } else {
-                x_wait<0>();
-            }
+            if (steps > 1) x_wait<NP>();
+            else x_wait<0>();
             x_barrier();
             read(S0{}, 0);
         }
-        for (int kc = 0; kc < steps; ++kc) {
-            const int cur = kc & 1, nxt = cur ^ 1;
+        for (int s = 0; s < steps; ++s) {
+            const int cur = s & 1, nxt = cur ^ 1;
             multiply(0);
             read(S1{}, cur);
             multiply(1);
@@ -470,172 +465,271 @@ __global__ void __launch_bounds__(X_NT) xent_tile_kernel(XentArgs a, const uint6
             x_wait<0>();
             x_barrier();
             multiply(1);
-            if (kc + 2 < steps) next_step(cur, kc + 2);
+            if (s + 2 < steps) next_step(cur);
             __builtin_amdgcn_sched_barrier(0);
-            if (kc + 1 < steps) read(S0{}, nxt);
+            if (s + 1 < steps) read(S0{}, nxt);
         }
-
-        // ---- epilogue: rows mrow(i), columns nw + ncol(j, q) .. + 3
-        const int wrow = wm * (BM / WM) + lo;
-        auto mrow = [&](int i) { return m0 + wrow + i * 32; };
-        int label[MI];
-        float lse[MI], up[MI];
-        if constexpr (MODE != XE_OUT) {
+    } else {
+        // One barrier per step: in front of it every wavefront waits for its loads of this step, behind it the stage of the step
+        // before is free.
+        if (steps > 1) next_step(1);
+        if (steps > 2) next_step(2);
+        int stage = 0;
+        for (int s = 0; s < steps; ++s) {
+            if (s + NS - 2 < steps) x_wait<(NS - 2) * NP>();
+            else x_wait<0>();
+            x_barrier();
+            if (s + NS - 1 < steps) next_step(stage == 0 ? NS - 1 : stage - 1);
+            x_bf16x8 fa[4], fb[4];
+            const uint32_t so = stage * STAGE;
+            const uint32_t q[4] = {aat[0] + so, aat[OpA::KC ? 1 : 0] + so, aat[OpA::KC ? 2 : 0] + so, aat[OpA::KC ? 3 : 0] + so};
+            const uint32_t b[4] = {bat[0] + so, bat[OpB::KC ? 1 : 0] + so, bat[OpB::KC ? 2 : 0] + so, bat[OpB::KC ? 3 : 0] + so};
+            if constexpr (OpA::KC && OpB::KC) read_step(q, b, fa, fb);
+            else if constexpr (OpA::KC) read_step(q, b[0], fa, fb);
+            else read_step(q[0], b[0], fa, fb);
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const long m = mrow(i) < a.M ? mrow(i) : a.M - 1;
-                label[i] = a.e.labels[m];
-                if constexpr (MODE == XE_GRAD) {
-                    lse[i] = a.e.lse[m];
-                    up[i] = a.e.dloss[m];
+            for (int k = 0; k < 4; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k], fa[k], acc[0][0], 0, 0, 0);
+            stage = stage + 1 == NS ? 0 : stage + 1;
+        }
+    }
+
+    // ---- epilogue: this lane has rows mrow(i), columns nw + ncol(j, q) .. + 3
+    const int wrow = wm * TM + lo;
+    auto mrow = [&](int i) { return m0 + wrow + i * 32; };
+    const long nw = n0 + wn * TN;
+    const int cols = (int)(a.N - nw < TN ? a.N - nw : TN);       // of the wavefront's, those that there are
+    auto ncol = [&](int j, int q) { return j * 32 + 8 * q + 4 * hi; };
+    int label[MI];
+    float lse[MI], up[MI];
+    // where row i's label is among the columns, else below zero
+    auto label_col = [&](int i) {
+        const long ln = (long)label[i] - a.e.col0 - nw;
+        return mrow(i) < a.M && is_class(label[i], a.e.classes) && ln >= 0 && ln < cols ? (int)ln : -1;
+    };
+    if constexpr (MODE != XE_OUT) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const long m = mrow(i) < a.M ? mrow(i) : a.M - 1;
+            label[i] = a.e.labels[m];
+            if constexpr (MODE == XE_GRAD) {
+                lse[i] = a.e.lse[m];
+                up[i] = a.e.dloss[m];
+            }
+        }
+        if (tid < BN) s_bias[tid] = a.e.bias && n0 + tid < a.N ? a.e.bias[a.e.col0 + n0 + tid] : 0.f;
+        if (MODE == XE_GRAD && a.e.mask && nt == 0 && tid < BM) {
+            const uint64_t b = __ballot(m0 + tid < a.M && is_class(a.e.labels[m0 + tid < a.M ? m0 + tid : 0], a.e.classes));
+            if (lane == 0) a.e.mask[(m0 + tid) / 64] = b;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float4 b = *(const float4*)(s_bias + wn * TN + ncol(j, q));
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    acc[i][j][4 * q] += b.x;
+                    acc[i][j][4 * q + 1] += b.y;
+                    acc[i][j][4 * q + 2] += b.z;
+                    acc[i][j][4 * q + 3] += b.w;
                 }
             }
-            if (tid < BN) s_bias[tid] = a.e.bias && n0 + tid < a.N ? a.e.bias[a.e.col0 + n0 + tid] : 0.f;
-            __syncthreads();
-        }
-        const long nw = n0 + wn * (BN / WN);
-        const int cols = (int)(a.N - nw < BN / WN ? a.N - nw : BN / WN);     // of the wavefront's, those that there are
-        // where row i's label is among them, else below zero
-        auto label_col = [&](int i) {
-            const long ln = (long)label[i] - a.e.col0 - nw;
-            return mrow(i) < a.M && is_class(label[i], a.e.classes) && ln >= 0 && ln < cols ? (int)ln : -1;
-        };
-        auto ncol = [&](int j, int q) { return j * 32 + 8 * q + 4 * hi; };
-        if constexpr (MODE != XE_OUT) {
+        if (n0 + BN > a.N) {                                     // the last column tile: nothing behind the last class
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float4 b = *(const float4*)(s_bias + wn * (BN / WN) + ncol(j, q));
+                for (int r = 0; r < 16; ++r)
+                    if (ncol(j, r / 4) + r % 4 >= cols)
 #pragma unroll
-                    for (int i = 0; i < MI; ++i) {
-                        acc[i][j][4 * q] += b.x;
-                        acc[i][j][4 * q + 1] += b.y;
-                        acc[i][j][4 * q + 2] += b.z;
-                        acc[i][j][4 * q + 3] += b.w;
-                    }
-                }
-            if (n0 + BN > a.N) {                                // the last column tile: nothing behind the last class
+                        for (int i = 0; i < MI; ++i) acc[i][j][r] = -__builtin_inff();
+        }
+    }
+    if constexpr (MODE == XE_STATS) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            __builtin_amdgcn_sched_barrier(0);                   // one row at a time, within the registers
+            const int ln = label_col(i);
+            if (__any(ln >= 0)) {
 #pragma unroll
                 for (int j = 0; j < NJ; ++j)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (ncol(j, r / 4) + r % 4 >= cols)
+                        if (ln == ncol(j, r / 4) + r % 4) a.e.picked[mrow(i)] = acc[i][j][r];
+            }
+            float mx = -__builtin_inff();
 #pragma unroll
-                            for (int i = 0; i < MI; ++i) acc[i][j][r] = -__builtin_inff();
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float from = mx == -__builtin_inff() ? 0.f : mx;           // (a row of minus infinities sums to zero)
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[i][j][r] - from) * L2E);
+            s += __shfl_xor(s, 32, 64);
+            if (hi == 0) s_part[wn * BM + wrow + i * 32] = make_float2(mx, s);
+        }
+        x_wait_lds();
+        x_barrier();
+        if (tid < BM && m0 + tid < a.M) {
+            float2 p = s_part[tid];
+#pragma unroll
+            for (int w = 1; w < WN; ++w) join_softmax(p.x, p.y, s_part[w * BM + tid].x, s_part[w * BM + tid].y);
+            a.e.part[nt * a.M + m0 + tid] = p;
+        }
+    } else if constexpr (MODE == XE_GRAD) {
+        // this lane's first row in the block of G that has the wavefront's columns
+        bf16_t* G = a.e.G + m0 / X_GTILE * a.e.ldg + nw / XBK * (X_GTILE * XBK) + (m0 % X_GTILE + wrow) * XBK + nw % XBK;
+        static_assert(TN == XBK || TN == 32, "a wavefront's columns are of one block of G");
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            __builtin_amdgcn_sched_barrier(0);                   // one row at a time, within the registers
+            const bool use = mrow(i) < a.M && is_class(label[i], a.e.classes);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)                                 // (zero behind the last class: s is minus infinity there)
+                    acc[i][j][r] = use ? up[i] * __builtin_amdgcn_exp2f((acc[i][j][r] - lse[i]) * L2E) : 0.f;
+            const int ln = label_col(i);
+            if (__any(ln >= 0)) {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (ln == ncol(j, r / 4) + r % 4) acc[i][j][r] -= up[i];
             }
         }
-        if constexpr (MODE == XE_STATS) {
+        if constexpr (DB) {
+            // sums over the wavefront's rows, then over the wavefronts
+            float* s_sum = (float*)s_part;
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                __builtin_amdgcn_sched_barrier(0);               // one row at a time, within the registers
-                const long m = mrow(i);
-                const int ln = label_col(i);
-                if (__any(ln >= 0)) {
+            for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j)
+                for (int r = 0; r < 16; ++r) {
+                    float t = acc[0][j][r];
 #pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (ln == ncol(j, r / 4) + r % 4) a.e.picked[m] = acc[i][j][r];
+                    for (int i = 1; i < MI; ++i) t += acc[i][j][r];
+                    t = sum32(t);
+                    if (lo == 31) s_sum[wm * BN + wn * TN + ncol(j, r / 4) + r % 4] = t;
                 }
-                float mx = -__builtin_inff();
+        }
+        constexpr int PARTS = SPLIT ? 3 : 1;
 #pragma unroll
-                for (int j = 0; j < NJ; ++j)
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
-                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-                const float from = mx == -__builtin_inff() ? 0.f : mx;       // (a row of minus infinities sums to zero)
-                float s = 0.f;
+            for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                for (int j = 0; j < NJ; ++j)
+                for (int q = 0; q < 4; q += 2) {
+                    float f[8];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[i][j][r] - from) * L2E);
-                s += __shfl_xor(s, 32, 64);
-                if (hi == 0) s_part[wn * BM + wrow + i * 32] = make_float2(mx, s);
-            }
+                    for (int t = 0; t < 8; ++t) f[t] = acc[i][j][4 * q + t];
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            w[t] = pack_bf16x2(f[2 * t], f[2 * t + 1]);
+                            if (part + 1 < PARTS) {
+                                f[2 * t] -= __uint_as_float(w[t] << 16);
+                                f[2 * t + 1] -= __uint_as_float(w[t] & 0xffff0000u);
+                            }
+                        }
+                        swap_halves(w[0], w[2]);
+                        swap_halves(w[1], w[3]);
+                        *(any_u32x4*)(G + part * a.e.gplane + i * 32 * XBK + j * 32 + 8 * (q + hi)) = any_u32x4{w[0], w[1], w[2], w[3]};
+                    }
+                }
+        if constexpr (DB) {
+            const float* s_sum = (const float*)s_part;
             x_wait_lds();
             x_barrier();
-            if (tid < BM && m0 + tid < a.M) {
-                float2 p = s_part[tid];
+            if (tid < BN && n0 + tid < a.N) {
+                float t = s_sum[tid];
 #pragma unroll
-                for (int w = 1; w < WN; ++w) join_softmax(p.x, p.y, s_part[w * BM + tid].x, s_part[w * BM + tid].y);
-                a.e.part[nt * a.M + m0 + tid] = p;
-            }
-        } else if constexpr (MODE == XE_GRAD) {
-            bf16_t* G = (bf16_t*)a.e.G + mt * a.e.ldg + nw * X_GTILE + wrow * XBK;      // the wavefront's block, this lane's row
-            static_assert(BM == X_GTILE && BN / WN == XBK, "a wavefront's columns are those of a block of G");
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                __builtin_amdgcn_sched_barrier(0);               // one row at a time, within the registers
-                const bool use = mrow(i) < a.M && is_class(label[i], a.e.classes);
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)                             // (zero behind the last class: s is minus infinity there)
-                        acc[i][j][r] = use ? up[i] * __builtin_amdgcn_exp2f((acc[i][j][r] - lse[i]) * L2E) : 0.f;
-                const int ln = label_col(i);
-                if (__any(ln >= 0)) {
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (ln == ncol(j, r / 4) + r % 4) acc[i][j][r] -= up[i];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int q = 0; q < 4; q += 2) {
-                        uint32_t w0 = pack_bf16x2(acc[i][j][4 * q], acc[i][j][4 * q + 1]), w1 = pack_bf16x2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-                        uint32_t w2 = pack_bf16x2(acc[i][j][4 * q + 4], acc[i][j][4 * q + 5]), w3 = pack_bf16x2(acc[i][j][4 * q + 6], acc[i][j][4 * q + 7]);
-                        swap_halves(w0, w2);
-                        swap_halves(w1, w3);
-                        *(any_u32x4*)(G + i * 32 * XBK + j * 32 + 8 * (q + hi)) = any_u32x4{w0, w1, w2, w3};
-                    }
-            if constexpr (DB) {
-                // sums over the wavefront's rows, then over the wavefronts
-                float* s_sum = (float*)s_part;
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float t = sum32((acc[0][j][r] + acc[1][j][r]) + (acc[2][j][r] + acc[3][j][r]));
-                        if (lo == 31) s_sum[wm * BN + wn * (BN / WN) + ncol(j, r / 4) + r % 4] = t;
-                    }
-                x_wait_lds();
-                x_barrier();
-                if (tid < BN && n0 + tid < a.N) a.e.dbias_part[mt * a.e.lddb + n0 + tid] = s_sum[tid] + s_sum[BN + tid];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const long m = mrow(i);
-                if (m >= a.M) continue;
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const long n = nw + ncol(j, q);       // (N is a multiple of 8)
-                        if (n >= a.N) continue;
-                        float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-                        if (a.e.acc) {
-                            const float4 o = *(const float4*)(a.e.acc + m * a.N + n);
-                            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
-                        }
-                        if (a.e.out_f32) *(float4*)(a.e.out_f32 + (z * a.M + m) * a.N + n) = v;
-                        else *(uint2*)((bf16_t*)a.e.out + m * a.N + n) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-                    }
+                for (int w = 1; w < WM; ++w) t += s_sum[w * BN + tid];
+                a.e.dbias_part[mt * a.e.lddb + n0 + tid] = t;
             }
         }
+    } else {
+        const bool whole = a.N % 4 == 0;                         // rows of whole quads, at their alignment
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const long m = mrow(i);
+            if (m >= a.M) continue;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const long n = nw + ncol(j, q);
+                    if (n >= a.N) continue;
+                    float v[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) v[t] = acc[i][j][4 * q + t];
+                    if (whole) {
+                        if (a.e.acc) {
+                            const float4 o = *(const float4*)(a.e.acc + m * a.N + n);
+                            v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w;
+                        }
+                        if (a.e.out_f32) *(float4*)(a.e.out_f32 + (z * a.M + m) * a.N + n) = make_float4(v[0], v[1], v[2], v[3]);
+                        else *(uint2*)(a.e.out + m * a.N + n) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                    } else {
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)
+                            if (n + t < a.N) {
+                                if (a.e.acc) v[t] += a.e.acc[m * a.N + n + t];
+                                if (a.e.out_f32) a.e.out_f32[(z * a.M + m) * a.N + n + t] = v[t];
+                                else a.e.out[m * a.N + n + t] = f32_to_bf16(v[t]);
+                            }
+                    }
+                }
+        }
+    }
 }
 
-// bit r of word r / 64: row r has a label
-__global__ void __launch_bounds__(256) xent_mask_kernel(const int32_t* __restrict__ labels, long rows, long classes, uint64_t* __restrict__ mask) {
-    for (long r = (long)blockIdx.x * 256 + threadIdx.x; r < (rows + 63) / 64 * 64; r += (long)gridDim.x * 256) {
-        const uint64_t b = __ballot(r < rows && is_class(labels[r], classes));
-        if ((threadIdx.x & 63) == 0) mask[r / 64] = b;
+// Rows of C values as operands: PARTS bf16 parts (fp32: three, exact), rows of Cp values, zero behind the C-th.
+template <typename T, int PARTS>
+__global__ void __launch_bounds__(256) xent_parts_kernel(const T* __restrict__ in, long rows, int C, int Cp, bf16_t* __restrict__ out, long plane) {
+    const long pieces = rows * (Cp / 8);
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (long)gridDim.x * 256) {
+        const long r = i / (Cp / 8);
+        const int c = (int)(i % (Cp / 8)) * 8;
+        const T* p = in + r * C + c;
+        float f[8];
+        if constexpr (sizeof(T) == 2) {
+            const auto v = raw_load<T, 8>(p, C - c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = raw_get<T>(v, e);
+        } else {
+            const auto v = raw_load<T, 4>(p, C - c), w = raw_load<T, 4>(p + 4, C - c - 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f[e] = raw_get<T>(v, e);
+                f[4 + e] = raw_get<T>(w, e);
+            }
+        }
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+            any_u32x4 o;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint32_t w = pack_bf16x2(f[2 * q], f[2 * q + 1]);
+                if constexpr (PARTS > 1) {
+                    // A finite value that rounds to infinity is cut off instead; what is infinite or NaN is so in its first part alone.
+                    float lo = __uint_as_float(w << 16), hi = __uint_as_float(w & 0xffff0000u);
+                    if (__builtin_isinf(lo) && !__builtin_isinf(f[2 * q])) w = (w & 0xffff0000u) | (__float_as_uint(f[2 * q]) >> 16);
+                    if (__builtin_isinf(hi) && !__builtin_isinf(f[2 * q + 1])) w = (w & 0xffffu) | (__float_as_uint(f[2 * q + 1]) & 0xffff0000u);
+                    lo = f[2 * q] - __uint_as_float(w << 16);
+                    hi = f[2 * q + 1] - __uint_as_float(w & 0xffff0000u);
+                    f[2 * q] = lo == lo ? lo : 0.f;
+                    f[2 * q + 1] = hi == hi ? hi : 0.f;
+                }
+                o[q] = w;
+            }
+            *(any_u32x4*)(out + part * plane + r * Cp + c) = o;
+        }
     }
 }
 
@@ -684,51 +778,79 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float* __restrict_
 // ---- host --------------------------------------------------------------------------------
 struct XentPlan {
     long piece, pieces;           // classes of a piece of G, number of pieces
-    long ldg, lddb;               // elements from row (main: row tile) to row of G, of the partial sums of db
-    long ntiles;                  // column tiles of the forward pass
-    long mtiles;                  // row tiles of G
-    int zdx, zdw;                 // splits of K of the two products
+    long Cp;                      // row pitch of x and w as operands
+    bool cut;                     // x and w are made into operands in the workspace
+    int size;                     // the tiles of s
+    int sizedx, sizedw;           // of the two products that read G
+    int zdx, zdw;                 // their splits of K
+    long ntiles, mtiles;          // tiles of s: of all columns, of the rows
+    long ldg, gplane, xplane, wplane, lddb;
     size_t fwd_bytes, bwd_bytes;
-    size_t o_part, o_picked, o_G, o_acc, o_dw, o_dbias, o_mask;
-    bool main;                    // on the main tiles
+    size_t o_x, o_w, o_part, o_picked, o_G, o_acc, o_dw, o_dbias, o_mask;
 };
 
 static constexpr size_t XENT_G_BYTES = (size_t)512 << 20;   // of a piece of G, at most (a piece has 1024 classes at least)
 
-static int splits_of(long tiles, long K, long fill) {
+static long x_tiles(long M, long N, int t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }
+
+static int x_tile(int size) { return size == X_BIG ? 256 : size == X_MID ? 128 : 64; }
+static int x_room(int size) { return size == X_BIG ? 256 : 512; }      // blocks that run at one time
+
+// Splits of K that fill the chip, each of 512 at least.
+static int x_splits(int size, long M, long N, long K) {
+    const long tiles = x_tiles(M, N, x_tile(size)), fill = x_room(size);
     long z = tiles < fill ? fill / tiles : 1;
     const long most = K / 512 > 1 ? K / 512 : 1;
     if (z > most) z = most;
     return (int)(z > 64 ? 64 : z);
 }
 
+// The largest tiles that fill half the chip, K split (split) or not, and are not more than half empty where the matrix is narrow.
+// us of the products with small, middle, large tiles: statistics of 1777 x 1000 x 32003 244, 150, 144, of 512 x 1024 x 10007 in fp32 111,
+// 83, 131, of 4 x 2048 x 65536 45, 45, 58, of 64 x 2048 x 400 17, 28, 50; dx of them 231, 131 + 11, 110 + 18 and 103, 72, 88.
+static int x_size(long M, long N, long K, bool split) {
+    const long narrow = M < N ? M : N;
+    for (int size = narrow > 128 ? X_BIG : X_MID; size > X_SMALL; --size)
+        if (x_tiles(M, N, x_tile(size)) * (split ? x_splits(size, M, N, K) : 1) >= x_room(size) / 2) return size;
+    return X_SMALL;
+}
+
 static XentPlan xent_plan(const tsm_xent_desc* d) {
     XentPlan p{};
-    const long R = d->rows, D = d->features, V = d->classes, es = (long)dtype_size(d->dtype);
-    p.main = d->dtype == TSM_BF16 && D % 8 == 0 && D <= (1 << 21);
-    const long bm = p.main ? X_BM : 64, bn = p.main ? X_BN : 64, fill = p.main ? 256 : 512;
-    p.ntiles = (V + bn - 1) / bn;
-    p.mtiles = (R + bm - 1) / bm;
-    Arena f(nullptr, 0);
-    p.o_part = f.used; f.take((size_t)p.ntiles * R * 8);
-    p.o_picked = f.used; f.take((size_t)R * 4);
-    p.fwd_bytes = f.used;
-    long piece = (long)(XENT_G_BYTES / es) / R / 1024 * 1024;
+    const long R = d->rows, D = d->features, V = d->classes;
+    const int parts = d->dtype == TSM_F32 ? 3 : 1;
+    p.cut = parts > 1 || D % 8 != 0;
+    p.Cp = (D + 7) / 8 * 8;
+    long piece = (long)(XENT_G_BYTES / (2 * parts)) / R / 1024 * 1024;
     if (piece < 1024) piece = 1024;
     if (piece > V) piece = V;
     p.piece = piece;
     p.pieces = (V + piece - 1) / piece;
+    p.size = x_size(R, piece, D, false);
+    const long t = x_tile(p.size);
+    p.ntiles = (p.pieces - 1) * ((piece + t - 1) / t) + (V - (p.pieces - 1) * piece + t - 1) / t;
+    p.mtiles = (R + t - 1) / t;
+    p.xplane = R * p.Cp;
+    p.wplane = piece * p.Cp;
+    p.ldg = (piece + t - 1) / t * t * X_GTILE;
+    p.gplane = (R + X_GTILE - 1) / X_GTILE * p.ldg;
     p.lddb = (piece + 7) / 8 * 8;
-    p.ldg = p.main ? (piece + X_GTILE - 1) / X_GTILE * X_GTILE * X_GTILE : p.lddb;
-    const long dt = (D + bn - 1) / bn;
-    p.zdx = p.pieces > 1 ? 1 : splits_of(p.mtiles * dt, V, fill);
-    p.zdw = splits_of((piece + bm - 1) / bm * dt, R, fill);
-    Arena b(nullptr, 0);
-    p.o_G = b.used; b.take((size_t)(p.main ? p.mtiles : R) * p.ldg * es);
-    p.o_acc = b.used; b.take(p.pieces > 1 || p.zdx > 1 ? (size_t)p.zdx * R * D * 4 : 0);
+    Arena f(nullptr, 0);
+    p.o_x = f.used; f.take(p.cut ? (size_t)parts * p.xplane * 2 : 0);
+    p.o_w = f.used; f.take(p.cut ? (size_t)parts * p.wplane * 2 : 0);
+    Arena b = f;
+    p.o_part = f.used; f.take((size_t)p.ntiles * R * 8);
+    p.o_picked = f.used; f.take((size_t)R * 4);
+    p.fwd_bytes = f.used;
+    p.sizedx = x_size(R, D, V, p.pieces == 1);
+    p.zdx = p.pieces > 1 ? 1 : x_splits(p.sizedx, R, D, V);
+    p.sizedw = x_size(piece, D, R, true);
+    p.zdw = x_splits(p.sizedw, piece, D, R);
+    p.o_G = b.used; b.take((size_t)parts * p.gplane * 2);
+    p.o_acc = b.used; b.take((parts == 1 && p.pieces > 1) || p.zdx > 1 ? (size_t)p.zdx * R * D * 4 : 0);
     p.o_dw = b.used; b.take(p.zdw > 1 ? (size_t)p.zdw * piece * D * 4 : 0);
     p.o_dbias = b.used; b.take((size_t)p.mtiles * p.lddb * 4);
-    p.o_mask = b.used; b.take((size_t)(R + 63) / 64 * 8);
+    p.o_mask = b.used; b.take((size_t)(R + 255) / 256 * 4 * 8);
     p.bwd_bytes = b.used;
     return p;
 }
@@ -737,35 +859,37 @@ static int xent_check(const tsm_xent_desc* d, const char* who) {
     if (!d) return fail(TSM_ERR_NULLPTR, "%s: null descriptor", who);
     if (d->dtype != TSM_F32 && d->dtype != TSM_BF16) return fail(TSM_ERR_DTYPE, "%s: unknown dtype %d", who, d->dtype);
     if (d->rows <= 0 || d->features <= 0 || d->classes <= 0) return fail(TSM_ERR_SHAPE, "%s: non-positive dimension", who);
+    if (d->features > (1 << 21)) return fail(TSM_ERR_SHAPE, "%s: more than 2^21 features", who);   // (a tile's offsets have 31 bits)
     if ((double)d->rows * d->features > 1e14 || (double)d->classes * d->features > 1e14) return fail(TSM_ERR_SHAPE, "%s: tensor too large", who);
     return TSM_OK;
 }
 
 static size_t xent_ws(const XentPlan& p) { return p.fwd_bytes > p.bwd_bytes ? p.fwd_bytes : p.bwd_bytes; }
 
-template <typename T, int MODE, bool AK, bool BK, bool DB = false>
-static int xent_product(const XentArgs& a, const XentPlan& p, int splits, const uint64_t* kmask, const char* what, hipStream_t s) {
-    XentArgs b = a;
-    if constexpr (sizeof(T) == 2) {
-        if (p.main) {
-            const long jobs = ((a.N + X_BN - 1) / X_BN) * ((a.M + X_BM - 1) / X_BM) * splits;
-            auto kernel = xent_tile_kernel<MODE, MODE != XE_OUT ? X_ROWS : AK ? X_GROWS : X_GCOLS, BK ? X_ROWS : X_COLS, DB>;
-            static bool configured = false;
-            if (!configured) {
-                if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-                    return fail(TSM_ERR_LAUNCH, "%s: cannot raise dynamic LDS limit", what);
-                configured = true;
-            }
-            b.ksplit = ((a.K + splits - 1) / splits + 63) / 64 * 64;
-            for (long j = 0; j < jobs; j += X_BLOCKS)
-                kernel<<<dim3((unsigned)(jobs - j < X_BLOCKS ? jobs - j : X_BLOCKS)), dim3(X_NT), X_SMEM, s>>>(b, kmask, j);
-            return check_launch(what);
-        }
+template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
+static int x_launch(XentArgs a, int splits, const char* what, hipStream_t s) {
+    auto kernel = xent_tile_kernel<C, MODE, AKIND, BKIND, SPLIT, DB>;
+    static bool configured = false;
+    if (!configured) {
+        if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
+            return fail(TSM_ERR_LAUNCH, "%s: cannot raise dynamic LDS limit", what);
+        configured = true;
     }
-    const long nt = (a.N + 63) / 64, mt = (a.M + 63) / 64;
-    b.ksplit = ((a.K + splits - 1) / splits + 63) / 64 * 64;
-    xent_plain_kernel<T, MODE, AK, BK><<<dim3((unsigned)(nt * mt < 65536 ? nt * mt : 65536), 1, (unsigned)splits), dim3(256), 0, s>>>(b);
-    return check_launch(what);
+    const long jobs = x_tiles(a.M, a.N, C::BM) * splits;
+    a.ksplit = ((a.K + splits - 1) / splits + XBK - 1) / XBK * XBK;
+    for (a.job0 = 0; a.job0 < jobs; a.job0 += X_LAUNCH) {
+        const long n = jobs - a.job0;
+        kernel<<<dim3((unsigned)(n < X_LAUNCH ? n : X_LAUNCH)), dim3(C::WM * C::WN * 64), x_smem<C>(), s>>>(a);
+        TSM_TRY(check_launch(what));
+    }
+    return TSM_OK;
+}
+
+template <int MODE, int AKIND, int BKIND, bool SPLIT, bool DB = false>
+static int x_product(int size, const XentArgs& a, int splits, const char* what, hipStream_t s) {
+    if (size == X_BIG) return x_launch<XBig, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+    if (size == X_MID) return x_launch<XMid, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+    return x_launch<XSmall, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
 }
 
 template <typename T>
@@ -775,70 +899,102 @@ static int xent_join(const float* part, int splits, long n, void* out, const cha
     return check_launch(what);
 }
 
+// Rows as operands: the caller's own where they can be, else made in the workspace.
+template <typename T>
+static int x_operand(const XentPlan& p, const void* in, long rows, int C, char* at, long plane, const bf16_t** out, hipStream_t s) {
+    *out = (const bf16_t*)in;
+    if (!p.cut) return TSM_OK;
+    *out = (const bf16_t*)at;
+    const long blocks = (rows * (p.Cp / 8) + 255) / 256;
+    xent_parts_kernel<T, sizeof(T) == 2 ? 1 : 3><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, s>>>((const T*)in, rows, C, (int)p.Cp, (bf16_t*)at, plane);
+    return check_launch("xent_parts");
+}
+
 template <typename T>
 static int xent_fwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, const void* w, const float* bias, const int32_t* labels, float* loss,
                     float* lse, char* ws, hipStream_t s) {
+    constexpr bool F32 = sizeof(T) == 4;
+    const long D = d->features, V = d->classes;
     XentArgs a{};
-    a.A = x; a.B = w;
-    a.lda = a.ldb = a.K = d->features;
-    a.M = d->rows; a.N = d->classes;
-    a.e.part = (float2*)(ws + p.o_part);
+    a.lda = a.ldb = p.Cp;
+    a.K = D;
+    a.M = d->rows;
+    a.aplane = p.xplane;
+    a.bplane = p.wplane;
     a.e.picked = (float*)(ws + p.o_picked);
-    a.e.bias = bias; a.e.labels = labels; a.e.classes = d->classes;
-    TSM_TRY((xent_product<T, XE_STATS, true, true>(a, p, 1, nullptr, "xent_stats", s)));
+    a.e.bias = bias; a.e.labels = labels; a.e.classes = V;
+    TSM_TRY(x_operand<T>(p, x, a.M, (int)D, ws + p.o_x, p.xplane, &a.A, s));
+    // (nothing of the pieces' size but the operands of w: where the caller's own serve, the classes go in one piece)
+    const long piece = p.cut ? p.piece : V, t = x_tile(p.size);
+    long tiles = 0;
+    for (long v0 = 0; v0 < V; v0 += piece) {
+        a.N = V - v0 < piece ? V - v0 : piece;
+        a.e.col0 = v0;
+        a.e.part = (float2*)(ws + p.o_part) + tiles * a.M;
+        TSM_TRY(x_operand<T>(p, (const T*)w + v0 * D, a.N, (int)D, ws + p.o_w, p.wplane, &a.B, s));
+        TSM_TRY((x_product<XE_STATS, X_ROWS, X_ROWS, F32>(p.size, a, 1, "xent_stats", s)));
+        tiles += (a.N + t - 1) / t;
+    }
     const long blocks = (a.M + 3) / 4;
-    xent_finish_kernel<<<dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s>>>(a.e.part, a.e.picked, labels, loss, lse, a.M, p.ntiles, d->classes);
+    xent_finish_kernel<<<dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s>>>((const float2*)(ws + p.o_part), a.e.picked, labels, loss, lse, a.M, tiles, V);
     return check_launch("xent_finish");
 }
 
 template <typename T>
 static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, const void* w, const float* bias, const int32_t* labels,
                     const float* lse, const float* dloss, void* dx, void* dw, float* dbias, char* ws, hipStream_t s) {
+    constexpr bool F32 = sizeof(T) == 4;
     const long R = d->rows, D = d->features, V = d->classes;
-    void* G = ws + p.o_G;
-    float *acc = (float*)(ws + p.o_acc), *dwp = (float*)(ws + p.o_dw), *dbp = (float*)(ws + p.o_dbias);
-    uint64_t* mask = nullptr;
-    if (dw && p.main) {
-        mask = (uint64_t*)(ws + p.o_mask);
-        const long blocks = (R + 255) / 256;
-        xent_mask_kernel<<<dim3((unsigned)(blocks < 1024 ? blocks : 1024)), dim3(256), 0, s>>>(labels, R, V, mask);
-        TSM_TRY(check_launch("xent_mask"));
-    }
+    bf16_t* G = (bf16_t*)(ws + p.o_G);
+    // fp32 results are added up where they go
+    float *acc = F32 && p.zdx == 1 ? (float*)dx : (float*)(ws + p.o_acc), *dwp = (float*)(ws + p.o_dw), *dbp = (float*)(ws + p.o_dbias);
+    uint64_t* mask = (uint64_t*)(ws + p.o_mask);
+    const bf16_t *xo, *wo;
+    TSM_TRY(x_operand<T>(p, x, R, (int)D, ws + p.o_x, p.xplane, &xo, s));
     for (long c = 0; c < p.pieces; ++c) {
         const long v0 = c * p.piece, n = V - v0 < p.piece ? V - v0 : p.piece;
-        const T* wc = (const T*)w + v0 * D;
+        TSM_TRY(x_operand<T>(p, (const T*)w + v0 * D, n, (int)D, ws + p.o_w, p.wplane, &wo, s));
         XentArgs a{};
-        a.A = x; a.B = wc;
-        a.lda = a.ldb = a.K = D;
-        a.M = R; a.N = n;
+        a.A = xo; a.B = wo;
+        a.lda = a.ldb = p.Cp;
+        a.aplane = p.xplane; a.bplane = p.wplane;
+        a.M = R; a.N = n; a.K = D;
         a.e.bias = bias; a.e.labels = labels; a.e.classes = V; a.e.col0 = v0;
-        a.e.lse = lse; a.e.dloss = dloss; a.e.G = G; a.e.ldg = p.ldg; a.e.dbias_part = dbias ? dbp : nullptr;
-        a.e.lddb = p.lddb;
-        if (dbias) TSM_TRY((xent_product<T, XE_GRAD, true, true, true>(a, p, 1, nullptr, "xent_grad", s)));
-        else TSM_TRY((xent_product<T, XE_GRAD, true, true>(a, p, 1, nullptr, "xent_grad", s)));
+        a.e.lse = lse; a.e.dloss = dloss; a.e.G = G; a.e.ldg = p.ldg; a.e.gplane = p.gplane;
+        a.e.mask = dw && c == 0 ? mask : nullptr;
         if (dbias) {
-            xent_colsum_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(dbp, p.mtiles, p.lddb, n, dbias + v0);
-            TSM_TRY(check_launch("xent_dbias"));
+            // one row tile: its sums are the result
+            a.e.dbias_part = p.mtiles == 1 ? dbias + v0 : dbp;
+            a.e.lddb = p.lddb;
+            TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, F32, true>(p.size, a, 1, "xent_grad", s)));
+            if (p.mtiles > 1) {
+                xent_colsum_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(dbp, p.mtiles, p.lddb, n, dbias + v0);
+                TSM_TRY(check_launch("xent_dbias"));
+            }
+        } else {
+            TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, F32>(p.size, a, 1, "xent_grad", s)));
         }
         if (dx) {
             XentArgs b{};
-            b.A = G; b.lda = p.ldg; b.B = wc; b.ldb = D;
+            b.A = G; b.lda = p.ldg; b.aplane = p.gplane;
+            b.B = wo; b.ldb = p.Cp; b.bplane = p.wplane;
             b.M = R; b.N = D; b.K = n;
             b.e.acc = c > 0 ? acc : nullptr;
-            if (p.zdx > 1 || c + 1 < p.pieces) b.e.out_f32 = acc;
-            else b.e.out = dx;
-            TSM_TRY((xent_product<T, XE_OUT, true, false>(b, p, p.zdx, nullptr, "xent_dx", s)));
+            if (F32 || p.zdx > 1 || c + 1 < p.pieces) b.e.out_f32 = acc;
+            else b.e.out = (bf16_t*)dx;
+            TSM_TRY((x_product<XE_OUT, X_GROWS, X_COLS, F32>(p.sizedx, b, p.zdx, "xent_dx", s)));
             if (p.zdx > 1) TSM_TRY(xent_join<T>(acc, p.zdx, R * D, dx, "xent_dx_join", s));
         }
         if (dw) {
             XentArgs b{};
-            b.A = G; b.lda = p.ldg; b.B = x; b.ldb = D;
+            b.A = G; b.lda = p.ldg; b.aplane = p.gplane;
+            b.B = xo; b.ldb = p.Cp; b.bplane = p.xplane;
             b.M = n; b.N = D; b.K = R;
-            b.klabels = labels; b.e.classes = V;
+            b.kmask = mask;
             T* out = (T*)dw + v0 * D;
-            if (p.zdw > 1) b.e.out_f32 = dwp;
-            else b.e.out = out;
-            TSM_TRY((xent_product<T, XE_OUT, false, false>(b, p, p.zdw, mask, "xent_dw", s)));
+            if (F32 || p.zdw > 1) b.e.out_f32 = p.zdw > 1 ? dwp : (float*)out;
+            else b.e.out = (bf16_t*)out;
+            TSM_TRY((x_product<XE_OUT, X_GCOLS, X_COLS, F32>(p.sizedw, b, p.zdw, "xent_dw", s)));
             if (p.zdw > 1) TSM_TRY(xent_join<T>(dwp, p.zdw, n * D, out, "xent_dw_join", s));
         }
     }
