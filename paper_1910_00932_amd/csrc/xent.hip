@@ -320,30 +320,34 @@ __device__ __forceinline__ float sum32(float v) {
     return v + __shfl_xor(v, 16, 64);
 }
 
-// The two shapes of a tile.  The large one: eight wavefronts of 128 x 64, one block per CU, for whatever fills the chip with it.  The
-// small one: four of 32 x 32, two blocks per CU, loads three steps ahead, for the rest.
-struct XBig { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NS = 2; };
-struct XMid { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, NS = 2; };
-struct XSmall { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 4; };
+// The shapes of a tile.  Large: eight wavefronts of 128 x 64, one block per CU, for whatever fills the chip with it.  Middle: four of
+// 64 x 64, two blocks per CU.  Small: four of 32 x 32, two blocks per CU, loads three steps ahead.  Deep: a small one by four groups of
+// wavefronts that take every fourth step of K each and add their sums up at the end, for fewer tiles than CUs.
+struct XBig { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NS = 2, KG = 1; };
+struct XMid { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, NS = 2, KG = 1; };
+struct XSmall { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 4, KG = 1; };
+struct XDeep { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 2, KG = 4; };
 template <typename C> constexpr int x_stage() { return (C::BM + C::BN) * XBK * 2; }
-template <typename C> constexpr int x_smem() { return C::NS * x_stage<C>() + C::WN * C::BM * 8 + C::BN * 4; }   // stages, row statistics, biases
+template <typename C> constexpr int x_smem() { return C::KG * C::NS * x_stage<C>() + C::WN * C::BM * 8 + C::BN * 4; }   // stages, row statistics, biases
 static constexpr int X_LAUNCH = 1 << 22;   // blocks of one launch, at most
 
 // SPLIT: operands in three parts.  DB: the column sums of G are wanted.
 template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
-__global__ void __launch_bounds__(C::WM * C::WN * 64) xent_tile_kernel(XentArgs a) {
+__global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(XentArgs a) {
     constexpr int BM = C::BM, BN = C::BN, WM = C::WM, WN = C::WN, NT = WM * WN * 64, MI = BM / (WM * 32), NJ = BN / (WN * 32);
     constexpr bool BIG = NJ == 2;
     static_assert((BIG && (MI == 4 || MI == 2)) || (MI == 1 && NJ == 1 && BN == 64), "read_frags, read_step");
-    constexpr int TM = BM / WM, TN = BN / WN, NS = C::NS, STAGE = x_stage<C>();
+    constexpr int TM = BM / WM, TN = BN / WN, NS = C::NS, KG = C::KG, STAGE = x_stage<C>();
+    static_assert(KG == 1 || (AKIND == X_ROWS && BKIND == X_ROWS), "groups skip steps");
     typedef XOperand<BM, AKIND, NT> OpA;
     typedef XOperand<BN, BKIND, NT> OpB;
     constexpr int NP = OpA::PIECES + OpB::PIECES;
     constexpr float L2E = 1.44269502f;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    float2* s_part = (float2*)(smem + NS * STAGE);              // [WN][BM]; the column sums of G as floats [WM][BN]
-    float* s_bias = (float*)(smem + NS * STAGE + WN * BM * 8);  // [BN]
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5, lo = lane & 31;
+    float2* s_part = (float2*)(smem + KG * NS * STAGE);         // [WN][BM]; the column sums of G as floats [WM][BN]
+    float* s_bias = (float*)(smem + KG * NS * STAGE + WN * BM * 8);     // [BN]
+    const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT), tid = threadIdx.x % NT;      // within the group
+    const int lane = tid & 63, wave = tid >> 6, hi = lane >> 5, lo = lane & 31;
     const int wave_u = __builtin_amdgcn_readfirstlane(wave);
     const int wm = wave_u / WN, wn = wave_u % WN;
 
@@ -365,7 +369,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * 64) xent_tile_kernel(XentArgs 
     OpB pb;
     int kc = 0, pair = 0;                                       // of the step at the operands' windows
     auto load_step = [&](int stage) {
-        unsigned char* st = smem + stage * STAGE;
+        unsigned char* st = smem + (group * NS + stage) * STAGE;
         const long l = ke - kb - (long)kc * XBK;
         const int left = l < XBK ? (int)l : XBK;
         uint64_t mask = ~0ull;
@@ -376,6 +380,16 @@ __global__ void __launch_bounds__(C::WM * C::WN * 64) xent_tile_kernel(XentArgs 
         for (int q = 0; q < OpB::PIECES; ++q) pb.load(st + OpA::BYTES, q, left, mask, wave_u);
     };
     auto next_step = [&](int stage) {
+        if constexpr (KG > 1) {                                 // this group's next step: KG further on
+            for (kc += KG; SPLIT && kc >= ksteps;) {
+                kc -= ksteps;
+                ++pair;
+            }
+            pa.restart(a.aplane * ((0x001102 >> (4 * pair)) & 3) * SPLIT + (long)kc * XBK);
+            pb.restart(a.bplane * ((0x010120 >> (4 * pair)) & 3) * SPLIT + (long)kc * XBK);
+            load_step(stage);
+            return;
+        }
         ++kc;
         if (SPLIT && kc == ksteps) {                            // the next pair of parts: 2 0, 0 2, 1 1, 1 0, 0 1, 0 0
             kc = 0;
@@ -407,7 +421,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * 64) xent_tile_kernel(XentArgs 
         pa.init(a.A, a.lda, m0, a.M, kb, tid);
         pb.init(a.B, a.ldb, n0, a.N, kb, tid);
         if constexpr (SPLIT) pa.restart(a.aplane * 2);
-        load_step(0);
+        if constexpr (KG == 1) load_step(0);
     }
     if constexpr (BIG) {
         x_bf16x8 af[2][MI], bf[2][NJ];
@@ -469,6 +483,40 @@ __global__ void __launch_bounds__(C::WM * C::WN * 64) xent_tile_kernel(XentArgs 
             __builtin_amdgcn_sched_barrier(0);
             if (s + 1 < steps) read(S0{}, nxt);
         }
+    } else if constexpr (KG > 1) {
+        kc = group - KG;
+        if (group < steps) next_step(0);
+        for (int s = 0; s < steps; s += KG) {                   // (as many barriers for every group)
+            const int stage = s / KG & 1;
+            x_wait<0>();
+            x_barrier();
+            if (s + KG + group < steps) next_step(stage ^ 1);
+            if (s + group < steps) {
+                x_bf16x8 fa[4], fb[4];
+                const uint32_t so = (group * NS + stage) * STAGE;
+                const uint32_t q[4] = {aat[0] + so, aat[1] + so, aat[2] + so, aat[3] + so}, b[4] = {bat[0] + so, bat[1] + so, bat[2] + so, bat[3] + so};
+                read_step(q, b, fa, fb);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k], fa[k], acc[0][0], 0, 0, 0);
+            }
+        }
+        x_wait<0>();
+        x_barrier();
+        float4* sums = (float4*)smem;                           // [KG - 1][4][NT]
+        if (group > 0) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                sums[((group - 1) * 4 + r) * NT + tid] = make_float4(acc[0][0][4 * r], acc[0][0][4 * r + 1], acc[0][0][4 * r + 2], acc[0][0][4 * r + 3]);
+        }
+        __syncthreads();
+        if (group > 0) return;                                  // (barriers are among the wavefronts that are left)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int g = 0; g < KG - 1; ++g) {
+                const float4 o = sums[(g * 4 + r) * NT + tid];
+                acc[0][0][4 * r] += o.x; acc[0][0][4 * r + 1] += o.y; acc[0][0][4 * r + 2] += o.z; acc[0][0][4 * r + 3] += o.w;
+            }
     } else {
         // One barrier per step: in front of it every wavefront waits for its loads of this step, behind it the stage of the step
         // before is free.
@@ -879,7 +927,7 @@ static int x_launch(XentArgs a, int splits, const char* what, hipStream_t s) {
     a.ksplit = ((a.K + splits - 1) / splits + XBK - 1) / XBK * XBK;
     for (a.job0 = 0; a.job0 < jobs; a.job0 += X_LAUNCH) {
         const long n = jobs - a.job0;
-        kernel<<<dim3((unsigned)(n < X_LAUNCH ? n : X_LAUNCH)), dim3(C::WM * C::WN * 64), x_smem<C>(), s>>>(a);
+        kernel<<<dim3((unsigned)(n < X_LAUNCH ? n : X_LAUNCH)), dim3(C::WM * C::WN * C::KG * 64), x_smem<C>(), s>>>(a);
         TSM_TRY(check_launch(what));
     }
     return TSM_OK;
@@ -889,6 +937,8 @@ template <int MODE, int AKIND, int BKIND, bool SPLIT, bool DB = false>
 static int x_product(int size, const XentArgs& a, int splits, const char* what, hipStream_t s) {
     if (size == X_BIG) return x_launch<XBig, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     if (size == X_MID) return x_launch<XMid, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+    if constexpr (MODE != XE_OUT)      // (us at 64 x 2048 x 400: 14.2 with small tiles, 10.3 with deep ones)
+        if (x_tiles(a.M, a.N, 64) <= 256 && a.K * (SPLIT ? 6 : 1) >= 512) return x_launch<XDeep, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     return x_launch<XSmall, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
 }
 
