@@ -15,6 +15,17 @@ namespace tsm {
 
 static constexpr int LN_NT = 256;
 
+// N values of a row vector from c0, zero behind the C-th
+template <int N>
+__device__ __forceinline__ void ln_params(const float* p, int c0, int C, float (&f)[N]) {
+#pragma unroll
+    for (int h = 0; h < N; h += 4) {
+        const auto v = raw_load<float, 4>(p + c0 + h, C - c0 - h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[h + e] = raw_get<float>(v, e);
+    }
+}
+
 // Sum over L adjacent lanes (L <= 64), or over the block's wavefronts as well (L == LN_NT; red: one slot per wavefront and
 // parity, so that two sums in a row need one barrier each).
 template <int L>
@@ -38,7 +49,12 @@ __global__ void __launch_bounds__(LN_NT) ln_fwd_kernel(const T* __restrict__ x, 
     constexpr int VE = Elem<T>::VEC;
     __shared__ float red[2][L > 64 ? LN_NT / 64 : 1];
     const int lane = threadIdx.x % L;
-    const float inv = 1.f / (float)C;
+    float gm[R][VE], bt[R][VE];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        ln_params<VE>(gamma, (lane + r * L) * VE, C, gm[r]);
+        ln_params<VE>(beta, (lane + r * L) * VE, C, bt[r]);
+    }
     for (long row = (long)blockIdx.x * (LN_NT / L) + threadIdx.x / L; row < rows; row += (long)gridDim.x * (LN_NT / L)) {
         const T* xr = x + row * C;
         typename RawVec<T, VE>::type raw[R];
@@ -59,7 +75,7 @@ __global__ void __launch_bounds__(LN_NT) ln_fwd_kernel(const T* __restrict__ x, 
                 const float d = (lane + r * L) * VE + e < C ? raw_get<T>(raw[r], e) - mean : 0.f;
                 q = fmaf(d, d, q);
             }
-        const float rstd = 1.f / sqrtf(ln_sum<L>(q, red[1]) * inv + eps);
+        const float rstd = 1.f / sqrtf(ln_sum<L>(q, red[1]) / (float)C + eps);
         if (lane == 0) {
             if (mean_out) mean_out[row] = mean;
             if (rstd_out) rstd_out[row] = rstd;
@@ -71,10 +87,7 @@ __global__ void __launch_bounds__(LN_NT) ln_fwd_kernel(const T* __restrict__ x, 
             if (c0 >= C) break;
             float f[VE];
 #pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const int c = c0 + e < C ? c0 + e : C - 1;
-                f[e] = fmaf((raw_get<T>(raw[r], e) - mean) * rstd, gamma[c], beta[c]);
-            }
+            for (int e = 0; e < VE; ++e) f[e] = fmaf((raw_get<T>(raw[r], e) - mean) * rstd, gm[r][e], bt[r][e]);
             raw_store<T, VE>(yr + c0, f, C - c0);
         }
     }
@@ -136,13 +149,11 @@ __global__ void __launch_bounds__(LN_NT) ln_bwd_kernel(const T* __restrict__ x, 
     const float inv = 1.f / (float)C;
     float gm[R][VE], ag[R][VE], ab[R][VE];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+        ln_params<VE>(gamma, (lane + r * L) * VE, C, gm[r]);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            const int c = (lane + r * L) * VE + e;
-            gm[r][e] = c < C ? gamma[c] : 0.f;
-            ag[r][e] = ab[r][e] = 0.f;
-        }
+        for (int e = 0; e < VE; ++e) ag[r][e] = ab[r][e] = 0.f;
+    }
     for (long row = (long)blockIdx.x * G + grp; row < rows; row += (long)gridDim.x * G) {
         typename RawVec<T, VE>::type rx[R], rd[R];
 #pragma unroll
@@ -309,7 +320,9 @@ __global__ void __launch_bounds__(1024) ln_join_kernel(const float* __restrict__
 }
 
 // ---- host --------------------------------------------------------------------------------
-static constexpr int LN_BLOCKS = 512;     // of the backward pass: two per CU, each writes one partial row
+// Blocks keep gamma and beta over their rows (200704 x 256 bf16: 512 52, 1024 37, 2048 36, 4096 48, 8192 67 us).
+static constexpr int LN_FWD_BLOCKS = 2048;
+static constexpr int LN_BLOCKS = 512;     // of the backward pass: two per CU, each writes one partial row (25088 x 2048 bf16: 256 73, 512 56, 1024 63 us)
 
 // Lanes and vectors per lane of a row; 0 lanes: the row exceeds a block's registers.  Few vectors per lane keep many rows in
 // flight, up to four they cost no barrier.
@@ -363,9 +376,9 @@ static int ln_fwd(const tsm_layernorm_desc* d, const void* x, const float* gamma
     int L, R;
     ln_shape(d->C, d->dtype, &L, &R);
     const int64_t jobs = L ? (d->rows + LN_NT / L - 1) / (LN_NT / L) : d->rows;
-    const dim3 grid((unsigned)(jobs < (1 << 22) ? jobs : (1 << 22))), block(LN_NT);
+    const dim3 grid((unsigned)(jobs < LN_FWD_BLOCKS ? jobs : LN_FWD_BLOCKS)), block(LN_NT);
 #define CALL(T, L, R) ln_fwd_kernel<T, L, R><<<grid, block, 0, s>>>((const T*)x, gamma, beta, (T*)y, mean, rstd, d->rows, d->C, d->eps)
-    if (L == 0) ln_fwd_long_kernel<T><<<grid, block, 0, s>>>((const T*)x, gamma, beta, (T*)y, mean, rstd, d->rows, d->C, d->eps);
+    if (L == 0) ln_fwd_long_kernel<T><<<dim3((unsigned)(jobs < (1 << 22) ? jobs : (1 << 22))), block, 0, s>>>((const T*)x, gamma, beta, (T*)y, mean, rstd, d->rows, d->C, d->eps);
     else LN_DISPATCH(T, CALL);
 #undef CALL
     return check_launch("layernorm_fwd");
