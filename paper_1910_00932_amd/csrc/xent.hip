@@ -702,7 +702,55 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
             }
         }
     } else {
-        const bool whole = a.N % 4 == 0;                         // rows of whole quads, at their alignment
+        // Whole vectors of 16 bytes: 32 rows of the wavefront at a time through LDS (behind the last barrier the stages are free, the small
+        // tiles' but for their last step), so that rows are stored in stretches of its columns, results past the caches
+        // (dw of 4 x 2048 x 65536, which is little but its store, 110 -> 65 us).
+        if (a.N % (a.e.out_f32 ? 4 : 8) == 0) {
+            if constexpr (!BIG) x_barrier();
+            constexpr int Q = TN / 4;                            // quads of a row, permuted by the row
+            float4* mine = (float4*)smem + wave_u * (32 * Q);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        mine[lo * Q + ((j * 8 + 2 * q + hi) ^ (lo & (Q - 1)))] = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                if (a.e.out_f32) {
+#pragma unroll
+                    for (int t = 0; t < 32 * Q / 64; ++t) {
+                        const int r = (t * 64 + lane) / Q, c = (t * 64 + lane) % Q;
+                        const long m = m0 + wm * TM + i * 32 + r, n = nw + c * 4;
+                        if (m >= a.M || n >= a.N) continue;
+                        const float4 v = mine[r * Q + (c ^ (r & (Q - 1)))];
+                        float f[4] = {v.x, v.y, v.z, v.w};
+                        if (a.e.acc) {
+                            const float4 o = *(const float4*)(a.e.acc + m * a.N + n);
+                            f[0] += o.x; f[1] += o.y; f[2] += o.z; f[3] += o.w;
+                        }
+                        float* to = a.e.out_f32 + (z * a.M + m) * a.N + n;
+                        if (a.ksplit < a.K) *(float4*)to = make_float4(f[0], f[1], f[2], f[3]);      // (read again soon)
+                        else raw_store<float, 4>(to, f, 4);
+                    }
+                } else {
+#pragma unroll
+                    for (int t = 0; t < 16 * Q / 64; ++t) {
+                        const int r = (t * 64 + lane) / (Q / 2), c = (t * 64 + lane) % (Q / 2);
+                        const long m = m0 + wm * TM + i * 32 + r, n = nw + c * 8;
+                        if (m >= a.M || n >= a.N) continue;
+                        const float4 v = mine[r * Q + ((2 * c) ^ (r & (Q - 1)))], w = mine[r * Q + ((2 * c + 1) ^ (r & (Q - 1)))];
+                        float f[8] = {v.x, v.y, v.z, v.w, w.x, w.y, w.z, w.w};
+                        if (a.e.acc) {
+                            const float4 o = *(const float4*)(a.e.acc + m * a.N + n), u = *(const float4*)(a.e.acc + m * a.N + n + 4);
+                            f[0] += o.x; f[1] += o.y; f[2] += o.z; f[3] += o.w;
+                            f[4] += u.x; f[5] += u.y; f[6] += u.z; f[7] += u.w;
+                        }
+                        raw_store<bf16_t, 8>(a.e.out + m * a.N + n, f, 8);
+                    }
+                }
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const long m = mrow(i);
@@ -710,41 +758,30 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const long n = nw + ncol(j, q);
+                for (int r = 0; r < 16; ++r) {
+                    const long n = nw + ncol(j, r / 4) + r % 4;
                     if (n >= a.N) continue;
-                    float v[4];
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) v[t] = acc[i][j][4 * q + t];
-                    if (whole) {
-                        if (a.e.acc) {
-                            const float4 o = *(const float4*)(a.e.acc + m * a.N + n);
-                            v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w;
-                        }
-                        if (a.e.out_f32) *(float4*)(a.e.out_f32 + (z * a.M + m) * a.N + n) = make_float4(v[0], v[1], v[2], v[3]);
-                        else *(uint2*)(a.e.out + m * a.N + n) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-                    } else {
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-                            if (n + t < a.N) {
-                                if (a.e.acc) v[t] += a.e.acc[m * a.N + n + t];
-                                if (a.e.out_f32) a.e.out_f32[(z * a.M + m) * a.N + n + t] = v[t];
-                                else a.e.out[m * a.N + n + t] = f32_to_bf16(v[t]);
-                            }
-                    }
+                    float v = acc[i][j][r];
+                    if (a.e.acc) v += a.e.acc[m * a.N + n];
+                    if (a.e.out_f32) a.e.out_f32[(z * a.M + m) * a.N + n] = v;
+                    else a.e.out[m * a.N + n] = f32_to_bf16(v);
                 }
         }
     }
 }
 
-// Rows of C values as operands: PARTS bf16 parts (fp32: three, exact), rows of Cp values, zero behind the C-th.
+// Rows of C values as operands: PARTS bf16 parts (fp32: three, exact), rows of Cp values, zero behind the C-th.  Two tensors in a launch.
 template <typename T, int PARTS>
-__global__ void __launch_bounds__(256) xent_parts_kernel(const T* __restrict__ in, long rows, int C, int Cp, bf16_t* __restrict__ out, long plane) {
-    const long pieces = rows * (Cp / 8);
+__global__ void __launch_bounds__(256) xent_parts_kernel(const T* __restrict__ in0, long rows0, bf16_t* __restrict__ out0, long plane0,
+                                                         const T* __restrict__ in1, long rows1, bf16_t* __restrict__ out1, long plane1, int C, int Cp) {
+    const long pieces = (rows0 + rows1) * (Cp / 8);
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (long)gridDim.x * 256) {
-        const long r = i / (Cp / 8);
+        const long row = i / (Cp / 8);
         const int c = (int)(i % (Cp / 8)) * 8;
-        const T* p = in + r * C + c;
+        const bool second = row >= rows0;
+        const long r = second ? row - rows0 : row, plane = second ? plane1 : plane0;
+        bf16_t* out = second ? out1 : out0;
+        const T* p = (second ? in1 : in0) + r * C + c;
         float f[8];
         if constexpr (sizeof(T) == 2) {
             const auto v = raw_load<T, 8>(p, C - c);
@@ -855,10 +892,10 @@ static int x_splits(int size, long M, long N, long K) {
 
 // The largest tiles that fill half the chip, K split (split) or not, and are not more than half empty where the matrix is narrow.
 // us of the products with small, middle, large tiles: statistics of 1777 x 1000 x 32003 244, 150, 144, of 512 x 1024 x 10007 in fp32 111,
-// 83, 131, of 4 x 2048 x 65536 45, 45, 58, of 64 x 2048 x 400 17, 28, 50; dx of them 231, 131 + 11, 110 + 18 and 103, 72, 88.
+// 83, 131, of 4 x 2048 x 65536 (w read from HBM) 61, 69, 75, of 64 x 2048 x 400 17, 28, 50; dx of them 231, 131 + 11, 110 + 18 and 103, 72, 88.
 static int x_size(long M, long N, long K, bool split) {
     const long narrow = M < N ? M : N;
-    for (int size = narrow > 128 ? X_BIG : X_MID; size > X_SMALL; --size)
+    for (int size = narrow > 128 ? X_BIG : narrow > 64 ? X_MID : X_SMALL; size > X_SMALL; --size)
         if (x_tiles(M, N, x_tile(size)) * (split ? x_splits(size, M, N, K) : 1) >= x_room(size) / 2) return size;
     return X_SMALL;
 }
@@ -949,14 +986,18 @@ static int xent_join(const float* part, int splits, long n, void* out, const cha
     return check_launch(what);
 }
 
-// Rows as operands: the caller's own where they can be, else made in the workspace.
+// x (with the first piece) and a piece of w as operands: the caller's own where they can be, else made in the workspace.
 template <typename T>
-static int x_operand(const XentPlan& p, const void* in, long rows, int C, char* at, long plane, const bf16_t** out, hipStream_t s) {
-    *out = (const bf16_t*)in;
+static int x_operands(const XentPlan& p, const void* x, long R, const void* w, long n, int C, char* ws, bool first, const bf16_t** xo, const bf16_t** wo,
+                      hipStream_t s) {
+    *xo = (const bf16_t*)x;
+    *wo = (const bf16_t*)w;
     if (!p.cut) return TSM_OK;
-    *out = (const bf16_t*)at;
-    const long blocks = (rows * (p.Cp / 8) + 255) / 256;
-    xent_parts_kernel<T, sizeof(T) == 2 ? 1 : 3><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, s>>>((const T*)in, rows, C, (int)p.Cp, (bf16_t*)at, plane);
+    *xo = (const bf16_t*)(ws + p.o_x);
+    *wo = (const bf16_t*)(ws + p.o_w);
+    const long rows = first ? R : 0, blocks = ((rows + n) * (p.Cp / 8) + 255) / 256;
+    xent_parts_kernel<T, sizeof(T) == 2 ? 1 : 3><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, s>>>(
+        (const T*)x, rows, (bf16_t*)(ws + p.o_x), p.xplane, (const T*)w, n, (bf16_t*)(ws + p.o_w), p.wplane, C, (int)p.Cp);
     return check_launch("xent_parts");
 }
 
@@ -973,7 +1014,6 @@ static int xent_fwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
     a.bplane = p.wplane;
     a.e.picked = (float*)(ws + p.o_picked);
     a.e.bias = bias; a.e.labels = labels; a.e.classes = V;
-    TSM_TRY(x_operand<T>(p, x, a.M, (int)D, ws + p.o_x, p.xplane, &a.A, s));
     // (nothing of the pieces' size but the operands of w: where the caller's own serve, the classes go in one piece)
     const long piece = p.cut ? p.piece : V, t = x_tile(p.size);
     long tiles = 0;
@@ -981,7 +1021,7 @@ static int xent_fwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
         a.N = V - v0 < piece ? V - v0 : piece;
         a.e.col0 = v0;
         a.e.part = (float2*)(ws + p.o_part) + tiles * a.M;
-        TSM_TRY(x_operand<T>(p, (const T*)w + v0 * D, a.N, (int)D, ws + p.o_w, p.wplane, &a.B, s));
+        TSM_TRY(x_operands<T>(p, x, a.M, (const T*)w + v0 * D, a.N, (int)D, ws, v0 == 0, &a.A, &a.B, s));
         TSM_TRY((x_product<XE_STATS, X_ROWS, X_ROWS, F32>(p.size, a, 1, "xent_stats", s)));
         tiles += (a.N + t - 1) / t;
     }
@@ -1000,10 +1040,9 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
     float *acc = F32 && p.zdx == 1 ? (float*)dx : (float*)(ws + p.o_acc), *dwp = (float*)(ws + p.o_dw), *dbp = (float*)(ws + p.o_dbias);
     uint64_t* mask = (uint64_t*)(ws + p.o_mask);
     const bf16_t *xo, *wo;
-    TSM_TRY(x_operand<T>(p, x, R, (int)D, ws + p.o_x, p.xplane, &xo, s));
     for (long c = 0; c < p.pieces; ++c) {
         const long v0 = c * p.piece, n = V - v0 < p.piece ? V - v0 : p.piece;
-        TSM_TRY(x_operand<T>(p, (const T*)w + v0 * D, n, (int)D, ws + p.o_w, p.wplane, &wo, s));
+        TSM_TRY(x_operands<T>(p, x, R, (const T*)w + v0 * D, n, (int)D, ws, c == 0, &xo, &wo, s));
         XentArgs a{};
         a.A = xo; a.B = wo;
         a.lda = a.ldb = p.Cp;
