@@ -403,7 +403,7 @@ int tsm_recur_bwd(const tsm_recur_desc* d, const void* x, const void* g, const f
  *         dgamma = sum over rows of dy * xhat, dbeta = sum over rows of dy (overwritten, summed in a fixed order)
  * x, y, dy, dx: `rows` dense rows of C values of dtype -- the pixels of a TSM_NTHWC tensor, or feature vectors.
  * gamma, beta, dgamma, dbeta: fp32 [C].  mean, rstd: fp32 [rows], written by the forward pass (each may be NULL there)
- * and read by the backward pass.  Any C.  No output may overlap an input or another output: TSM_ERR_SHAPE.
+ * and read by the backward pass.  Any C up to 2^30.  No output may overlap an input or another output: TSM_ERR_SHAPE.
  * Workspace (backward only): tsm_layernorm_workspace_bytes(desc).
  * ---------------------------------------------------------------------- */
 typedef struct {
@@ -429,7 +429,9 @@ int tsm_layernorm_bwd(const tsm_layernorm_desc* d, const void* x, const void* dy
  * loss, lse: fp32 [rows], per row; the mean of a batch is the caller's (dloss[r] = 1 / number of rows with a label).
  * dx, dw: the types of x and w, overwritten; dbias fp32; each may be NULL where it is not wanted, not all of them.
  * The backward pass forms the logits again, in pieces of the classes; lse is the forward pass's.  In TSM_BF16 the
- * entries of G are rounded to bf16 for the two products (dbias is summed before that), everything else is fp32.
+ * entries of G are rounded to bf16 for the two products (dbias is summed before that), everything else is fp32.  In
+ * TSM_F32 a product is the sum of six products of bf16 parts, good to 2^-24 of it for operands of 2^-110 and more; an
+ * infinite operand makes the sums it enters NaN.
  * Logits of minus infinity (a bias that takes a class out) are classes without weight; where no class of a row is left
  * its lse is minus infinity, and its loss and gradients are NaN.  No output may overlap an input or another output.
  * Workspace of both calls: tsm_xent_workspace_bytes(desc).  At most 2^21 features.

@@ -346,6 +346,39 @@ def tsm_lr_schedule(epoch, total_batch, warm_batch=8, warmup_epochs=5.0, total_e
     return v
 
 
+_TORCH_DTYPE = {TSM_F32: torch.float32, TSM_BF16: torch.bfloat16}
+
+
+def _arg(t, n, dtype, name):
+    """The pointer of a tensor of n elements of dtype (a tsm dtype or a torch one) on the current device; None stays None."""
+    if t is None or isinstance(t, int):
+        return t
+    p = _ptr(t)
+    want = _TORCH_DTYPE.get(dtype, dtype)
+    if t.dtype != want or t.numel() != n:
+        raise ValueError("%s: expected %d values of %s, got %d of %s" % (name, n, want, t.numel(), t.dtype))
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, t.device.index, torch.cuda.current_device()))
+    return p
+
+
+def _rows(t, n, name):
+    """Per-row statistics: at least n fp32 values."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.numel() < n:
+        raise ValueError("%s: expected at least %d values, got %d" % (name, n, t.numel()))
+    return _arg(t, t.numel(), torch.float32, name)
+
+
+def _saved(t, n):
+    if t is None or isinstance(t, int):
+        return t
+    if t.numel() * t.element_size() < n:
+        raise ValueError("saved: expected at least %d bytes, got %d" % (n, t.numel() * t.element_size()))
+    return _ptr(t)
+
+
 def tsm_recur_saved_bytes(desc):
     return int(lib().tsm_recur_saved_bytes(ctypes.addressof(desc)))
 
@@ -355,15 +388,22 @@ def tsm_recur_workspace_bytes(desc):
 
 
 def tsm_recur_fwd(desc, x, g, h0, y, h_last, saved, ws, stream=None):
-    p, n = _ws(ws)
-    _check(lib().tsm_recur_fwd(ctypes.addressof(desc), _ptr(x), _ptr(g), _ptr(h0), _ptr(y), _ptr(h_last), _ptr(saved), p, n,
-                               _stream(stream)))
+    m = desc.N * desc.C * desc.H * desc.W
+    n, dt, f = m * desc.T, desc.dtype, torch.float32
+    p, nb = _ws(ws)
+    _check(lib().tsm_recur_fwd(ctypes.addressof(desc), _arg(x, n, dt, "x"), _arg(g, n, dt, "g"), _arg(h0, m, f, "h0"),
+                               _arg(y, n, dt, "y"), _arg(h_last, m, f, "h_last"),
+                               _saved(saved, tsm_recur_saved_bytes(desc)) if saved is not None else None, p, nb, _stream(stream)))
 
 
 def tsm_recur_bwd(desc, x, g, h0, saved, dy, dh_last, dx, dg, dh0, ws, stream=None):
-    p, n = _ws(ws)
-    _check(lib().tsm_recur_bwd(ctypes.addressof(desc), _ptr(x), _ptr(g), _ptr(h0), _ptr(saved), _ptr(dy), _ptr(dh_last),
-                               _ptr(dx), _ptr(dg), _ptr(dh0), p, n, _stream(stream)))
+    m = desc.N * desc.C * desc.H * desc.W
+    n, dt, f = m * desc.T, desc.dtype, torch.float32
+    p, nb = _ws(ws)
+    _check(lib().tsm_recur_bwd(ctypes.addressof(desc), _arg(x, n, dt, "x"), _arg(g, n, dt, "g"), _arg(h0, m, f, "h0"),
+                               _saved(saved, tsm_recur_saved_bytes(desc)) if saved is not None else None,
+                               _arg(dy, n, dt, "dy"), _arg(dh_last, m, f, "dh_last"), _arg(dx, n, dt, "dx"),
+                               _arg(dg, n, dt, "dg"), _arg(dh0, m, f, "dh0"), p, nb, _stream(stream)))
 
 
 def tsm_layernorm_workspace_bytes(desc):
@@ -371,14 +411,19 @@ def tsm_layernorm_workspace_bytes(desc):
 
 
 def tsm_layernorm_fwd(desc, x, gamma, beta, y, mean, rstd, stream=None):
-    _check(lib().tsm_layernorm_fwd(ctypes.addressof(desc), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd),
-                                   _stream(stream)))
+    n, r, c, dt, f = desc.rows * desc.C, desc.rows, desc.C, desc.dtype, torch.float32
+    _check(lib().tsm_layernorm_fwd(ctypes.addressof(desc), _arg(x, n, dt, "x"), _arg(gamma, c, f, "gamma"),
+                                   _arg(beta, c, f, "beta"), _arg(y, n, dt, "y"), _rows(mean, r, "mean"),
+                                   _rows(rstd, r, "rstd"), _stream(stream)))
 
 
 def tsm_layernorm_bwd(desc, x, dy, gamma, mean, rstd, dx, dgamma, dbeta, ws, stream=None):
-    p, n = _ws(ws)
-    _check(lib().tsm_layernorm_bwd(ctypes.addressof(desc), _ptr(x), _ptr(dy), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dx),
-                                   _ptr(dgamma), _ptr(dbeta), p, n, _stream(stream)))
+    n, r, c, dt, f = desc.rows * desc.C, desc.rows, desc.C, desc.dtype, torch.float32
+    p, nb = _ws(ws)
+    _check(lib().tsm_layernorm_bwd(ctypes.addressof(desc), _arg(x, n, dt, "x"), _arg(dy, n, dt, "dy"),
+                                   _arg(gamma, c, f, "gamma"), _rows(mean, r, "mean"), _rows(rstd, r, "rstd"),
+                                   _arg(dx, n, dt, "dx"), _arg(dgamma, c, f, "dgamma"), _arg(dbeta, c, f, "dbeta"), p, nb,
+                                   _stream(stream)))
 
 
 def tsm_xent_workspace_bytes(desc):
@@ -386,12 +431,17 @@ def tsm_xent_workspace_bytes(desc):
 
 
 def tsm_xent_fwd(desc, x, w, bias, labels, loss, lse, ws, stream=None):
-    p, n = _ws(ws)
-    _check(lib().tsm_xent_fwd(ctypes.addressof(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), _ptr(loss), _ptr(lse), p, n,
-                              _stream(stream)))
+    r, d, v, dt, f = desc.rows, desc.features, desc.classes, desc.dtype, torch.float32
+    p, nb = _ws(ws)
+    _check(lib().tsm_xent_fwd(ctypes.addressof(desc), _arg(x, r * d, dt, "x"), _arg(w, v * d, dt, "w"),
+                              _arg(bias, v, f, "bias"), _arg(labels, r, torch.int32, "labels"), _arg(loss, r, f, "loss"),
+                              _arg(lse, r, f, "lse"), p, nb, _stream(stream)))
 
 
 def tsm_xent_bwd(desc, x, w, bias, labels, lse, dloss, dx, dw, dbias, ws, stream=None):
-    p, n = _ws(ws)
-    _check(lib().tsm_xent_bwd(ctypes.addressof(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), _ptr(lse), _ptr(dloss),
-                              _ptr(dx), _ptr(dw), _ptr(dbias), p, n, _stream(stream)))
+    r, d, v, dt, f = desc.rows, desc.features, desc.classes, desc.dtype, torch.float32
+    p, nb = _ws(ws)
+    _check(lib().tsm_xent_bwd(ctypes.addressof(desc), _arg(x, r * d, dt, "x"), _arg(w, v * d, dt, "w"),
+                              _arg(bias, v, f, "bias"), _arg(labels, r, torch.int32, "labels"), _arg(lse, r, f, "lse"),
+                              _arg(dloss, r, f, "dloss"), _arg(dx, r * d, dt, "dx"), _arg(dw, v * d, dt, "dw"),
+                              _arg(dbias, v, f, "dbias"), p, nb, _stream(stream)))

@@ -353,7 +353,7 @@ static int ln_check(const tsm_layernorm_desc* d, const char* who) {
     if (!d) return fail(TSM_ERR_NULLPTR, "%s: null descriptor", who);
     if (d->dtype != TSM_F32 && d->dtype != TSM_BF16) return fail(TSM_ERR_DTYPE, "%s: unknown dtype %d", who, d->dtype);
     if (d->rows <= 0 || d->C <= 0) return fail(TSM_ERR_SHAPE, "%s: non-positive dimension", who);
-    if (d->rows > ((int64_t)1 << 60) / d->C || d->C > 0x7fffff00) return fail(TSM_ERR_SHAPE, "%s: tensor too large", who);
+    if (d->rows > ((int64_t)1 << 60) / d->C || d->C > (1 << 30)) return fail(TSM_ERR_SHAPE, "%s: tensor too large", who);
     if (!(d->eps >= 0.f)) return fail(TSM_ERR_SHAPE, "%s: eps must not be negative or NaN", who);
     return TSM_OK;
 }

@@ -20,7 +20,7 @@
 
 namespace tsm {
 
-static constexpr int RC_NT = 256, RC_V = 4, RC_K = 8;     // threads, columns per thread (one where there are fewer), steps per thread
+static constexpr int RC_NT = 256, RC_V = 4, RC_STEPS = 8;   // threads, columns per thread (one where there are fewer), steps per thread (fewer for the shortest clips)
 static constexpr int RC_SAVE = 128;                       // steps between saved states
 
 struct RecurArgs {
@@ -129,7 +129,7 @@ struct RecurLds {
     }
 };
 
-template <typename T, int V, int SEG>
+template <typename T, int V, int SEG, int RC_K = RC_STEPS>
 __global__ void __launch_bounds__(RC_NT) recur_fwd_kernel(RecurArgs a) {
     constexpr int LC = RC_NT / SEG, STEPS = SEG * RC_K;
     typedef RecurCols<T, V> Cols;
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(RC_NT) recur_fwd_kernel(RecurArgs a) {
 
 // The tiles of a span from the last to the first.  STEPS is a multiple of RC_SAVE or T does not exceed it, so that the state in
 // front of every tile is at hand.
-template <typename T, int V, int SEG>
+template <typename T, int V, int SEG, int RC_K = RC_STEPS>
 __global__ void __launch_bounds__(RC_NT) recur_bwd_kernel(RecurArgs a) {
     constexpr int LC = RC_NT / SEG, STEPS = SEG * RC_K;
     typedef RecurCols<T, V> Cols;
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(RC_NT) recur_bwd_kernel(RecurArgs a) {
 // in front of it, or (BWD) E in front of it as a map of E behind it.
 template <typename T, int V, bool BWD>
 __global__ void __launch_bounds__(RC_NT) recur_span_kernel(RecurArgs a, int steps_per_span) {
-    constexpr int SEG = 16, LC = RC_NT / SEG, STEPS = SEG * RC_K;
+    constexpr int SEG = 16, LC = RC_NT / SEG, RC_K = RC_STEPS, STEPS = SEG * RC_K;
     typedef RecurCols<T, V> Cols;
     typedef RecurLds<SEG, 2, V> Lds;
     __shared__ Lds lds;
@@ -463,8 +463,8 @@ static RecurPlan recur_plan(const tsm_recur_desc* d, bool bwd) {
     RecurPlan p;
     const long M = (long)d->C * d->H * d->W;
     p.v = M < RC_V ? 1 : RC_V;
-    p.seg = d->T <= RC_K ? 1 : d->T <= 4 * RC_K ? 4 : d->T <= 8 * RC_K ? 8 : 16;
-    const int steps = p.seg * RC_K, tiles = cdiv(d->T, steps), width = RC_NT / p.seg * p.v;
+    p.seg = d->T <= RC_STEPS ? 1 : d->T <= 4 * RC_STEPS ? 4 : d->T <= 8 * RC_STEPS ? 8 : 16;
+    const int steps = p.seg * RC_STEPS, tiles = cdiv(d->T, steps), width = RC_NT / p.seg * p.v;
     p.cblocks = (M + width - 1) / width;
     const long blocks = p.cblocks * d->N;
     long want = blocks <= (bwd ? 224 : 160) ? 1024 / blocks : 1;
@@ -509,17 +509,19 @@ static int recur_run(const RecurArgs& a, const RecurPlan& p, bool bwd, hipStream
     if (p.spans > 1) {
         const long jobs = (a.M + 16 * V - 1) / (16 * V) * a.N * a.spans;
         const dim3 sgrid((unsigned)(jobs < cap ? jobs : cap));
-        const int steps = a.tiles_per_span * p.seg * RC_K;
+        const int steps = a.tiles_per_span * p.seg * RC_STEPS;
         if (bwd) recur_span_kernel<T, V, true><<<sgrid, block, 0, s>>>(a, steps);
         else recur_span_kernel<T, V, false><<<sgrid, block, 0, s>>>(a, steps);
         TSM_TRY(check_launch(bwd ? "recur_bwd_spans" : "recur_fwd_spans"));
     }
-#define CALL(SEG)                                                        \
-    do {                                                                 \
-        if (bwd) recur_bwd_kernel<T, V, SEG><<<grid, block, 0, s>>>(a);  \
-        else recur_fwd_kernel<T, V, SEG><<<grid, block, 0, s>>>(a);      \
+#define CALL(...)                                                                \
+    do {                                                                         \
+        if (bwd) recur_bwd_kernel<T, V, __VA_ARGS__><<<grid, block, 0, s>>>(a);  \
+        else recur_fwd_kernel<T, V, __VA_ARGS__><<<grid, block, 0, s>>>(a);      \
     } while (0)
-    if (p.seg == 1) CALL(1);
+    if (a.T == 1) CALL(1, 1);
+    else if (a.T <= 4) CALL(1, 4);
+    else if (p.seg == 1) CALL(1);
     else if (p.seg == 4) CALL(4);
     else if (p.seg == 8) CALL(8);
     else CALL(16);

@@ -351,10 +351,10 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     const int wave_u = __builtin_amdgcn_readfirstlane(wave);
     const int wm = wave_u / WN, wn = wave_u % WN;
 
-    // Jobs: the tiles of every split of K, four row tiles at a time (eight where the classes run along columns), column by column.
+    // Jobs: the tiles of every split of K, four row tiles at a time, column by column.
     // Every XCD takes a stretch of that order, so that the tiles it works on at one time share their operands in its L2 (bands
-    // of 2, 4, 8, 16, 32 row tiles: dw 4.23, 4.19, 4.42, 4.98, 5.24 ms of 8192 x 2048 x 131072, statistics 3.95, 3.89, 3.80, 3.90, 4.35).
-    constexpr int BAND = MODE == XE_OUT ? 4 : 8;
+    // of 2, 4, 8, 16, 32 row tiles: dw 4.23, 4.19, 4.42, 4.98, 5.24 ms of 8192 x 2048 x 131072, statistics, with the final loop, at 4, 8, 16 3.61, 3.66, 3.76).
+    constexpr int BAND = 4;
     const long mtiles = (a.M + BM - 1) / BM, ntiles = (a.N + BN - 1) / BN, tiles = mtiles * ntiles;
     const int njobs = gridDim.x;
     const int xcd = blockIdx.x & 7;
