@@ -67,12 +67,11 @@ __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float
 }
 
 // ---- tiles: BM x BN results of wavefronts that share the operands through LDS ---------------------------------------------
-// Operands come 64 steps of K at a time, straight from memory into an LDS stage while another is multiplied.  An operand with
-// consecutive K lies there as rows of 128 bytes whose eight 16-byte pieces are permuted by the row (piece ^ (row/2)%8),
+// Operands come 64 steps of K at a time (32 for those in three parts), straight from memory into an LDS stage while another is
+// multiplied.  An operand with consecutive K lies there as rows of 128 bytes whose eight 16-byte pieces are permuted by the row,
 // so that the 32 rows of a fragment read spread over all banks; one whose rows are K lies there as it does in memory, its
 // 32-byte granules permuted by K, and fragments are read through the transposing LDS read, four K of 16 columns at a time.
-static constexpr int XBK = 64;
-static constexpr int X_GTILE = 256;                // rows of a block of G, and columns of the tiles that write them
+static constexpr int X_GTILE = 256, X_GCOLUMNS = 64;        // rows and columns of a block of G
 static constexpr uint32_t X_OOB = 0x80000000u;     // beyond every buffer: such lanes of a load leave zeros
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t x_rsrc(const void* base) {
@@ -101,60 +100,64 @@ typedef short x_s16x8 __attribute__((ext_vector_type(8)));
 // step of either product reads stretches of 8 KB, where rows of G as such would lie 64 KB apart.
 enum { X_ROWS = 0, X_COLS = 1, X_GROWS = 2, X_GCOLS = 3 };     // [rows][K], [K][rows], G with its columns as K, with its rows as K
 
-// One operand of a tile: ROWS rows of the result's side, loaded by NT threads.
-template <int ROWS, int KIND, int NT>
+// One operand of a tile: ROWS rows of the result's side, BK steps of K at a time, loaded by NT threads.
+template <int ROWS, int KIND, int NT, int BK>
 struct XOperand {
     static constexpr bool KC = KIND == X_ROWS || KIND == X_GROWS;     // K consecutive in LDS
-    static constexpr int BYTES = ROWS * XBK * 2;
+    static constexpr int BYTES = ROWS * BK * 2;
     static constexpr int PIECES = BYTES / (NT * 16);          // per thread and step
-    static constexpr int RPP = KC ? NT / 8 : NT / (ROWS / 8); // rows of the LDS image per pass
-    static constexpr int PITCH = KC ? XBK * 2 : ROWS * 2;     // its bytes
+    static constexpr int KV = BK / 8;                         // KC: 16-byte pieces of a row
+    static constexpr int RPP = KC ? NT / KV : NT / (ROWS / 8);// rows of the LDS image per pass
+    static constexpr int PITCH = KC ? BK * 2 : ROWS * 2;      // its bytes
     uint32_t off[PIECES];         // byte offset in the step's window of this thread's pieces
     int kfirst;                   // KC: K of the piece, else K of the thread's row in a pass
     const char *base, *base0;     // of the step's window, of the first one of the first part
     long step;                    // bytes from one step to the next
-    int quarter, quarter0;        // X_GCOLS: steps into 256 rows
+    int part, part0;              // G: steps into a block (X_GROWS), into 256 rows (X_GCOLS)
+    static constexpr int PARTS = KIND == X_GROWS ? X_GCOLUMNS / BK : X_GTILE / BK;
 
+    // XOR of the piece number in a row of consecutive K: the rows of a fragment read spread over all banks
+    __device__ __forceinline__ static int kswz(int r) { return (r / (16 / KV)) & (KV - 1); }
     // XOR of the granule number: four consecutive K and the two granules of a fragment fall on different banks
     __device__ __forceinline__ static int swz(int k) {
         return ROWS == 64 ? ((k >> 1) & 1) << 1 : ((((k & 3) << 1) | (((k >> 3) & 1) << 3))) & (ROWS / 16 - 1);
     }
 
-    // row0: first row of the tile, rows: of the matrix; k0: first K.
+    // row0: first row of the tile, rows: of the matrix; k0: first K, a multiple of 64.
     __device__ __forceinline__ void init(const bf16_t* p, long ld, long row0, long rows, long k0, int tid) {
-        quarter0 = 0;
+        part0 = 0;
         if constexpr (KC) {
-            const int r = tid / 8;
-            const int kv = (tid % 8) ^ ((r >> 1) & 7);
+            const int r = tid / KV;
+            const int kv = (tid % KV) ^ kswz(r);
             kfirst = kv * 8;
-            const long pitch = KIND == X_GROWS ? XBK : ld;
+            const long pitch = KIND == X_GROWS ? X_GCOLUMNS : ld;
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
                 off[i] = row0 + i * RPP + r < rows ? (uint32_t)((i * RPP + r) * pitch * 2 + kv * 16) : X_OOB;
-            base0 = (const char*)(KIND == X_GROWS ? p + row0 / X_GTILE * ld + row0 % X_GTILE * XBK + k0 * X_GTILE : p + row0 * ld + k0);
-            step = KIND == X_GROWS ? X_GTILE * XBK * 2 : XBK * 2;
+            base0 = (const char*)(KIND == X_GROWS ? p + row0 / X_GTILE * ld + row0 % X_GTILE * X_GCOLUMNS + k0 * X_GTILE : p + row0 * ld + k0);
+            step = KIND == X_GROWS ? (X_GTILE * X_GCOLUMNS - (X_GCOLUMNS - BK)) * 2 : BK * 2;      // (into the next block)
         } else {
             const int k = tid / (ROWS / 8), slot = tid % (ROWS / 8);
             kfirst = k;
             const int col = (((slot >> 1) ^ swz(k)) << 4) + (slot & 1) * 8;
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
-                const long at = KIND == X_GCOLS ? col / XBK * (X_GTILE * XBK) + (i * RPP + k) * XBK + col % XBK : (i * RPP + k) * ld + col;
+                const long at = KIND == X_GCOLS ? col / X_GCOLUMNS * (X_GTILE * X_GCOLUMNS) + (i * RPP + k) * X_GCOLUMNS + col % X_GCOLUMNS : (i * RPP + k) * ld + col;
                 off[i] = row0 + col < rows ? (uint32_t)(at * 2) : X_OOB;
             }
             if constexpr (KIND == X_GCOLS) {
-                quarter0 = (int)(k0 % X_GTILE / XBK);
-                base0 = (const char*)(p + k0 / X_GTILE * ld + row0 * X_GTILE + k0 % X_GTILE * XBK);
-                step = (ld - (X_GTILE - XBK) * XBK) * 2;       // into the next 256 rows
+                part0 = (int)(k0 % X_GTILE / BK);
+                base0 = (const char*)(p + k0 / X_GTILE * ld + row0 * X_GTILE + k0 % X_GTILE * X_GCOLUMNS);
+                step = (ld - (X_GTILE - BK) * X_GCOLUMNS) * 2;         // into the next 256 rows
             } else {
                 base0 = (const char*)(p + k0 * ld + row0);
-                step = XBK * 2 * ld;
+                step = BK * 2 * ld;
             }
         }
         // (the same in all lanes, which the compiler has to know for a load's descriptor)
         base0 = (const char*)uniform((uint64_t)base0);
         step = (long)uniform((uint64_t)step);
-        quarter0 = __builtin_amdgcn_readfirstlane(quarter0);
+        part0 = __builtin_amdgcn_readfirstlane(part0);
         restart(0);
     }
     __device__ __forceinline__ static uint64_t uniform(uint64_t v) {
@@ -162,28 +165,29 @@ struct XOperand {
     }
     __device__ __forceinline__ void restart(long elements) {   // the first step again, of another part
         base = base0 + elements * 2;
-        quarter = quarter0;
+        part = part0;
     }
     __device__ __forceinline__ void advance() {
-        if constexpr (KIND == X_GCOLS) {
-            const bool last = quarter == X_GTILE / XBK - 1;
-            base += last ? step : (long)XBK * XBK * 2;
-            quarter = last ? 0 : quarter + 1;
+        if constexpr ((KIND == X_GROWS && PARTS > 1) || KIND == X_GCOLS) {
+            const bool last = part == PARTS - 1;
+            base += last ? step : (long)(KIND == X_GROWS ? BK : BK * X_GCOLUMNS) * 2;
+            part = last ? 0 : part + 1;
         } else {
             base += step;
         }
     }
-    // Piece i of the step at the window: left = K from its start to the end; mask: bit k clear for rows k that count as zero.
-    __device__ __forceinline__ void load(unsigned char* stage, int i, int left, uint64_t mask, int wave_u) const {
+    // Piece i of the step at the window, `more` bytes behind it: left = K from its start to the end; mask: bit k clear for rows k that
+    // count as zero.
+    __device__ __forceinline__ void load(unsigned char* stage, int i, int left, uint64_t mask, int wave_u, long more = 0) const {
         const int k = KC ? kfirst : i * RPP + kfirst;
         const bool in = k < left && (KC || (mask >> k) & 1);
-        x_load_lds16(x_rsrc(base), stage + i * (NT * 16) + wave_u * 1024, in ? off[i] : X_OOB, 0);
+        x_load_lds16(x_rsrc(base + more), stage + i * (NT * 16) + wave_u * 1024, in ? off[i] : X_OOB, 0);
     }
     // Where a lane reads the fragment of the 32 rows from row0 (a multiple of 32), K consecutive: of slice ks, else of slice 0.
     __device__ __forceinline__ static uint32_t frag_at(int row0, int ks, int lane) {
         if constexpr (KC) {
             const int r = lane & 31, hi = lane >> 5;
-            return (row0 + r) * PITCH + (((2 * ks + hi) ^ ((r >> 1) & 7)) * 16);
+            return (row0 + r) * PITCH + (((2 * ks + hi) ^ kswz(r)) * 16);
         } else {
             const int c = lane & 3, e = (lane >> 2) & 3, mblk = (lane >> 4) & 1, kg = lane >> 5;
             return (8 * kg + e) * PITCH + ((row0 / 16 + mblk) ^ swz(8 * kg + e)) * 32 + c * 8;
@@ -299,6 +303,48 @@ __device__ __forceinline__ void read_step(uint32_t a, uint32_t b, x_bf16x8 (&fa)
     }
 }
 
+// Three parts of a slice, two fragments of A and one of B each: f[part]; parts 8192 bytes apart.  KC: slices at addresses of their own.
+__device__ __forceinline__ void read_parts(uint32_t a, uint32_t b, x_bf16x8 (&fa)[3][2], x_bf16x8 (&fb)[3]) {
+    asm volatile("ds_read_b128 %0, %9\n ds_read_b128 %6, %10\n ds_read_b128 %1, %9 offset:2048\n ds_read_b128 %2, %9 offset:8192\n"
+                 "ds_read_b128 %7, %10 offset:8192\n ds_read_b128 %3, %9 offset:10240\n ds_read_b128 %4, %9 offset:16384\n"
+                 "ds_read_b128 %8, %10 offset:16384\n ds_read_b128 %5, %9 offset:18432\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(fa[0][0]), "=&v"(fa[0][1]), "=&v"(fa[1][0]), "=&v"(fa[1][1]), "=&v"(fa[2][0]), "=&v"(fa[2][1]), "=&v"(fb[0]), "=&v"(fb[1]), "=&v"(fb[2])
+                 : "v"(a), "v"(b) : "memory");
+}
+// (the transposing read: rows of 256 bytes, OFF of the slice)
+template <int OFF>
+__device__ __forceinline__ void read_parts(uint32_t a, uint32_t b, x_bf16x8 (&fa)[3][2], x_bf16x8 (&fb)[3]) {
+    x_s16x4 l[3], u[3];
+    asm volatile("ds_read_b128 %0, %12\n ds_read_b64_tr_b16 %6, %13 offset:%14\n ds_read_b64_tr_b16 %7, %13 offset:%15\n ds_read_b128 %1, %12 offset:2048\n"
+                 "ds_read_b128 %2, %12 offset:8192\n ds_read_b64_tr_b16 %8, %13 offset:%16\n ds_read_b64_tr_b16 %9, %13 offset:%17\n"
+                 "ds_read_b128 %3, %12 offset:10240\n ds_read_b128 %4, %12 offset:16384\n ds_read_b64_tr_b16 %10, %13 offset:%18\n"
+                 "ds_read_b64_tr_b16 %11, %13 offset:%19\n ds_read_b128 %5, %12 offset:18432\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(fa[0][0]), "=&v"(fa[0][1]), "=&v"(fa[1][0]), "=&v"(fa[1][1]), "=&v"(fa[2][0]), "=&v"(fa[2][1]), "=&v"(l[0]), "=&v"(u[0]),
+                   "=&v"(l[1]), "=&v"(u[1]), "=&v"(l[2]), "=&v"(u[2])
+                 : "v"(a), "v"(b), "n"(OFF), "n"(OFF + 1024), "n"(OFF + 8192), "n"(OFF + 9216), "n"(OFF + 16384), "n"(OFF + 17408) : "memory");
+#pragma unroll
+    for (int k = 0; k < 3; ++k) fb[k] = x_join(l[k], u[k]);
+}
+template <int OFF>
+__device__ __forceinline__ void read_parts(const uint32_t (&a)[2], uint32_t b, x_bf16x8 (&fa)[3][2], x_bf16x8 (&fb)[3]) {
+    x_s16x4 l[9], u[9];
+    asm volatile("ds_read_b64_tr_b16 %0, %18 offset:%21\n ds_read_b64_tr_b16 %1, %18 offset:%22\n ds_read_b64_tr_b16 %12, %20 offset:%21\n"
+                 "ds_read_b64_tr_b16 %13, %20 offset:%22\n ds_read_b64_tr_b16 %2, %19 offset:%21\n ds_read_b64_tr_b16 %3, %19 offset:%22\n"
+                 "ds_read_b64_tr_b16 %4, %18 offset:%23\n ds_read_b64_tr_b16 %5, %18 offset:%24\n ds_read_b64_tr_b16 %14, %20 offset:%23\n"
+                 "ds_read_b64_tr_b16 %15, %20 offset:%24\n ds_read_b64_tr_b16 %6, %19 offset:%23\n ds_read_b64_tr_b16 %7, %19 offset:%24\n"
+                 "ds_read_b64_tr_b16 %8, %18 offset:%25\n ds_read_b64_tr_b16 %9, %18 offset:%26\n ds_read_b64_tr_b16 %16, %20 offset:%25\n"
+                 "ds_read_b64_tr_b16 %17, %20 offset:%26\n ds_read_b64_tr_b16 %10, %19 offset:%25\n ds_read_b64_tr_b16 %11, %19 offset:%26\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(l[0]), "=&v"(u[0]), "=&v"(l[1]), "=&v"(u[1]), "=&v"(l[2]), "=&v"(u[2]), "=&v"(l[3]), "=&v"(u[3]), "=&v"(l[4]), "=&v"(u[4]),
+                   "=&v"(l[5]), "=&v"(u[5]), "=&v"(l[6]), "=&v"(u[6]), "=&v"(l[7]), "=&v"(u[7]), "=&v"(l[8]), "=&v"(u[8])
+                 : "v"(a[0]), "v"(a[1]), "v"(b), "n"(OFF), "n"(OFF + 1024), "n"(OFF + 8192), "n"(OFF + 9216), "n"(OFF + 16384), "n"(OFF + 17408) : "memory");
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        fa[k][0] = x_join(l[2 * k], u[2 * k]);
+        fa[k][1] = x_join(l[2 * k + 1], u[2 * k + 1]);
+        fb[k] = x_join(l[6 + k], u[6 + k]);
+    }
+}
+
 // Two words that the two halves of a wavefront hold of adjacent column quads, x of quads 0 | 1, y of quads 2 | 3: afterwards the lower
 // half has quads 0, 1 and the upper half quads 2, 3.
 __device__ __forceinline__ void swap_halves(uint32_t& x, uint32_t& y) {
@@ -322,12 +368,15 @@ __device__ __forceinline__ float sum32(float v) {
 
 // The shapes of a tile.  Large: eight wavefronts of 128 x 64, one block per CU, for whatever fills the chip with it.  Middle: four of
 // 64 x 64, two blocks per CU.  Small: four of 32 x 32, two blocks per CU, loads three steps ahead.  Deep: a small one by four groups of
-// wavefronts that take every fourth step of K each and add their sums up at the end, for fewer tiles than CUs.
-struct XBig { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NS = 2, KG = 1; };
-struct XMid { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, NS = 2, KG = 1; };
-struct XSmall { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 4, KG = 1; };
-struct XDeep { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 2, KG = 4; };
-template <typename C> constexpr int x_stage() { return (C::BM + C::BN) * XBK * 2; }
+// wavefronts that take every fourth step of K each and add their sums up at the end, for fewer tiles than CUs.  Parts: for operands in three
+// parts, all of which a stage holds, so that each is loaded once for the six products (the others take the pairs of parts one after
+// the other along K): eight wavefronts of 64 x 32, one block per CU.
+struct XBig { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NS = 2, KG = 1, BK = 64, PARTS = 1; };
+struct XMid { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, NS = 2, KG = 1, BK = 64, PARTS = 1; };
+struct XSmall { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 4, KG = 1, BK = 64, PARTS = 1; };
+struct XDeep { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 2, KG = 4, BK = 64, PARTS = 1; };
+struct XParts { static constexpr int BM = 128, BN = 128, WM = 2, WN = 4, NS = 2, KG = 1, BK = 32, PARTS = 3; };
+template <typename C> constexpr int x_stage() { return (C::BM + C::BN) * C::BK * 2 * C::PARTS; }
 template <typename C> constexpr int x_smem() { return C::KG * C::NS * x_stage<C>() + C::WN * C::BM * 8 + C::BN * 4; }   // stages, row statistics, biases
 static constexpr int X_LAUNCH = 1 << 22;   // blocks of one launch, at most
 
@@ -336,12 +385,14 @@ template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
 __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(XentArgs a) {
     constexpr int BM = C::BM, BN = C::BN, WM = C::WM, WN = C::WN, NT = WM * WN * 64, MI = BM / (WM * 32), NJ = BN / (WN * 32);
     constexpr bool BIG = NJ == 2;
-    static_assert((BIG && (MI == 4 || MI == 2)) || (MI == 1 && NJ == 1 && BN == 64), "read_frags, read_step");
+    static_assert((BIG && (MI == 4 || MI == 2)) || (MI == 1 && NJ == 1 && BN == 64) || (C::PARTS == 3 && MI == 2 && NJ == 1 && SPLIT), "read_frags, read_step, read_parts");
     constexpr int TM = BM / WM, TN = BN / WN, NS = C::NS, KG = C::KG, STAGE = x_stage<C>();
     static_assert(KG == 1 || (AKIND == X_ROWS && BKIND == X_ROWS), "groups skip steps");
-    typedef XOperand<BM, AKIND, NT> OpA;
-    typedef XOperand<BN, BKIND, NT> OpB;
-    constexpr int NP = OpA::PIECES + OpB::PIECES;
+    constexpr int BK = C::BK, PARTS = C::PARTS;
+    constexpr bool PAIRS = SPLIT && PARTS == 1;                 // the parts one pair after the other
+    typedef XOperand<BM, AKIND, NT, BK> OpA;
+    typedef XOperand<BN, BKIND, NT, BK> OpB;
+    constexpr int NP = (OpA::PIECES + OpB::PIECES) * PARTS;
     constexpr float L2E = 1.44269502f;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     float2* s_part = (float2*)(smem + KG * NS * STAGE);         // [WN][BM]; the column sums of G as floats [WM][BN]
@@ -364,34 +415,40 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     const long mt = band * BAND + rest % high, nt = rest / high;
     const long m0 = mt * BM, n0 = nt * BN;
     const long kb = z * a.ksplit, ke = kb + a.ksplit < a.K ? kb + a.ksplit : a.K;
-    const int ksteps = ke > kb ? (int)((ke - kb + XBK - 1) / XBK) : 0, steps = ksteps * (SPLIT ? 6 : 1);
+    const int ksteps = ke > kb ? (int)((ke - kb + BK - 1) / BK) : 0, steps = ksteps * (PAIRS ? 6 : 1);
     OpA pa;
     OpB pb;
     int kc = 0, pair = 0;                                       // of the step at the operands' windows
     auto load_step = [&](int stage) {
         unsigned char* st = smem + (group * NS + stage) * STAGE;
-        const long l = ke - kb - (long)kc * XBK;
-        const int left = l < XBK ? (int)l : XBK;
+        const long l = ke - kb - (long)kc * BK;
+        const int left = l < BK ? (int)l : BK;
         uint64_t mask = ~0ull;
-        if constexpr (AKIND == X_GCOLS) mask = ((const __attribute__((address_space(4))) uint64_t*)a.kmask)[kb / XBK + kc];
+        if constexpr (AKIND == X_GCOLS) {
+            const long k = kb + (long)kc * BK;
+            mask = ((const __attribute__((address_space(4))) uint64_t*)a.kmask)[k / 64] >> (BK < 64 ? k % 64 : 0);
+        }
 #pragma unroll
-        for (int q = 0; q < OpA::PIECES; ++q) pa.load(st, q, left, ~0ull, wave_u);
+        for (int part = 0; part < PARTS; ++part) {
 #pragma unroll
-        for (int q = 0; q < OpB::PIECES; ++q) pb.load(st + OpA::BYTES, q, left, mask, wave_u);
+            for (int q = 0; q < OpA::PIECES; ++q) pa.load(st + part * OpA::BYTES, q, left, ~0ull, wave_u, part * a.aplane * 2);
+#pragma unroll
+            for (int q = 0; q < OpB::PIECES; ++q) pb.load(st + PARTS * OpA::BYTES + part * OpB::BYTES, q, left, mask, wave_u, part * a.bplane * 2);
+        }
     };
     auto next_step = [&](int stage) {
         if constexpr (KG > 1) {                                 // this group's next step: KG further on
-            for (kc += KG; SPLIT && kc >= ksteps;) {
+            for (kc += KG; PAIRS && kc >= ksteps;) {
                 kc -= ksteps;
                 ++pair;
             }
-            pa.restart(a.aplane * ((0x001102 >> (4 * pair)) & 3) * SPLIT + (long)kc * XBK);
-            pb.restart(a.bplane * ((0x010120 >> (4 * pair)) & 3) * SPLIT + (long)kc * XBK);
+            pa.restart((PAIRS ? a.aplane * ((0x001102 >> (4 * pair)) & 3) : 0) + (long)kc * BK);
+            pb.restart((PAIRS ? a.bplane * ((0x010120 >> (4 * pair)) & 3) : 0) + (long)kc * BK);
             load_step(stage);
             return;
         }
         ++kc;
-        if (SPLIT && kc == ksteps) {                            // the next pair of parts: 2 0, 0 2, 1 1, 1 0, 0 1, 0 0
+        if (PAIRS && kc == ksteps) {                            // the next pair of parts: 2 0, 0 2, 1 1, 1 0, 0 1, 0 0
             kc = 0;
             ++pair;
             pa.restart(a.aplane * ((0x001102 >> (4 * pair)) & 3));
@@ -407,8 +464,8 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     uint32_t aat[4], bat[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        if (OpA::KC || q < MI) aat[q] = lds0 + (OpA::KC ? OpA::frag_at(wm * TM, q, lane) : OpA::frag_at(wm * TM + q * 32, 0, lane));
-        if (OpB::KC || q < NJ) bat[q] = lds0 + OpA::BYTES + (OpB::KC ? OpB::frag_at(wn * TN, q, lane) : OpB::frag_at(wn * TN + q * 32, 0, lane));
+        if (OpA::KC ? q < BK / 16 : q < MI) aat[q] = lds0 + (OpA::KC ? OpA::frag_at(wm * TM, q, lane) : OpA::frag_at(wm * TM + q * 32, 0, lane));
+        if (OpB::KC ? q < BK / 16 : q < NJ) bat[q] = lds0 + PARTS * OpA::BYTES + (OpB::KC ? OpB::frag_at(wn * TN, q, lane) : OpB::frag_at(wn * TN + q * 32, 0, lane));
     }
     x_f32x16 acc[MI][NJ];
 #pragma unroll
@@ -420,7 +477,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     if (steps > 0) {
         pa.init(a.A, a.lda, m0, a.M, kb, tid);
         pb.init(a.B, a.ldb, n0, a.N, kb, tid);
-        if constexpr (SPLIT) pa.restart(a.aplane * 2);
+        if constexpr (PAIRS) pa.restart(a.aplane * 2);
         if constexpr (KG == 1) load_step(0);
     }
     if constexpr (BIG) {
@@ -517,6 +574,37 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
                 const float4 o = sums[(g * 4 + r) * NT + tid];
                 acc[0][0][4 * r] += o.x; acc[0][0][4 * r + 1] += o.y; acc[0][0][4 * r + 2] += o.z; acc[0][0][4 * r + 3] += o.w;
             }
+    } else if constexpr (PARTS > 1) {
+        static_assert(NS == 2, "two stages");
+        for (int s = 0; s < steps; ++s) {                       // (three stages instead of two: the same time)
+            const int stage = s & 1;
+            x_wait<0>();
+            x_barrier();
+            if (s + 1 < steps) next_step(stage ^ 1);
+            __builtin_amdgcn_sched_barrier(0);
+            const uint32_t so = stage * STAGE;
+            auto slice = [&](auto number) {
+                constexpr int ks = decltype(number)::value, OFF = ks * 16 * OpB::PITCH;
+                x_bf16x8 fa[3][2], fb[3];
+                if constexpr (OpA::KC && OpB::KC) {
+                    read_parts(aat[ks] + so, bat[ks] + so, fa, fb);
+                } else if constexpr (OpA::KC) {
+                    read_parts<OFF>(aat[ks] + so, bat[0] + so, fa, fb);
+                } else {
+                    const uint32_t q[2] = {aat[0] + so, aat[1] + so};
+                    read_parts<OFF>(q, bat[0] + so, fa, fb);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};      // the small products first
+#pragma unroll
+                for (int k = 0; k < 6; ++k)
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) acc[i][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[PB[k]], fa[PA[k]][i], acc[i][0], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            slice(std::integral_constant<int, 0>{});
+            slice(std::integral_constant<int, 1>{});
+        }
     } else {
         // One barrier per step: in front of it every wavefront waits for its loads of this step, behind it the stage of the step
         // before is free.
@@ -630,8 +718,8 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
         }
     } else if constexpr (MODE == XE_GRAD) {
         // this lane's first row in the block of G that has the wavefront's columns
-        bf16_t* G = a.e.G + m0 / X_GTILE * a.e.ldg + nw / XBK * (X_GTILE * XBK) + (m0 % X_GTILE + wrow) * XBK + nw % XBK;
-        static_assert(TN == XBK || TN == 32, "a wavefront's columns are of one block of G");
+        bf16_t* G = a.e.G + m0 / X_GTILE * a.e.ldg + nw / X_GCOLUMNS * (X_GTILE * X_GCOLUMNS) + (m0 % X_GTILE + wrow) * X_GCOLUMNS + nw % X_GCOLUMNS;
+        static_assert(TN == X_GCOLUMNS || TN == 32, "a wavefront's columns are of one block of G");
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             __builtin_amdgcn_sched_barrier(0);                   // one row at a time, within the registers
@@ -664,7 +752,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
                     if (lo == 31) s_sum[wm * BN + wn * TN + ncol(j, r / 4) + r % 4] = t;
                 }
         }
-        constexpr int PARTS = SPLIT ? 3 : 1;
+        constexpr int GPARTS = SPLIT ? 3 : 1;
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -675,19 +763,19 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
 #pragma unroll
                     for (int t = 0; t < 8; ++t) f[t] = acc[i][j][4 * q + t];
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part) {
+                    for (int part = 0; part < GPARTS; ++part) {
                         uint32_t w[4];
 #pragma unroll
                         for (int t = 0; t < 4; ++t) {
                             w[t] = pack_bf16x2(f[2 * t], f[2 * t + 1]);
-                            if (part + 1 < PARTS) {
+                            if (part + 1 < GPARTS) {
                                 f[2 * t] -= __uint_as_float(w[t] << 16);
                                 f[2 * t + 1] -= __uint_as_float(w[t] & 0xffff0000u);
                             }
                         }
                         swap_halves(w[0], w[2]);
                         swap_halves(w[1], w[3]);
-                        *(any_u32x4*)(G + part * a.e.gplane + i * 32 * XBK + j * 32 + 8 * (q + hi)) = any_u32x4{w[0], w[1], w[2], w[3]};
+                        *(any_u32x4*)(G + part * a.e.gplane + i * 32 * X_GCOLUMNS + j * 32 + 8 * (q + hi)) = any_u32x4{w[0], w[1], w[2], w[3]};
                     }
                 }
         if constexpr (DB) {
@@ -879,11 +967,11 @@ static constexpr size_t XENT_G_BYTES = (size_t)512 << 20;   // of a piece of G, 
 static long x_tiles(long M, long N, int t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }
 
 static int x_tile(int size) { return size == X_BIG ? 256 : size == X_MID ? 128 : 64; }
-static int x_room(int size) { return size == X_BIG ? 256 : 512; }      // blocks that run at one time
+static int x_room(int size, bool parts) { return size == X_BIG || (size == X_MID && parts) ? 256 : 512; }      // blocks that run at one time
 
 // Splits of K that fill the chip, each of 512 at least.
-static int x_splits(int size, long M, long N, long K) {
-    const long tiles = x_tiles(M, N, x_tile(size)), fill = x_room(size);
+static int x_splits(int size, long M, long N, long K, bool parts) {
+    const long tiles = x_tiles(M, N, x_tile(size)), fill = x_room(size, parts);
     long z = tiles < fill ? fill / tiles : 1;
     const long most = K / 512 > 1 ? K / 512 : 1;
     if (z > most) z = most;
@@ -891,12 +979,12 @@ static int x_splits(int size, long M, long N, long K) {
 }
 
 // The largest tiles that fill half the chip, K split (split) or not, and are not more than half empty where the matrix is narrow.
-// us of the products with small, middle, large tiles: statistics of 1777 x 1000 x 32003 244, 150, 144, of 512 x 1024 x 10007 in fp32 111,
-// 83, 131, of 4 x 2048 x 65536 (w read from HBM) 61, 69, 75, of 64 x 2048 x 400 17, 28, 50; dx of them 231, 131 + 11, 110 + 18 and 103, 72, 88.
-static int x_size(long M, long N, long K, bool split) {
+// us of the products with small, middle, large tiles: statistics of 1777 x 1000 x 32003 244, 150, 144, of 2048 x 1024 x 10000 in fp32 with
+// large tiles that take the pairs of parts one after the other and middle ones that take them together 288, 222, of 4 x 2048 x 65536 (w read from HBM) 61, 69, 75, of 64 x 2048 x 400 17, 28, 50; dx of the first 231, 131 + 11, 110 + 18.
+static int x_size(long M, long N, long K, bool split, bool parts) {
     const long narrow = M < N ? M : N;
-    for (int size = narrow > 128 ? X_BIG : narrow > 64 ? X_MID : X_SMALL; size > X_SMALL; --size)
-        if (x_tiles(M, N, x_tile(size)) * (split ? x_splits(size, M, N, K) : 1) >= x_room(size) / 2) return size;
+    for (int size = narrow > 128 && !parts ? X_BIG : narrow > 64 ? X_MID : X_SMALL; size > X_SMALL; --size)
+        if (x_tiles(M, N, x_tile(size)) * (split ? x_splits(size, M, N, K, parts) : 1) >= x_room(size, parts) / 2) return size;
     return X_SMALL;
 }
 
@@ -911,7 +999,8 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     if (piece > V) piece = V;
     p.piece = piece;
     p.pieces = (V + piece - 1) / piece;
-    p.size = x_size(R, piece, D, false);
+    const bool f32 = parts == 3;
+    p.size = x_size(R, piece, D, false, f32);
     const long t = x_tile(p.size);
     p.ntiles = (p.pieces - 1) * ((piece + t - 1) / t) + (V - (p.pieces - 1) * piece + t - 1) / t;
     p.mtiles = (R + t - 1) / t;
@@ -927,10 +1016,10 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     p.o_part = f.used; f.take((size_t)p.ntiles * R * 8);
     p.o_picked = f.used; f.take((size_t)R * 4);
     p.fwd_bytes = f.used;
-    p.sizedx = x_size(R, D, V, p.pieces == 1);
-    p.zdx = p.pieces > 1 ? 1 : x_splits(p.sizedx, R, D, V);
-    p.sizedw = x_size(piece, D, R, true);
-    p.zdw = x_splits(p.sizedw, piece, D, R);
+    p.sizedx = x_size(R, D, V, p.pieces == 1, f32);
+    p.zdx = p.pieces > 1 ? 1 : x_splits(p.sizedx, R, D, V, f32);
+    p.sizedw = x_size(piece, D, R, true, f32);
+    p.zdw = x_splits(p.sizedw, piece, D, R, f32);
     p.o_G = b.used; b.take((size_t)parts * p.gplane * 2);
     p.o_acc = b.used; b.take((parts == 1 && p.pieces > 1) || p.zdx > 1 ? (size_t)p.zdx * R * D * 4 : 0);
     p.o_dw = b.used; b.take(p.zdw > 1 ? (size_t)p.zdw * piece * D * 4 : 0);
@@ -961,7 +1050,7 @@ static int x_launch(XentArgs a, int splits, const char* what, hipStream_t s) {
         configured = true;
     }
     const long jobs = x_tiles(a.M, a.N, C::BM) * splits;
-    a.ksplit = ((a.K + splits - 1) / splits + XBK - 1) / XBK * XBK;
+    a.ksplit = ((a.K + splits - 1) / splits + 63) / 64 * 64;
     for (a.job0 = 0; a.job0 < jobs; a.job0 += X_LAUNCH) {
         const long n = jobs - a.job0;
         kernel<<<dim3((unsigned)(n < X_LAUNCH ? n : X_LAUNCH)), dim3(C::WM * C::WN * C::KG * 64), x_smem<C>(), s>>>(a);
@@ -972,8 +1061,12 @@ static int x_launch(XentArgs a, int splits, const char* what, hipStream_t s) {
 
 template <int MODE, int AKIND, int BKIND, bool SPLIT, bool DB = false>
 static int x_product(int size, const XentArgs& a, int splits, const char* what, hipStream_t s) {
-    if (size == X_BIG) return x_launch<XBig, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
-    if (size == X_MID) return x_launch<XMid, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+    if constexpr (SPLIT) {
+        if (size == X_MID) return x_launch<XParts, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+    } else {
+        if (size == X_BIG) return x_launch<XBig, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+        if (size == X_MID) return x_launch<XMid, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+    }
     if constexpr (MODE != XE_OUT)      // (us at 64 x 2048 x 400: 14.2 with small tiles, 10.3 with deep ones)
         if (x_tiles(a.M, a.N, 64) <= 256 && a.K * (SPLIT ? 6 : 1) >= 512) return x_launch<XDeep, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     return x_launch<XSmall, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
