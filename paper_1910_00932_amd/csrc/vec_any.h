@@ -10,6 +10,8 @@ typedef uint32_t any_u32x4 __attribute__((ext_vector_type(4)));
 typedef any_u32x2 any_u32x2_at2 __attribute__((aligned(2)));
 typedef any_u32x4 any_u32x4_at2 __attribute__((aligned(2)));
 typedef any_u32x4 any_u32x4_at4 __attribute__((aligned(4)));
+typedef float any_f32x4 __attribute__((ext_vector_type(4)));
+typedef any_f32x4 any_f32x4_at4 __attribute__((aligned(4)));
 
 // N elements of T as they lie in memory.
 template <typename T, int N> struct RawVec;

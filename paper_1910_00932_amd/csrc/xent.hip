@@ -11,6 +11,7 @@
 // all sums are fp32.  fp32: x, w and G are cut into three bf16 parts each, exactly (8 + 8 + 8 bits), and a product is the sum of the
 // six largest part products (the method of Henry, Tang and Heinecke, "Leveraging the bfloat16 artificial intelligence datatype for
 // higher-precision computations", 2019; what is left out is at most 2^-24 of it), one after the other along K, the small parts first.
+#include <algorithm>
 #include <type_traits>
 #include "internal.h"
 #include "args.h"
@@ -790,70 +791,53 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
             }
         }
     } else {
-        // Whole vectors of 16 bytes: 32 rows of the wavefront at a time through LDS (behind the last barrier the stages are free, the small
-        // tiles' but for their last step), so that rows are stored in stretches of its columns, results past the caches
-        // (dw of 4 x 2048 x 65536, which is little but its store, 110 -> 65 us).
-        if (a.N % (a.e.out_f32 ? 4 : 8) == 0) {
-            if constexpr (!BIG) x_barrier();
-            constexpr int Q = TN / 4;                            // quads of a row, permuted by the row
-            float4* mine = (float4*)smem + wave_u * (32 * Q);
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        mine[lo * Q + ((j * 8 + 2 * q + hi) ^ (lo & (Q - 1)))] = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-                if (a.e.out_f32) {
-#pragma unroll
-                    for (int t = 0; t < 32 * Q / 64; ++t) {
-                        const int r = (t * 64 + lane) / Q, c = (t * 64 + lane) % Q;
-                        const long m = m0 + wm * TM + i * 32 + r, n = nw + c * 4;
-                        if (m >= a.M || n >= a.N) continue;
-                        const float4 v = mine[r * Q + (c ^ (r & (Q - 1)))];
-                        float f[4] = {v.x, v.y, v.z, v.w};
-                        if (a.e.acc) {
-                            const float4 o = *(const float4*)(a.e.acc + m * a.N + n);
-                            f[0] += o.x; f[1] += o.y; f[2] += o.z; f[3] += o.w;
-                        }
-                        float* to = a.e.out_f32 + (z * a.M + m) * a.N + n;
-                        if (a.ksplit < a.K) *(float4*)to = make_float4(f[0], f[1], f[2], f[3]);      // (read again soon)
-                        else raw_store<float, 4>(to, f, 4);
-                    }
-                } else {
-#pragma unroll
-                    for (int t = 0; t < 16 * Q / 64; ++t) {
-                        const int r = (t * 64 + lane) / (Q / 2), c = (t * 64 + lane) % (Q / 2);
-                        const long m = m0 + wm * TM + i * 32 + r, n = nw + c * 8;
-                        if (m >= a.M || n >= a.N) continue;
-                        const float4 v = mine[r * Q + ((2 * c) ^ (r & (Q - 1)))], w = mine[r * Q + ((2 * c + 1) ^ (r & (Q - 1)))];
-                        float f[8] = {v.x, v.y, v.z, v.w, w.x, w.y, w.z, w.w};
-                        if (a.e.acc) {
-                            const float4 o = *(const float4*)(a.e.acc + m * a.N + n), u = *(const float4*)(a.e.acc + m * a.N + n + 4);
-                            f[0] += o.x; f[1] += o.y; f[2] += o.z; f[3] += o.w;
-                            f[4] += u.x; f[5] += u.y; f[6] += u.z; f[7] += u.w;
-                        }
-                        raw_store<bf16_t, 8>(a.e.out + m * a.N + n, f, 8);
-                    }
-                }
-            }
-            return;
-        }
+        // 32 rows of the wavefront at a time through LDS (behind the last barrier the stages are free, the small tiles' but for their last
+        // step), so that rows are stored in stretches of its columns, results past the caches (dw of 4 x 2048 x 65536, which is little
+        // but its store, 110 -> 65 us).
+        if constexpr (!BIG) x_barrier();
+        constexpr int Q = TN / 4;                                // quads of a row, permuted by the row
+        float4* mine = (float4*)smem + wave_u * (32 * Q);
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-            const long m = mrow(i);
-            if (m >= a.M) continue;
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const long n = nw + ncol(j, r / 4) + r % 4;
-                    if (n >= a.N) continue;
-                    float v = acc[i][j][r];
-                    if (a.e.acc) v += a.e.acc[m * a.N + n];
-                    if (a.e.out_f32) a.e.out_f32[(z * a.M + m) * a.N + n] = v;
-                    else a.e.out[m * a.N + n] = f32_to_bf16(v);
+                for (int q = 0; q < 4; ++q)
+                    mine[lo * Q + ((j * 8 + 2 * q + hi) ^ (lo & (Q - 1)))] = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+            // the quad c of row r with what is added to it; `there` columns of it and more
+            auto quad = [&](int r, int c, long at, int there, float* f) {
+                const float4 v = mine[r * Q + (c ^ (r & (Q - 1)))];
+                f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+                if (a.e.acc) {
+                    const any_u32x4 o = raw_load<float, 4>(a.e.acc + at, there);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) f[t] += raw_get<float>(o, t);
                 }
+            };
+            if (a.e.out_f32) {
+#pragma unroll
+                for (int t = 0; t < 32 * Q / 64; ++t) {
+                    const int r = (t * 64 + lane) / Q, c = (t * 64 + lane) % Q, there = cols - c * 4;
+                    const long m = m0 + wm * TM + i * 32 + r, at = m * a.N + nw + c * 4;
+                    if (m >= a.M || there <= 0) continue;
+                    float f[4];
+                    quad(r, c, at, there, f);
+                    float* to = a.e.out_f32 + z * a.M * a.N + at;
+                    if (a.ksplit < a.K && there >= 4) *(any_f32x4_at4*)to = any_f32x4{f[0], f[1], f[2], f[3]};      // (read again soon)
+                    else raw_store<float, 4>(to, f, there);
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < 16 * Q / 64; ++t) {
+                    const int r = (t * 64 + lane) / (Q / 2), c = (t * 64 + lane) % (Q / 2), there = cols - c * 8;
+                    const long m = m0 + wm * TM + i * 32 + r, at = m * a.N + nw + c * 8;
+                    if (m >= a.M || there <= 0) continue;
+                    float f[8];
+                    quad(r, 2 * c, at, there, f);
+                    quad(r, 2 * c + 1, at + 4, there - 4, f + 4);
+                    raw_store<bf16_t, 8>(a.e.out + at, f, there);
+                }
+            }
         }
     }
 }
@@ -934,6 +918,7 @@ __global__ void __launch_bounds__(256) xent_colsum_kernel(const float* __restric
     const long c = (long)blockIdx.x * 256 + threadIdx.x;
     if (c >= n) return;
     float s = 0.f;
+#pragma unroll 8
     for (long r = 0; r < rows; ++r) s += part[r * ld + c];
     out[c] = s;
 }
@@ -943,6 +928,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) xent_join_kernel(const float* __restrict__ part, int splits, long n, T* __restrict__ out) {
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
         float s = 0.f;
+#pragma unroll 8
         for (int z = 0; z < splits; ++z) s += part[z * n + i];
         out[i] = Elem<T>::st(s);
     }
@@ -969,18 +955,19 @@ static long x_tiles(long M, long N, int t) { return ((M + t - 1) / t) * ((N + t 
 static int x_tile(int size) { return size == X_BIG ? 256 : size == X_MID ? 128 : 64; }
 static int x_room(int size, bool parts) { return size == X_BIG || (size == X_MID && parts) ? 256 : 512; }      // blocks that run at one time
 
-// Splits of K that fill the chip, each of 512 at least.
+// Splits of K that fill the chip, each of 512 products per result at least (fp32: of parts).
 static int x_splits(int size, long M, long N, long K, bool parts) {
     const long tiles = x_tiles(M, N, x_tile(size)), fill = x_room(size, parts);
     long z = tiles < fill ? fill / tiles : 1;
-    const long most = K / 512 > 1 ? K / 512 : 1;
+    const long most = std::max(1L, K * (parts ? 6 : 1) / 512);
     if (z > most) z = most;
     return (int)(z > 64 ? 64 : z);
 }
 
 // The largest tiles that fill half the chip, K split (split) or not, and are not more than half empty where the matrix is narrow.
-// us of the products with small, middle, large tiles: statistics of 1777 x 1000 x 32003 244, 150, 144, of 2048 x 1024 x 10000 in fp32 with
-// large tiles that take the pairs of parts one after the other and middle ones that take them together 288, 222, of 4 x 2048 x 65536 (w read from HBM) 61, 69, 75, of 64 x 2048 x 400 17, 28, 50; dx of the first 231, 131 + 11, 110 + 18.
+// us of the products with small, middle, large tiles: statistics of 1777 x 1000 x 32003 244, 150, 144, of 4 x 2048 x 65536 (w read from HBM)
+// 61, 69, 75, of 64 x 2048 x 400 17, 28, 50; dx of the first 231, 131 + 11, 110 + 18.  fp32, 2048 x 1024 x 10000: large tiles that took
+// the pairs of parts one after the other 288, middle ones that take them together 222.
 static int x_size(long M, long N, long K, bool split, bool parts) {
     const long narrow = M < N ? M : N;
     for (int size = narrow > 128 && !parts ? X_BIG : narrow > 64 ? X_MID : X_SMALL; size > X_SMALL; --size)
