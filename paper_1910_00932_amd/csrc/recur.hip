@@ -7,11 +7,13 @@
 // Both passes are bound by memory: forward reads x, g and writes y, backward reads x, g, dy and writes dx, dg.  The steps of a
 // column are maps h -> A h + B, which join associatively: a block takes a tile of SEG segments of 8 steps times LC*4 columns, one
 // thread per segment and four columns, holds the tile in registers, joins the segments' maps through LDS and runs every segment
-// again from its true start.  Tiles follow one another in time with the state carried along, so each tensor is read once (twice
-// where few columns make several blocks share the time axis).  The
+// again from its true start, so each tensor is read once.  Tiles follow one another in time with the state carried along; where few
+// columns would leave CUs idle, a column's tiles run side by side and hand their maps on through memory (JOIN).  The
 // state, the maps and what is carried are fp32 throughout; only y, dx and dg are rounded to the storage type.
 // The backward pass needs h inside a tile: it starts from the states that the forward pass left every 128 steps (1.6 % of a bf16
 // tensor), and forms h again from x and g, which it reads anyway, instead of reading y, which is rounded.
+// Measured, bf16: 64 clips of 8 frames of 7 x 7 x 2048: forward 53.5 us (5.8 TB/s), backward 82 us (6.3 TB/s); 4 clips of 4096 frames
+// of 2048 values: 43 and 68 us (4.7 and 4.9 TB/s; a copy of that size reaches 6.7).
 #include <algorithm>
 #include <type_traits>
 #include "internal.h"
@@ -22,6 +24,7 @@ namespace tsm {
 
 static constexpr int RC_NT = 256, RC_V = 4, RC_STEPS = 8;   // threads, columns per thread (one where there are fewer), steps per thread (fewer for the shortest clips)
 static constexpr int RC_SAVE = 128;                       // steps between saved states
+static constexpr int RC_GROUP = 64, RC_TICKET = 16;       // JOIN: tiles from one whole state to the next; words (64 bytes) of a ticket counter
 
 struct RecurArgs {
     const void *x, *g, *dy;
@@ -29,19 +32,42 @@ struct RecurArgs {
     const float *h0, *dh_last;
     float *h_last, *dh0;
     float* saved;         // [N][(T-1)/RC_SAVE][M]: the state in front of step RC_SAVE*(j+1)
-    float* maps;          // spans > 1: [N][spans][2][M], the spans' maps; behind them [N][M], the state in front of the first
-    long M, cblocks, jobs;
-    int N, T, spans, tiles_per_span;
+    uint64_t* slots;      // JOIN: [N][tiles + groups][M], see recur_join; in front of them
+    uint32_t* tickets;    // [N][cblocks], one in RC_TICKET words: how many tiles have been taken
+    long M, cblocks, jobs, ws_bytes;
+    int N, T, tiles, groups;
+    bool runs;            // the jobs in runs per XCD
 };
 
-// sigmoid(g) and 1 - sigmoid(g), neither by subtraction: e = exp(-|g|), 1/(1+e) and e/(1+e).  (The product with log2 e is rounded, which
-// makes e off by |g| units of its last place: half a unit of the sum 1 + e at most.)
-__device__ __forceinline__ void gate(float g, float& a, float& k) {
-    const float e = __builtin_amdgcn_exp2f(-fabsf(g) * 1.44269502f);
-    const float big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
-    a = g < 0.f ? small : big;
-    k = g < 0.f ? big : small;
-}
+// a = sigmoid(g) and k = 1 - a, neither by subtraction: e = exp(-|g|), 1/(1+e) and e/(1+e).  (The product with log2 e is rounded, which
+// makes e off by |g| units of its last place: half a unit of the sum 1 + e at most.)  PACKED: in one register, the smaller under the sign
+// of g; the larger is 1 less that, off by half a unit of its last place.
+template <bool PACKED> struct Gate {
+    float av, kv;
+    __device__ __forceinline__ static Gate of(float g) {
+        const float e = __builtin_amdgcn_exp2f(-fabsf(g) * 1.44269502f), big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
+        return g < 0.f ? Gate{small, big} : Gate{big, small};
+    }
+    __device__ __forceinline__ float a() const { return av; }
+    __device__ __forceinline__ float k() const { return kv; }
+    __device__ __forceinline__ void open() {                            // a step that changes nothing
+        av = 1.f;
+        kv = 0.f;
+    }
+    __device__ __forceinline__ void renew() {}
+};
+template <> struct Gate<true> {
+    float s;
+    __device__ __forceinline__ static Gate of(float g) {
+        const float e = __builtin_amdgcn_exp2f(-fabsf(g) * 1.44269502f);
+        return Gate{copysignf(e * __builtin_amdgcn_rcpf(1.f + e), g)};
+    }
+    __device__ __forceinline__ bool closed() const { return (int)__float_as_uint(s) < 0; }
+    __device__ __forceinline__ float a() const { return closed() ? -s : 1.f - s; }
+    __device__ __forceinline__ float k() const { return closed() ? 1.f + s : s; }
+    __device__ __forceinline__ void open() { s = 0.f; }
+    __device__ __forceinline__ void renew() { asm volatile("" : "+v"(s)); }     // to the compiler, another value: taken apart again, not held apart
+};
 
 // The columns of a thread: V from `col`, of which the first `skip` belong to the thread before.  Columns that would lie behind the last are
 // moved back onto it, so that loads need no condition (one under a condition is awaited where the branches join); only what a
@@ -63,6 +89,15 @@ struct RecurCols {
         if constexpr (V == 1) return Elem<T>::ld(r);
         else return raw_get<T>(r, e);
     }
+    __device__ __forceinline__ static void renew(Raw& r) {     // to the compiler, another value
+        if constexpr (V > 1)
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof(Raw) / 4); ++i) {
+                uint32_t w = r[i];
+                asm volatile("" : "+v"(w));
+                r[i] = w;
+            }
+    }
     __device__ __forceinline__ void store(T* p, const float (&f)[V]) const {
         if constexpr (V > 1) {
             if (skip == 0) {
@@ -83,6 +118,39 @@ struct RecurCols {
         for (int e = 0; e < V; ++e)
             if (e >= skip) p[col + e] = f[e];
     }
+};
+
+// Every XCD takes a run of the jobs, so that blocks beside one another share the lines of memory that lie across their border in its L2
+// (3 x 301 x 4995 fp32: forward 16.6 -> 13.9 us, backward 30.8 -> 25.3; rows of whole lines are better off without, 64 x 8 frames 142 -> 146).
+__device__ __forceinline__ long xcd_run(long job, long jobs) {
+    const long xcd = job & 7;
+    return xcd * (jobs / 8) + (xcd < jobs % 8 ? xcd : jobs % 8) + (job >> 3);
+}
+
+// A job's block of columns and what is left of its number; the division in 32 bits where they suffice.
+struct RecurJob {
+    long cb, n;
+    __device__ __forceinline__ RecurJob(const RecurArgs& a, long job) {
+        if (a.jobs >> 32 == 0) {
+            n = (uint32_t)job / (uint32_t)a.cblocks;
+            cb = (uint32_t)job - (uint32_t)n * (uint32_t)a.cblocks;
+        } else {
+            n = job / a.cblocks;
+            cb = job - n * a.cblocks;
+        }
+    }
+};
+
+// Where the values of a step lie, from the clip's first one; NEAR: from the tile's, in 32 bits, which cost a register less per address.
+// (Tiles lie side by side for few columns only: 128 steps of them are far below 2^32 bytes.)
+template <bool NEAR> struct RecurRows {
+    typedef typename std::conditional<NEAR, uint32_t, long>::type At;
+    long origin;
+    int t0;
+    At M, col;
+    __device__ __forceinline__ RecurRows(const RecurArgs& a, long n, int first, long c) : origin((n * a.T + first) * a.M), t0(first), M((At)a.M), col((At)c) {}
+    __device__ __forceinline__ At at(int t) const { return (At)(t - t0) * M + col; }
+    template <typename T> __device__ __forceinline__ T* of(const void* p, At at) const { return (T*)((char*)((T*)p + origin) + at * (At)sizeof(T)); }
 };
 
 // The maps of the tile's segments, one parity per tile so that one barrier per tile is enough.
@@ -129,92 +197,198 @@ struct RecurLds {
     }
 };
 
-template <typename T, int V, int SEG, int RC_K = RC_STEPS>
-__global__ void __launch_bounds__(RC_NT) recur_fwd_kernel(RecurArgs a) {
+// ---- JOIN: too few columns to fill the chip; a block takes one tile, and the tiles of a column run side by side ------------
+// A tile's map goes into a slot, one 64-bit word (A below, B above) per column, which says by itself that it is there: all slots are
+// filled with ones first, a NaN that no published A is.  A block then waits for the maps in front of it, joins them in an order that does
+// not depend on which came first, and runs its tile, which has stayed in registers.  The last tile of every RC_GROUP also leaves the
+// state behind it, where those of the next group begin.  A block of columns hands out its tiles by ticket, in their order: whoever
+// a tile waits for was taken before it, by a block that is on a CU and that waits for still earlier tiles only, so every wait ends.  (It is
+// bounded all the same, for callers that share a workspace between streams: what is missing then enters as the NaN of an empty
+// slot.)  One ticket counter for all columns costs 15 ns a tile in turn: 4 x 4096 frames of 2048 values forward 77 us, with a counter
+// per block of columns 43; a launch of its own for the maps, which reads x and g twice, 61.
+static constexpr int RC_TRIES = 1 << 22;
+
+__global__ void __launch_bounds__(256) recur_clear_kernel(any_u32x4* p, long n) {
+    for (long i = blockIdx.x * 256L + threadIdx.x; i < n; i += gridDim.x * 256L) p[i] = any_u32x4{~0u, ~0u, ~0u, ~0u};
+}
+
+// The next tile, in their order, of column block `at`.
+__device__ __forceinline__ int recur_ticket(const RecurArgs& a, long at, int* shared) {
+    __syncthreads();                                                    // (LDS of the block's last tile is free)
+    if (threadIdx.x == 0) *shared = (int)(__hip_atomic_fetch_add(a.tickets + at * RC_TICKET, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1);   // (from all ones)
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(*shared);
+}
+
+__device__ __forceinline__ void recur_publish(uint64_t* slot, float A, float B) {
+    const uint32_t lo = __float_as_uint(A);
+    __hip_atomic_store(slot, (uint64_t)__float_as_uint(B) << 32 | (lo == ~0u ? 0x7fc00000u : lo), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// What precedes the tile that is `order`-th of its columns (block `cb` of n), from the segments' maps in lds: f.  A lane per column:
+// the first wavefront joins the tile's own map and publishes it, then each of the four joins a quarter of the maps in front.
+// first: what precedes the first tile, or null.  It is read by the lane that publishes what depends on it, before it does.
+template <bool UP, typename T, int V, typename Lds>
+__device__ __forceinline__ void recur_join(const RecurArgs& a, long n, long cb, int order, const float* first, Lds& lds, int plane, int lc, float (&f)[V]) {
+    constexpr int SEG = 16, W = 16 * V, BATCH = 8;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x % W, e = l % V;
+    const RecurCols<T, V> cols((cb * 16 + l / V) * V, a.M);
+    const bool owner = threadIdx.x < W && e >= cols.skip;
+    uint64_t* slots = a.slots + n * (a.tiles + a.groups) * a.M + cols.col + e;
+    float A = order == 0 ? 0.f : 1.f, B = 0.f;                          // (a tile with nothing in front has a state behind it, not a map)
+    if (wave == 0) {
+        if (order == 0) {
+            B = first ? first[cols.col + e] : 0.f;
+            if (threadIdx.x < W) lds.m[1][1][0][l / V].f[e] = B;
+        }
+#pragma unroll 4
+        for (int i = 0; i < SEG; ++i) {
+            const int s = UP ? i : SEG - 1 - i;
+            const float fa = lds.m[0][0][s][l / V].f[e];
+            B = fmaf(fa, B, lds.m[0][plane][s][l / V].f[e]);
+            A *= fa;
+        }
+        if (owner) recur_publish(slots + (long)order * a.M, A, B);
+    }
+    // the state behind the last group, if there is one, and the maps of this group's tiles
+    const int group = order / RC_GROUP, lead = group > 0, count = order % RC_GROUP + lead, per = (count + 3) / 4;
+    const int i0 = wave * per, i1 = i0 + per < count ? i0 + per : count;
+    if (i0 < i1 && e >= cols.skip) {                                    // (columns that are not stored wait for none)
+        float PA = 1.f, PB = 0.f;
+        for (int b = i0; b < i1; b += BATCH) {
+            uint64_t v[BATCH];
+            bool there;
+            int tries = 0;
+            do {
+                there = true;
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) {
+                    const int i = b + k < i1 ? b + k : i1 - 1;
+                    v[k] = __hip_atomic_load(slots + (lead && i == 0 ? a.tiles + group - 1L : (long)group * RC_GROUP + i - lead) * a.M, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) there = there && (uint32_t)v[k] != ~0u;
+            } while (!there && ++tries < RC_TRIES);
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                if (b + k >= i1) break;
+                const float fa = __uint_as_float((uint32_t)v[k]);
+                PB = fmaf(fa, PB, __uint_as_float((uint32_t)(v[k] >> 32)));
+                PA *= fa;
+            }
+        }
+        if (threadIdx.x % 64 < W) {
+            lds.m[1][0][wave][l / V].f[e] = PA;
+            lds.m[1][1][wave][l / V].f[e] = PB;
+        }
+    }
+    __syncthreads();
+    const int parts = order == 0 ? 1 : (count + per - 1) / per;
+    Lds::get(lds.m[1][1][0][lc], f);
+    for (int w = 1; w < parts; ++w) {
+        float fa[V], fb[V];
+        Lds::get(lds.m[1][0][w][lc], fa);
+        Lds::get(lds.m[1][1][w][lc], fb);
+#pragma unroll
+        for (int k = 0; k < V; ++k) f[k] = fmaf(fa[k], f[k], fb[k]);
+    }
+    if (wave == 0 && order % RC_GROUP == RC_GROUP - 1 && order + 1 < a.tiles) {
+        float c = lds.m[1][1][0][l / V].f[e];
+        for (int w = 1; w < parts; ++w) c = fmaf(lds.m[1][0][w][l / V].f[e], c, lds.m[1][1][w][l / V].f[e]);
+        if (owner) recur_publish(slots + (a.tiles + (long)group) * a.M, 0.f, fmaf(A, c, B));
+    }
+}
+
+template <typename T, int V, int SEG, int RC_K = RC_STEPS, bool JOIN = false>
+__global__ void __launch_bounds__(RC_NT, JOIN ? 4 : 1) recur_fwd_kernel(RecurArgs a) {
     constexpr int LC = RC_NT / SEG, STEPS = SEG * RC_K;
     typedef RecurCols<T, V> Cols;
+    typedef RecurRows<JOIN> Rows;
     typedef RecurLds<SEG, 2, V> Lds;
     __shared__ Lds lds;
     const int lc = threadIdx.x % LC, seg = SEG == 1 ? 0 : threadIdx.x / LC;
     const int nsaved = (a.T - 1) / RC_SAVE;
     const int tiles = (a.T + STEPS - 1) / STEPS;
+    __shared__ int s_tile;
     int par = 0;
     for (long job = blockIdx.x; job < a.jobs; job += gridDim.x) {
-        const long cb = job % a.cblocks;
-        const int span = (int)(job / a.cblocks % a.spans);
-        const long n = job / a.cblocks / a.spans;
+        const RecurJob j(a, a.runs ? xcd_run(job, a.jobs) : job);
+        const long cb = j.cb, n = JOIN ? j.n % (uint32_t)a.N : j.n;
+        const int order = JOIN ? recur_ticket(a, n * a.cblocks + cb, &s_tile) : 0;
+        if (JOIN && (unsigned)order >= (unsigned)tiles) return;         // (a workspace that another call writes to)
         const Cols cols((cb * LC + lc) * V, a.M);
-        const T* x = (const T*)a.x + n * a.T * a.M + cols.col;
-        const T* g = (const T*)a.g + n * a.T * a.M + cols.col;
-        T* y = (T*)a.y + n * a.T * a.M + cols.col;
+        const Rows rows(a, n, JOIN ? order * STEPS : 0, cols.col);
         float c[V];                                                     // the state in front of the tile
-        if (a.spans > 1) {
-            const float* maps = a.maps + n * a.spans * 2 * a.M;
-            cols.load_state(a.maps + ((long)a.N * a.spans * 2 + n) * a.M, c);
-            for (int s = 0; s < span; ++s) {
-                float A[V], B[V];
-                cols.load_state(maps + (long)s * 2 * a.M, A);
-                cols.load_state(maps + ((long)s * 2 + 1) * a.M, B);
-#pragma unroll
-                for (int e = 0; e < V; ++e) c[e] = fmaf(A[e], c[e], B[e]);
-            }
-        } else {
-            cols.load_state(a.h0 ? a.h0 + n * a.M : nullptr, c);
-        }
-        const int tile0 = span * a.tiles_per_span, tile1 = tile0 + a.tiles_per_span < tiles ? tile0 + a.tiles_per_span : tiles;
+        if constexpr (!JOIN) cols.load_state(a.h0 ? a.h0 + n * a.M : nullptr, c);
+        const int tile0 = JOIN ? order : 0, tile1 = JOIN ? order + 1 : tiles;
         typename Cols::Raw rx[RC_K], rg[RC_K];
         auto load = [&](int tile) {                                     // (steps behind the last one read it again)
 #pragma unroll
             for (int i = 0; i < RC_K; ++i) {
                 const int t = tile * STEPS + seg * RC_K + i;
-                const long at = (long)(t < a.T ? t : a.T - 1) * a.M;
-                rx[i] = Cols::load(x + at);
-                rg[i] = Cols::load(g + at);
+                const auto at = rows.at(t < a.T ? t : a.T - 1);
+                rx[i] = Cols::load(rows.template of<T>(a.x, at));
+                rg[i] = Cols::load(rows.template of<T>(a.g, at));
             }
         };
         load(tile0);
         for (int tile = tile0; tile < tile1; ++tile) {
             const int t0 = tile * STEPS + seg * RC_K;
             const bool full = (tile + 1) * STEPS <= a.T;                // of all segments
-            float av[RC_K][V], kx[RC_K][V];
+            Gate<JOIN> gt[RC_K][V];
+            typename Cols::Raw xv[RC_K];
 #pragma unroll
-            for (int i = 0; i < RC_K; ++i)
+            for (int i = 0; i < RC_K; ++i) {
+                xv[i] = rx[i];
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    float k;
-                    gate(Cols::get(rg[i], e), av[i][e], k);
-                    kx[i][e] = k * Cols::get(rx[i], e);
+                    gt[i][e] = Gate<JOIN>::of(Cols::get(rg[i], e));
+                    if constexpr (!JOIN) gt[i][e].kv *= Cols::get(rx[i], e);
                 }
+            }
             if (tile + 1 < tile1) load(tile + 1);                       // on its way while this tile is joined and stored
             if (!full) {                                                // steps beyond the clip change nothing
 #pragma unroll
                 for (int i = 0; i < RC_K; ++i)
-                    if (t0 + i >= a.T)
+                    if (t0 + i >= a.T) {
+                        xv[i] = typename Cols::Raw{};
 #pragma unroll
-                        for (int e = 0; e < V; ++e) {
-                            av[i][e] = 1.f;
-                            kx[i][e] = 0.f;
-                        }
+                        for (int e = 0; e < V; ++e) gt[i][e].open();
+                    }
             }
+            auto kx = [&](int i, int e) {
+                if constexpr (JOIN) return gt[i][e].k() * Cols::get(xv[i], e);
+                else return gt[i][e].kv;
+            };
             float h[V];
             if constexpr (SEG > 1) {
                 float A[V], B[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    A[e] = av[0][e];
-                    B[e] = kx[0][e];
+                    A[e] = gt[0][e].a();
+                    B[e] = kx(0, e);
                 }
 #pragma unroll
                 for (int i = 1; i < RC_K; ++i)
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
-                        A[e] *= av[i][e];
-                        B[e] = fmaf(av[i][e], B[e], kx[i][e]);
+                        A[e] *= gt[i][e].a();
+                        B[e] = fmaf(gt[i][e].a(), B[e], kx(i, e));
                     }
                 Lds::put(lds.m[par][0][seg][lc], A);
                 Lds::put(lds.m[par][1][seg][lc], B);
                 __syncthreads();
-                if (tile > tile0) Lds::get(lds.carry[par ^ 1][lc], c);
+                if constexpr (JOIN) {
+                    recur_join<true, T, V>(a, n, cb, order, a.h0 ? a.h0 + n * a.M : nullptr, lds, 1, lc, c);
+#pragma unroll
+                    for (int i = 0; i < RC_K; ++i) {
+                        Cols::renew(xv[i]);
+#pragma unroll
+                        for (int e = 0; e < V; ++e) gt[i][e].renew();
+                    }
+                } else if (tile > tile0) {
+                    Lds::get(lds.carry[par ^ 1][lc], c);
+                }
 #pragma unroll
                 for (int e = 0; e < V; ++e) h[e] = c[e];
                 lds.template through<true>(par, 1, seg, lc, h);
@@ -226,57 +400,53 @@ __global__ void __launch_bounds__(RC_NT) recur_fwd_kernel(RecurArgs a) {
 #pragma unroll
             for (int i = 0; i < RC_K; ++i) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) h[e] = fmaf(av[i][e], h[e], kx[i][e]);
-                if (full || t0 + i < a.T) cols.store(y + (long)(t0 + i) * a.M, h);
+                for (int e = 0; e < V; ++e) h[e] = fmaf(gt[i][e].a(), h[e], kx(i, e));
+                if (full || t0 + i < a.T) cols.store(rows.template of<T>(a.y, rows.at(t0 + i)), h);
             }
-            if constexpr (SEG > 1) {
+            if constexpr (SEG > 1 && !JOIN) {
                 if (seg == SEG - 1) Lds::put(lds.carry[par][lc], h);
                 par ^= 1;
             }
 #pragma unroll
             for (int e = 0; e < V; ++e) c[e] = h[e];
         }
-        if (a.h_last && span == a.spans - 1 && seg == SEG - 1) cols.store_state(a.h_last + n * a.M, c);
+        if (a.h_last && tile1 == tiles && seg == SEG - 1) cols.store_state(a.h_last + n * a.M, c);
     }
 }
 
-// The tiles of a span from the last to the first.  STEPS is a multiple of RC_SAVE or T does not exceed it, so that the state in
+// The tiles from the last to the first.  STEPS is a multiple of RC_SAVE or T does not exceed it, so that the state in
 // front of every tile is at hand.
-template <typename T, int V, int SEG, int RC_K = RC_STEPS>
-__global__ void __launch_bounds__(RC_NT) recur_bwd_kernel(RecurArgs a) {
+template <typename T, int V, int SEG, int RC_K = RC_STEPS, bool JOIN = false>
+__global__ void __launch_bounds__(RC_NT, JOIN ? 2 : 1) recur_bwd_kernel(RecurArgs a) {
     constexpr int LC = RC_NT / SEG, STEPS = SEG * RC_K;
     typedef RecurCols<T, V> Cols;
+    typedef RecurRows<JOIN> Rows;
     typedef RecurLds<SEG, 3, V> Lds;
     __shared__ Lds lds;
     const int lc = threadIdx.x % LC, seg = SEG == 1 ? 0 : threadIdx.x / LC;
     const int nsaved = (a.T - 1) / RC_SAVE;
     const int tiles = (a.T + STEPS - 1) / STEPS;
+    __shared__ int s_tile;
     int par = 0;
     for (long job = blockIdx.x; job < a.jobs; job += gridDim.x) {
-        const long cb = job % a.cblocks;
-        const int span = (int)(job / a.cblocks % a.spans);
-        const long n = job / a.cblocks / a.spans;
+        const RecurJob j(a, a.runs ? xcd_run(job, a.jobs) : job);
+        const long cb = j.cb, n = JOIN ? j.n % (uint32_t)a.N : j.n;
+        const int order = JOIN ? recur_ticket(a, n * a.cblocks + cb, &s_tile) : 0;
+        if (JOIN && (unsigned)order >= (unsigned)tiles) return;         // (a workspace that another call writes to)
         const Cols cols((cb * LC + lc) * V, a.M);
-        const long base = n * a.T * a.M + cols.col;
         float e1[V];                                                    // E behind the tile
-        cols.load_state(a.dh_last ? a.dh_last + n * a.M : nullptr, e1);
-        for (int s = a.spans - 1; s > span; --s) {
-            float A[V], B[V];
-            cols.load_state(a.maps + (n * a.spans + s) * 2 * a.M, A);
-            cols.load_state(a.maps + ((n * a.spans + s) * 2 + 1) * a.M, B);
-#pragma unroll
-            for (int e = 0; e < V; ++e) e1[e] = fmaf(A[e], e1[e], B[e]);
-        }
-        const int tile0 = span * a.tiles_per_span, tile1 = tile0 + a.tiles_per_span < tiles ? tile0 + a.tiles_per_span : tiles;
+        if constexpr (!JOIN) cols.load_state(a.dh_last ? a.dh_last + n * a.M : nullptr, e1);
+        const int tile0 = JOIN ? tiles - 1 - order : 0, tile1 = JOIN ? tiles - order : tiles;
+        const Rows rows(a, n, JOIN ? tile0 * STEPS : 0, cols.col);
         typename Cols::Raw rx[RC_K], rg[RC_K], rd[RC_K];
         auto load = [&](int tile) {                                     // (steps behind the last one read it again)
 #pragma unroll
             for (int i = 0; i < RC_K; ++i) {
                 const int t = tile * STEPS + seg * RC_K + i;
-                const long at = base + (long)(t < a.T ? t : a.T - 1) * a.M;
-                rx[i] = Cols::load((const T*)a.x + at);
-                rg[i] = Cols::load((const T*)a.g + at);
-                rd[i] = Cols::load((const T*)a.dy + at);
+                const auto at = rows.at(t < a.T ? t : a.T - 1);
+                rx[i] = Cols::load(rows.template of<T>(a.x, at));
+                rg[i] = Cols::load(rows.template of<T>(a.g, at));
+                rd[i] = Cols::load(rows.template of<T>(a.dy, at));
             }
         };
         for (int tile = tile1 - 1; tile >= tile0; --tile) {
@@ -285,21 +455,18 @@ __global__ void __launch_bounds__(RC_NT) recur_bwd_kernel(RecurArgs a) {
             load(tile);
             float h[V];                                                 // the state in front of the tile, then of the segment
             cols.load_state(tile == 0 ? (a.h0 ? a.h0 + n * a.M : nullptr) : a.saved + (n * nsaved + tile * (STEPS / RC_SAVE) - 1) * a.M, h);
-            float av[RC_K][V], kv[RC_K][V];
+            Gate<JOIN> gt[RC_K][V];
 #pragma unroll
             for (int i = 0; i < RC_K; ++i)
 #pragma unroll
-                for (int e = 0; e < V; ++e) gate(Cols::get(rg[i], e), av[i][e], kv[i][e]);
+                for (int e = 0; e < V; ++e) gt[i][e] = Gate<JOIN>::of(Cols::get(rg[i], e));
             if (!full) {                                                // steps beyond the clip change nothing
 #pragma unroll
                 for (int i = 0; i < RC_K; ++i)
                     if (t0 + i >= a.T) {
                         rx[i] = rd[i] = typename Cols::Raw{};
 #pragma unroll
-                        for (int e = 0; e < V; ++e) {
-                            av[i][e] = 1.f;
-                            kv[i][e] = 0.f;
-                        }
+                        for (int e = 0; e < V; ++e) gt[i][e].open();
                     }
             }
             float en[V];                                                // E behind the segment
@@ -307,23 +474,34 @@ __global__ void __launch_bounds__(RC_NT) recur_bwd_kernel(RecurArgs a) {
                 float A[V], B[V], C[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    A[e] = av[0][e];
-                    B[e] = kv[0][e] * Cols::get(rx[0], e);
-                    C[e] = av[RC_K - 1][e] * Cols::get(rd[RC_K - 1], e);
+                    A[e] = gt[0][e].a();
+                    B[e] = gt[0][e].k() * Cols::get(rx[0], e);
+                    C[e] = A[e] * Cols::get(rd[0], e);
                 }
 #pragma unroll
                 for (int i = 1; i < RC_K; ++i)
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
-                        A[e] *= av[i][e];
-                        B[e] = fmaf(av[i][e], B[e], kv[i][e] * Cols::get(rx[i], e));
-                        C[e] = av[RC_K - 1 - i][e] * (Cols::get(rd[RC_K - 1 - i], e) + C[e]);
+                        A[e] *= gt[i][e].a();
+                        B[e] = fmaf(gt[i][e].a(), B[e], gt[i][e].k() * Cols::get(rx[i], e));
+                        C[e] = fmaf(A[e], Cols::get(rd[i], e), C[e]);
                     }
                 Lds::put(lds.m[par][0][seg][lc], A);
                 Lds::put(lds.m[par][1][seg][lc], B);
                 Lds::put(lds.m[par][2][seg][lc], C);
                 __syncthreads();
-                if (tile + 1 < tile1) Lds::get(lds.carry[par ^ 1][lc], e1);
+                if constexpr (JOIN) {
+                    recur_join<false, T, V>(a, n, cb, order, a.dh_last ? a.dh_last + n * a.M : nullptr, lds, 2, lc, e1);
+#pragma unroll
+                    for (int i = 0; i < RC_K; ++i) {
+                        Cols::renew(rx[i]);
+                        Cols::renew(rd[i]);
+#pragma unroll
+                        for (int e = 0; e < V; ++e) gt[i][e].renew();
+                    }
+                } else if (tile + 1 < tile1) {
+                    Lds::get(lds.carry[par ^ 1][lc], e1);
+                }
 #pragma unroll
                 for (int e = 0; e < V; ++e) en[e] = e1[e];
                 lds.template through<true>(par, 1, seg, lc, h);
@@ -338,7 +516,8 @@ __global__ void __launch_bounds__(RC_NT) recur_bwd_kernel(RecurArgs a) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     u[i][e] = h[e] - Cols::get(rx[i], e);
-                    h[e] = fmaf(av[i][e], h[e], kv[i][e] * Cols::get(rx[i], e));
+                    h[e] = fmaf(gt[i][e].a(), h[e], gt[i][e].k() * Cols::get(rx[i], e));
+                    gt[i][e].renew();
                 }
 #pragma unroll
             for (int i = RC_K - 1; i >= 0; --i) {
@@ -346,133 +525,52 @@ __global__ void __launch_bounds__(RC_NT) recur_bwd_kernel(RecurArgs a) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     const float D = Cols::get(rd[i], e) + en[e];
-                    ox[e] = kv[i][e] * D;
-                    en[e] = av[i][e] * D;
-                    og[e] = en[e] * (kv[i][e] * u[i][e]);
+                    ox[e] = gt[i][e].k() * D;
+                    en[e] = gt[i][e].a() * D;
+                    og[e] = en[e] * (gt[i][e].k() * u[i][e]);
                 }
                 if (full || t0 + i < a.T) {
-                    const long at = base + (long)(t0 + i) * a.M;
-                    cols.store((T*)a.dx + at, ox);
-                    cols.store((T*)a.dg + at, og);
+                    const auto at = rows.at(t0 + i);
+                    cols.store(rows.template of<T>(a.dx, at), ox);
+                    cols.store(rows.template of<T>(a.dg, at), og);
                 }
             }
-            if constexpr (SEG > 1) {
+            if constexpr (SEG > 1 && !JOIN) {
                 if (seg == 0) Lds::put(lds.carry[par][lc], en);
                 par ^= 1;
             }
 #pragma unroll
             for (int e = 0; e < V; ++e) e1[e] = en[e];
         }
-        if (a.dh0 && span == 0 && seg == 0) cols.store_state(a.dh0 + n * a.M, e1);
-    }
-}
-
-// The map of every span but the one that nothing follows, for launches that split the time axis: h behind the span as a map of h
-// in front of it, or (BWD) E in front of it as a map of E behind it.
-template <typename T, int V, bool BWD>
-__global__ void __launch_bounds__(RC_NT) recur_span_kernel(RecurArgs a, int steps_per_span) {
-    constexpr int SEG = 16, LC = RC_NT / SEG, RC_K = RC_STEPS, STEPS = SEG * RC_K;
-    typedef RecurCols<T, V> Cols;
-    typedef RecurLds<SEG, 2, V> Lds;
-    __shared__ Lds lds;
-    const int lc = threadIdx.x % LC, seg = threadIdx.x / LC;
-    const long cblocks = (a.M + LC * V - 1) / (LC * V), jobs = cblocks * a.spans * a.N;
-    int par = 0;
-    for (long job = blockIdx.x; job < jobs; job += gridDim.x) {
-        const long cb = job % cblocks;
-        const int span = (int)(job / cblocks % a.spans);
-        const long n = job / cblocks / a.spans;
-        const Cols cols((cb * LC + lc) * V, a.M);
-        if (!BWD && span == 0 && seg == 0) {    // a copy of the first state: h_last may be the same memory
-            float h[V];
-            cols.load_state(a.h0 ? a.h0 + n * a.M : nullptr, h);
-            cols.store_state(a.maps + ((long)a.N * a.spans * 2 + n) * a.M, h);
-        }
-        if (span == (BWD ? 0 : a.spans - 1)) continue;
-        const int begin = span * steps_per_span, end = begin + steps_per_span < a.T ? begin + steps_per_span : a.T;
-        const int tiles = (end - begin + STEPS - 1) / STEPS;
-        const long base = n * a.T * a.M + cols.col;
-        float A1[V], B1[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            A1[e] = 1.f;
-            B1[e] = 0.f;
-        }
-        for (int q = 0; q < tiles; ++q) {
-            const int t0 = begin + (BWD ? tiles - 1 - q : q) * STEPS + seg * RC_K;
-            typename Cols::Raw rb[RC_K], rg[RC_K];
-#pragma unroll
-            for (int i = 0; i < RC_K; ++i) {
-                const long at = base + (long)(t0 + i < end ? t0 + i : end - 1) * a.M;
-                rb[i] = Cols::load((const T*)(BWD ? a.dy : a.x) + at);
-                rg[i] = Cols::load((const T*)a.g + at);
-            }
-            float A[V], B[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                A[e] = 1.f;
-                B[e] = 0.f;
-            }
-#pragma unroll
-            for (int j = 0; j < RC_K; ++j) {
-                const int i = BWD ? RC_K - 1 - j : j;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float ga, gk;
-                    gate(Cols::get(rg[i], e), ga, gk);
-                    const float b = Cols::get(rb[i], e), nb = BWD ? ga * (b + B[e]) : fmaf(ga, B[e], gk * b);
-                    A[e] = t0 + i < end ? A[e] * ga : A[e];
-                    B[e] = t0 + i < end ? nb : B[e];
-                }
-            }
-            Lds::put(lds.m[par][0][seg][lc], A);
-            Lds::put(lds.m[par][1][seg][lc], B);
-            __syncthreads();
-            if (seg == 0) {
-#pragma unroll
-                for (int s = 0; s < SEG; ++s) {
-                    const typename Lds::Vec fa = lds.m[par][0][BWD ? SEG - 1 - s : s][lc], fb = lds.m[par][1][BWD ? SEG - 1 - s : s][lc];
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        A1[e] *= fa.f[e];
-                        B1[e] = fmaf(fa.f[e], B1[e], fb.f[e]);
-                    }
-                }
-            }
-            par ^= 1;
-        }
-        if (seg == 0) {
-            cols.store_state(a.maps + (n * a.spans + span) * 2 * a.M, A1);
-            cols.store_state(a.maps + ((n * a.spans + span) * 2 + 1) * a.M, B1);
-        }
+        if (a.dh0 && tile0 == 0 && seg == 0) cols.store_state(a.dh0 + n * a.M, e1);
     }
 }
 
 // ---- host --------------------------------------------------------------------------------
 struct RecurPlan {
     int v, seg;           // columns per thread, segments per tile
-    int spans, tiles_per_span;
+    bool join;            // the tiles of a column side by side
+    int tiles, groups;
     long cblocks, jobs;
 };
 
 // Segments: as few as hold the clip (8 steps each), so that threads lie along the columns, where a row of memory is, up to 16 with rows of
-// 64 columns.  What then leaves CUs idle splits the time axis into spans, whose maps a launch of their own takes first, at the price of
-// reading two tensors twice.  us in one span and in 1024 blocks of them, bf16, 2048 columns per clip: forward 4 clips of 4096 frames (128
-// blocks in one span) 84, 62, 5 of 2048 45, 45, 6 of 2048 45, 47, 8 of 2048 47, 59; backward 170, 94; 70, 56; 73, 65; 99, 91; 12 of 1024 50, 63.
+// 64 columns.  Tiles of a column run side by side where a block or less per CU would take four tiles and more in turn.  us in turn and side by
+// side, bf16, 2048 columns per clip: 4 clips of 300 frames (3 tiles) forward 10.5, 11.3, backward 13.7, 13.1; of 512 12.7, 11.3 and
+// 17.7, 13.7; of 1024 22.6, 14.3 and 35.3, 23.2; 8 clips of 1024 25.8, 23.7 and 42.7, 38.4; 16 clips 36.6, 38.6 and 58.4, 67.3.  fp32 forward,
+// which has registers for fewer tiles at a time: 4 clips of 512 13.5, 15.5, 8 clips of 1024 34.0, 41.7.
 static RecurPlan recur_plan(const tsm_recur_desc* d, bool bwd) {
     RecurPlan p;
     const long M = (long)d->C * d->H * d->W;
     p.v = M < RC_V ? 1 : RC_V;
     p.seg = d->T <= RC_STEPS ? 1 : d->T <= 4 * RC_STEPS ? 4 : d->T <= 8 * RC_STEPS ? 8 : 16;
-    const int steps = p.seg * RC_STEPS, tiles = cdiv(d->T, steps), width = RC_NT / p.seg * p.v;
+    const int width = RC_NT / p.seg * p.v;
+    p.tiles = cdiv(d->T, p.seg * RC_STEPS);
+    p.groups = (p.tiles - 1) / RC_GROUP;
     p.cblocks = (M + width - 1) / width;
-    const long blocks = p.cblocks * d->N;
-    long want = blocks <= (bwd ? 224 : 160) ? 1024 / blocks : 1;
-    if (want > 64) want = 64;
-    if (want > tiles) want = tiles;
-    p.tiles_per_span = cdiv(tiles, want);
-    p.spans = cdiv(tiles, p.tiles_per_span);
-    p.jobs = blocks * p.spans;
+    p.jobs = p.cblocks * d->N;
+    p.join = p.tiles >= 4 && p.jobs <= (!bwd && d->dtype == TSM_F32 ? 128 : 256);
+    if (p.join) p.jobs *= p.tiles;
     return p;
 }
 
@@ -486,8 +584,9 @@ static int recur_check(const tsm_recur_desc* d, const char* who) {
 }
 
 static size_t recur_saved(const tsm_recur_desc* d) { return (size_t)d->N * ((d->T - 1) / RC_SAVE) * d->C * d->H * d->W * sizeof(float); }
+static size_t recur_tickets(const tsm_recur_desc* d, const RecurPlan& p) { return align_up((size_t)d->N * p.cblocks * RC_TICKET * 4); }
 static size_t recur_ws(const tsm_recur_desc* d, const RecurPlan& p) {
-    return p.spans > 1 ? align_up((size_t)d->N * (2 * p.spans + 1) * d->C * d->H * d->W * sizeof(float)) : 0;
+    return p.join ? recur_tickets(d, p) + align_up((size_t)d->N * (p.tiles + p.groups) * d->C * d->H * d->W * sizeof(uint64_t)) : 0;
 }
 
 static RecurArgs recur_args(const tsm_recur_desc* d, const RecurPlan& p) {
@@ -497,29 +596,34 @@ static RecurArgs recur_args(const tsm_recur_desc* d, const RecurPlan& p) {
     a.jobs = p.jobs;
     a.N = d->N;
     a.T = d->T;
-    a.spans = p.spans;
-    a.tiles_per_span = p.tiles_per_span;
+    a.tiles = p.tiles;
+    a.groups = p.groups;
+    a.runs = p.seg > 1 && a.M * dtype_size(d->dtype) % 128 != 0;
     return a;
+}
+
+static void recur_slots(const tsm_recur_desc* d, const RecurPlan& p, RecurArgs& a, void* ws) {
+    a.tickets = (uint32_t*)ws;
+    a.slots = (uint64_t*)((char*)ws + recur_tickets(d, p));
+    a.ws_bytes = recur_ws(d, p);
 }
 
 template <typename T, int V>
 static int recur_run(const RecurArgs& a, const RecurPlan& p, bool bwd, hipStream_t s) {
-    const unsigned cap = 1u << 22;
-    const dim3 block(RC_NT), grid((unsigned)(a.jobs < cap ? a.jobs : cap));
-    if (p.spans > 1) {
-        const long jobs = (a.M + 16 * V - 1) / (16 * V) * a.N * a.spans;
-        const dim3 sgrid((unsigned)(jobs < cap ? jobs : cap));
-        const int steps = a.tiles_per_span * p.seg * RC_STEPS;
-        if (bwd) recur_span_kernel<T, V, true><<<sgrid, block, 0, s>>>(a, steps);
-        else recur_span_kernel<T, V, false><<<sgrid, block, 0, s>>>(a, steps);
-        TSM_TRY(check_launch(bwd ? "recur_bwd_spans" : "recur_fwd_spans"));
+    const long cap = 1 << 22;
+    const dim3 block(RC_NT), grid((unsigned)std::min(a.jobs, cap));
+    if (p.join) {
+        const long n = a.ws_bytes / 16;
+        recur_clear_kernel<<<dim3((unsigned)std::min((n + 255) / 256, 2048L)), dim3(256), 0, s>>>((any_u32x4*)a.tickets, n);
+        TSM_TRY(check_launch("recur_clear"));
     }
 #define CALL(...)                                                                \
     do {                                                                         \
         if (bwd) recur_bwd_kernel<T, V, __VA_ARGS__><<<grid, block, 0, s>>>(a);  \
         else recur_fwd_kernel<T, V, __VA_ARGS__><<<grid, block, 0, s>>>(a);      \
     } while (0)
-    if (a.T == 1) CALL(1, 1);
+    if (p.join) CALL(16, RC_STEPS, true);
+    else if (a.T == 1) CALL(1, 1);
     else if (a.T <= 4) CALL(1, 4);
     else if (p.seg == 1) CALL(1);
     else if (p.seg == 4) CALL(4);
@@ -561,7 +665,8 @@ int tsm_recur_fwd(const tsm_recur_desc* d, const void* x, const void* g, const f
     const Span in[] = {{x, n, "x"}, {g, n, "g"}, {h0 == h_last ? nullptr : h0, st, "h0"}};
     const Span out[] = {{y, n, "y"}, {h_last, st, "h_last"}, {saved, recur_saved(d), "saved"}, {ws, need, "the workspace"}};
     TSM_TRY(check_spans(who, in, 3, out, 4));
-    a.x = x; a.g = g; a.h0 = h0; a.y = y; a.h_last = h_last; a.saved = (float*)saved; a.maps = (float*)ws;
+    a.x = x; a.g = g; a.h0 = h0; a.y = y; a.h_last = h_last; a.saved = (float*)saved;
+    recur_slots(d, p, a, ws);
     return recur_any(a, p, d->dtype, false, (hipStream_t)stream);
 }
 
@@ -580,7 +685,8 @@ int tsm_recur_bwd(const tsm_recur_desc* d, const void* x, const void* g, const f
     const Span in[] = {{x, n, "x"}, {g, n, "g"}, {h0, st, "h0"}, {saved, sv, "saved"}, {dy, n, "dy"}, {dh_last, st, "dh_last"}};
     const Span out[] = {{dx, n, "dx"}, {dg, n, "dg"}, {dh0, st, "dh0"}, {ws, need, "the workspace"}};
     TSM_TRY(check_spans(who, in, 6, out, 4));
-    a.x = x; a.g = g; a.h0 = h0; a.saved = (float*)saved; a.dy = dy; a.dh_last = dh_last; a.dx = dx; a.dg = dg; a.dh0 = dh0; a.maps = (float*)ws;
+    a.x = x; a.g = g; a.h0 = h0; a.saved = (float*)saved; a.dy = dy; a.dh_last = dh_last; a.dx = dx; a.dg = dg; a.dh0 = dh0;
+    recur_slots(d, p, a, ws);
     return recur_any(a, p, d->dtype, true, (hipStream_t)stream);
 }
 

@@ -1119,7 +1119,7 @@ static int xent_fwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
         TSM_TRY((x_product<XE_STATS, X_ROWS, X_ROWS, F32>(p.size, a, 1, "xent_stats", s)));
         tiles += (a.N + t - 1) / t;
     }
-    // few rows: four wavefronts each (4 rows x 2048 tiles: 65.0 -> 61.0 us for the whole call)
+    // few rows: four wavefronts each (4 rows x 1024 tiles: 65.0 -> 61.0 us for the whole call)
     const float2* part = (const float2*)(ws + p.o_part);
     const bool wide = a.M < 1024;
     const long blocks = wide ? a.M : std::min((a.M + 3) / 4, 65536L);

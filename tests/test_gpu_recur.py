@@ -181,3 +181,109 @@ def test_gradient_is_that_of_the_kernels_own_forward():
     want = float((dx.double() * ux.double()).sum() + (dg.double() * ug.double()).sum())
     scale = float(np.sqrt((dx.double() ** 2).sum().item() + (dg.double() ** 2).sum().item()))
     assert abs(slope - want) < 1e-2 * scale, (slope, want, scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 512, 64, 1, 1), (3, 600, 131, 1, 1), (1, 1500, 67, 1, 1), (2, 640, 3, 1, 1), (1, 8193, 70, 1, 1), (2, 16500, 5, 1, 1)])
+def test_long_memory(shape, dtype):
+    """Gates that keep 99 % of a state of about 2, so that what one tile hands to the next is most of what follows (64 tiles
+    of 128 steps and more among them).
+    Bounds: a step adds 8 units of X to the error of the state (see above) and passes on a times what there was.  A rounding of a
+    product of gates, or of a map, of steps i to j is at most one unit of X times the gates behind j, what a step at j would add; a step
+    is part of at most five levels of maps (thread, tile, quarter, group, all) of two roundings each: 20 units per step for all.  The
+    same for E = a D, with the recurrence of |dy| in place of X."""
+    N, T, C, Hh, W = shape
+    M = C * Hh * W
+    x, g = values((N, T, M), 10, dtype, shift=2.0), values((N, T, M), 11, dtype, shift=5.0)
+    (x, g, h0, dy, dl), (y, hl, dx, dg, dh0) = _run(shape, dtype, True, x=x, g=g)
+    h = H.recur_fwd(x, g, h0)
+    rdx, rdg, rdh0 = H.recur_bwd(x, g, h0, dy, dl)
+    X = max(np.abs(x).max(), np.abs(h0).max())
+    a, k = H.sigmoid(g), H.sigmoid(-g)
+    F, E, Dabs = np.zeros_like(h), np.zeros_like(h), np.abs(dy).copy()
+    err = np.zeros((N, M))
+    for t in range(T):
+        F[:, t] = err = a[:, t] * err + 20 * U * X
+    e, err = np.abs(dl), np.zeros((N, M))
+    for t in reversed(range(T)):
+        Dabs[:, t] += e
+        E[:, t] = err = err + 20 * U * Dabs[:, t]              # of D
+        e, err = a[:, t] * Dabs[:, t], a[:, t] * err
+    half = HALF[dtype]
+    within(y, h, F + half * np.abs(h), "y")
+    within(hl, h[:, -1], F[:, -1], "h_last")
+    within(dx, rdx, k * E + 8 * U * k * Dabs + half * np.abs(rdx), "dx")
+    within(dg, rdg, k * (2 * X * E + Dabs * F.max() + 32 * U * Dabs * X) + half * np.abs(rdg), "dg")
+    within(dh0, rdh0, err + 8 * U * e, "dh0")
+
+
+def test_contents_of_the_workspace_do_not_matter():
+    N, T, M = 2, 700, 90
+    d = B.RecurDesc(N=N, T=T, C=M, H=1, W=1, dtype=B.TSM_F32)
+    x, g, dy = (values((N, T, M), s, "f32", shift=4.0 * (s == 1))[0] for s in range(3))
+    saved, ws = scratch(B.tsm_recur_saved_bytes(d)), scratch(B.tsm_recur_workspace_bytes(d))
+    assert ws is not None
+    got = []
+    for fill in (255, 0, 63, None):                # (None: what the call before has left)
+        y, dx, dg = (torch.empty_like(x) for _ in range(3))
+        if fill is not None:
+            ws.fill_(fill)
+        B.tsm_recur_fwd(d, x, g, None, y, None, saved, ws)
+        if fill is not None:
+            ws.fill_(fill)
+        B.tsm_recur_bwd(d, x, g, None, saved, dy, None, dx, dg, None, ws)
+        got.append([v.cpu().numpy() for v in (y, dx, dg)])
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert np.array_equal(a, b)
+
+
+def test_long_clips_on_two_streams_and_in_graphs_that_share_a_workspace():
+    N, T, M = 3, 2000, 300
+    d = B.RecurDesc(N=N, T=T, C=M, H=1, W=1, dtype=B.TSM_BF16)
+    sets = []
+    for s in range(2):
+        x, g, dy = (values((N, T, M), 3 * s + k, "bf16", shift=4.0 * (k == 1))[0] for k in range(3))
+        sets.append((x, g, dy, [torch.empty_like(x) for _ in range(3)], scratch(B.tsm_recur_saved_bytes(d)), scratch(B.tsm_recur_workspace_bytes(d))))
+
+    def run(s, ws=None):
+        x, g, dy, (y, dx, dg), saved, own = s
+        B.tsm_recur_fwd(d, x, g, None, y, None, saved, own if ws is None else ws)
+        B.tsm_recur_bwd(d, x, g, None, saved, dy, None, dx, dg, None, own if ws is None else ws)
+
+    def results(clear=False):
+        torch.cuda.synchronize()
+        out = [[v.float().cpu().numpy() for v in s[3]] for s in sets]
+        if clear:
+            for s in sets:
+                for v in s[3]:
+                    v.fill_(float("nan"))
+        return out
+    for s in sets:
+        run(s)
+    want = results(True)
+
+    def same(got):
+        for a, b in zip(want, got):
+            for u, v in zip(a, b):
+                assert np.array_equal(u, v)
+    streams = [torch.cuda.Stream() for _ in sets]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        for st, s in zip(streams, sets):
+            with torch.cuda.stream(st):
+                run(s)
+    same(results(True))
+    shared, graphs = scratch(B.tsm_recur_workspace_bytes(d)), []
+    for s in sets:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=streams[0]):
+            run(s, shared)
+        graphs.append(graph)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for graph in graphs:
+            graph.replay()
+        run(sets[0])
+        same(results(True))
