@@ -13,7 +13,8 @@
 // The backward pass needs h inside a tile: it starts from the states that the forward pass left every 128 steps (1.6 % of a bf16
 // tensor), and forms h again from x and g, which it reads anyway, instead of reading y, which is rounded.
 // Measured, bf16: 64 clips of 8 frames of 7 x 7 x 2048: forward 53.5 us (5.8 TB/s), backward 82 us (6.3 TB/s); 4 clips of 4096 frames
-// of 2048 values: 43 and 68 us (4.7 and 4.9 TB/s; a copy of that size reaches 6.7).
+// of 2048 values: 46 and 76 us (4.4 TB/s; a copy of that size reaches 6.7: a tile waits on loads, on the tiles in front and on its
+// stores in turn, with four and three tiles per CU to cover for one another).
 #include <algorithm>
 #include <type_traits>
 #include "internal.h"
@@ -121,7 +122,8 @@ struct RecurCols {
 };
 
 // Every XCD takes a run of the jobs, so that blocks beside one another share the lines of memory that lie across their border in its L2
-// (3 x 301 x 4995 fp32: forward 16.6 -> 13.9 us, backward 30.8 -> 25.3; rows of whole lines are better off without, 64 x 8 frames 142 -> 146).
+// (3 x 301 x 4995 fp32: forward 16.6 -> 13.9 us, backward 30.8 -> 25.3), and tiles side by side read neighbouring memory at one time (4 x
+// 4096 x 2048 142 -> 130).  Rows of whole lines in turn are better off without: 64 x 8 frames 142 -> 146.
 __device__ __forceinline__ long xcd_run(long job, long jobs) {
     const long xcd = job & 7;
     return xcd * (jobs / 8) + (xcd < jobs % 8 ? xcd : jobs % 8) + (job >> 3);
@@ -204,8 +206,8 @@ struct RecurLds {
 // state behind it, where those of the next group begin.  A block of columns hands out its tiles by ticket, in their order: whoever
 // a tile waits for was taken before it, by a block that is on a CU and that waits for still earlier tiles only, so every wait ends.  (It is
 // bounded all the same, for callers that share a workspace between streams: what is missing then enters as the NaN of an empty
-// slot.)  One ticket counter for all columns costs 15 ns a tile in turn: 4 x 4096 frames of 2048 values forward 77 us, with a counter
-// per block of columns 43; a launch of its own for the maps, which reads x and g twice, 61.
+// slot.)  One ticket counter for all columns costs 15 ns a tile in turn: 4 x 4096 frames of 2048 values forward, again and again
+// on the same tensors, 77 us, with a counter per block of columns 43; a launch of its own for the maps, which reads x and g twice, 61.
 static constexpr int RC_TRIES = 1 << 22;
 
 __global__ void __launch_bounds__(256) recur_clear_kernel(any_u32x4* p, long n) {
@@ -598,7 +600,7 @@ static RecurArgs recur_args(const tsm_recur_desc* d, const RecurPlan& p) {
     a.T = d->T;
     a.tiles = p.tiles;
     a.groups = p.groups;
-    a.runs = p.seg > 1 && a.M * dtype_size(d->dtype) % 128 != 0;
+    a.runs = p.join || (p.seg > 1 && a.M * dtype_size(d->dtype) % 128 != 0);
     return a;
 }
 
