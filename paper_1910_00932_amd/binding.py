@@ -349,6 +349,13 @@ def tsm_lr_schedule(epoch, total_batch, warm_batch=8, warmup_epochs=5.0, total_e
 _TORCH_DTYPE = {TSM_F32: torch.float32, TSM_BF16: torch.bfloat16}
 
 
+def _device():
+    try:
+        return torch.cuda.current_device()
+    except RuntimeError:        # no GPU: no tensor is on it
+        return -1
+
+
 def _arg(t, n, dtype, name, dev, at_least=False):
     """The pointer of a tensor of n values of a torch dtype on the current device, dev; None stays None."""
     if t is None or isinstance(t, int):
@@ -385,7 +392,7 @@ def tsm_recur_fwd(desc, x, g, h0, y, h_last, saved, ws, stream=None):
     m = desc.N * desc.C * desc.H * desc.W
     n, dt, f = m * desc.T, _TORCH_DTYPE.get(desc.dtype), torch.float32
     p, nb = _ws(ws)
-    dev = torch.cuda.current_device()
+    dev = _device()
     _check(lib().tsm_recur_fwd(ctypes.addressof(desc), _arg(x, n, dt, "x", dev), _arg(g, n, dt, "g", dev), _arg(h0, m, f, "h0", dev),
                                _arg(y, n, dt, "y", dev), _arg(h_last, m, f, "h_last", dev),
                                _saved(saved, desc), p, nb, _stream(stream)))
@@ -395,7 +402,7 @@ def tsm_recur_bwd(desc, x, g, h0, saved, dy, dh_last, dx, dg, dh0, ws, stream=No
     m = desc.N * desc.C * desc.H * desc.W
     n, dt, f = m * desc.T, _TORCH_DTYPE.get(desc.dtype), torch.float32
     p, nb = _ws(ws)
-    dev = torch.cuda.current_device()
+    dev = _device()
     _check(lib().tsm_recur_bwd(ctypes.addressof(desc), _arg(x, n, dt, "x", dev), _arg(g, n, dt, "g", dev), _arg(h0, m, f, "h0", dev),
                                _saved(saved, desc),
                                _arg(dy, n, dt, "dy", dev), _arg(dh_last, m, f, "dh_last", dev), _arg(dx, n, dt, "dx", dev),
@@ -408,7 +415,7 @@ def tsm_layernorm_workspace_bytes(desc):
 
 def tsm_layernorm_fwd(desc, x, gamma, beta, y, mean, rstd, stream=None):
     n, r, c, dt, f = desc.rows * desc.C, desc.rows, desc.C, _TORCH_DTYPE.get(desc.dtype), torch.float32
-    dev = torch.cuda.current_device()
+    dev = _device()
     _check(lib().tsm_layernorm_fwd(ctypes.addressof(desc), _arg(x, n, dt, "x", dev), _arg(gamma, c, f, "gamma", dev),
                                    _arg(beta, c, f, "beta", dev), _arg(y, n, dt, "y", dev), _arg(mean, r, f, "mean", dev, True),
                                    _arg(rstd, r, f, "rstd", dev, True), _stream(stream)))
@@ -417,7 +424,7 @@ def tsm_layernorm_fwd(desc, x, gamma, beta, y, mean, rstd, stream=None):
 def tsm_layernorm_bwd(desc, x, dy, gamma, mean, rstd, dx, dgamma, dbeta, ws, stream=None):
     n, r, c, dt, f = desc.rows * desc.C, desc.rows, desc.C, _TORCH_DTYPE.get(desc.dtype), torch.float32
     p, nb = _ws(ws)
-    dev = torch.cuda.current_device()
+    dev = _device()
     _check(lib().tsm_layernorm_bwd(ctypes.addressof(desc), _arg(x, n, dt, "x", dev), _arg(dy, n, dt, "dy", dev),
                                    _arg(gamma, c, f, "gamma", dev), _arg(mean, r, f, "mean", dev, True), _arg(rstd, r, f, "rstd", dev, True),
                                    _arg(dx, n, dt, "dx", dev), _arg(dgamma, c, f, "dgamma", dev), _arg(dbeta, c, f, "dbeta", dev), p, nb,
@@ -431,7 +438,7 @@ def tsm_xent_workspace_bytes(desc):
 def tsm_xent_fwd(desc, x, w, bias, labels, loss, lse, ws, stream=None):
     r, d, v, dt, f = desc.rows, desc.features, desc.classes, _TORCH_DTYPE.get(desc.dtype), torch.float32
     p, nb = _ws(ws)
-    dev = torch.cuda.current_device()
+    dev = _device()
     _check(lib().tsm_xent_fwd(ctypes.addressof(desc), _arg(x, r * d, dt, "x", dev), _arg(w, v * d, dt, "w", dev),
                               _arg(bias, v, f, "bias", dev), _arg(labels, r, torch.int32, "labels", dev), _arg(loss, r, f, "loss", dev),
                               _arg(lse, r, f, "lse", dev), p, nb, _stream(stream)))
@@ -440,7 +447,7 @@ def tsm_xent_fwd(desc, x, w, bias, labels, loss, lse, ws, stream=None):
 def tsm_xent_bwd(desc, x, w, bias, labels, lse, dloss, dx, dw, dbias, ws, stream=None):
     r, d, v, dt, f = desc.rows, desc.features, desc.classes, _TORCH_DTYPE.get(desc.dtype), torch.float32
     p, nb = _ws(ws)
-    dev = torch.cuda.current_device()
+    dev = _device()
     _check(lib().tsm_xent_bwd(ctypes.addressof(desc), _arg(x, r * d, dt, "x", dev), _arg(w, v * d, dt, "w", dev),
                               _arg(bias, v, f, "bias", dev), _arg(labels, r, torch.int32, "labels", dev), _arg(lse, r, f, "lse", dev),
                               _arg(dloss, r, f, "dloss", dev), _arg(dx, r * d, dt, "dx", dev), _arg(dw, v * d, dt, "dw", dev),
