@@ -557,7 +557,8 @@ struct RecurPlan {
 };
 
 // Segments: as few as hold the clip (8 steps each), so that threads lie along the columns, where a row of memory is, up to 16 with rows of
-// 64 columns.  Tiles of a column run side by side where a block or less per CU would take four tiles and more in turn.  us in turn and side by
+// 64 columns.  Tiles of a column run side by side where a block or less per CU would take four tiles and more in turn (backward three, at
+// half a block).  us in turn and side by
 // side, bf16, 2048 columns per clip: 4 clips of 300 frames (3 tiles) forward 10.5, 11.3, backward 13.7, 13.1; of 512 12.7, 11.3 and
 // 17.7, 13.7; of 1024 22.6, 14.3 and 35.3, 23.2; 8 clips of 1024 25.8, 23.7 and 42.7, 38.4; 16 clips 36.6, 38.6 and 58.4, 67.3.  fp32 forward,
 // which has registers for fewer tiles at a time: 4 clips of 512 13.5, 15.5, 8 clips of 1024 34.0, 41.7.
@@ -571,7 +572,7 @@ static RecurPlan recur_plan(const tsm_recur_desc* d, bool bwd) {
     p.groups = (p.tiles - 1) / RC_GROUP;
     p.cblocks = (M + width - 1) / width;
     p.jobs = p.cblocks * d->N;
-    p.join = p.tiles >= 4 && p.jobs <= (!bwd && d->dtype == TSM_F32 ? 128 : 256);
+    p.join = (p.tiles >= 4 && p.jobs <= (!bwd && d->dtype == TSM_F32 ? 128 : 256)) || (bwd && p.tiles == 3 && p.jobs <= 128);
     if (p.join) p.jobs *= p.tiles;
     return p;
 }
