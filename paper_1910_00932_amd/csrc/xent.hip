@@ -7,7 +7,7 @@
 // joined over the tiles) and the label's logit.  Backward: s is formed again in pieces of the classes, a piece of G lives in the
 // workspace for the two products that read it.  Four products of rows x features x classes in all, on the bf16 matrix cores.
 //
-// bf16: G is rounded once, to the type of the matrix cores' operands; lse, the losses, db (from G before that rounding) and
+// bf16: G, but for a factor (XScale), is rounded once, to the type of the matrix cores' operands; lse, the losses, db (from G before that rounding) and
 // all sums are fp32.  fp32: x, w and G are cut into three bf16 parts each, exactly (8 + 8 + 8 bits), and a product is the sum of the
 // six largest part products (the method of Henry, Tang and Heinecke, "Leveraging the bfloat16 artificial intelligence datatype for
 // higher-precision computations", 2019; what is left out is at most 2^-24 of it), one after the other along K, the small parts first.
@@ -31,7 +31,8 @@ struct XentEpi {
     const int32_t* labels;
     long col0, classes;
     // GRAD
-    const float *lse, *dloss;
+    const float *lse, *dloss;     // (dloss for OUT too, with labels and classes)
+    long rows;               // OUT: of the whole pass
     bf16_t* G;               // in blocks (X_GROWS): ldg elements per 256 rows, gplane from one part to the next
     long ldg, gplane;
     float* dbias_part;       // [row tiles][lddb]
@@ -65,6 +66,26 @@ __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float
     s = (m == t ? s : s * __expf(m - t)) + (m2 == t ? s2 : s2 * __expf(m2 - t));
     m = t;
 }
+
+// The factor in [1, 2) that bf16 G leaves out of dloss, and what reads G puts back: the mantissa of the first ordinary dloss among the
+// first 64 rows with a label, the same in every tile.  A mean's dloss is one number for all rows, and the entry of a row's label, by far
+// its largest, is almost that number: rounded with it, all of them would be off alike, by up to 2^-9 of the whole gradient.
+struct XScale {
+    float up;
+    bool ok;
+    __device__ __forceinline__ void load(const XentEpi& e, long M) {
+        const int lane = threadIdx.x & 63;
+        const long r = lane < M ? lane : M - 1;
+        up = e.dloss[r];
+        ok = is_class(e.labels[r], e.classes);
+    }
+    __device__ __forceinline__ float get() const {
+        const uint32_t bits = __float_as_uint(up), exponent = (bits >> 23) & 0xff;
+        const uint64_t rows = __ballot(ok && exponent != 0 && exponent != 0xff);
+        const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)bits, rows ? __builtin_ctzll(rows) : 0);
+        return rows ? __uint_as_float((first & 0x7fffffu) | 0x3f800000u) : 1.f;
+    }
+};
 
 // ---- tiles: BM x BN results of wavefronts that share the operands through LDS ---------------------------------------------
 // Operands come 64 steps of K at a time (32 for those in three parts), straight from memory into an LDS stage while another is
@@ -474,6 +495,10 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    constexpr bool SCALE = !SPLIT && MODE != XE_STATS;
+    XScale scale;
+    float factor = 1.f;
+    if constexpr (SCALE && MODE == XE_OUT) scale.load(a.e, a.e.rows);      // (awaited behind the first steps' loads)
     if (steps > 0) {
         pa.init(a.A, a.lda, m0, a.M, kb, tid);
         pb.init(a.B, a.ldb, n0, a.N, kb, tid);
@@ -519,6 +544,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
         // stages of 32 K, up to four steps ahead, gained nothing (18.0 against 17.6), four wavefronts of 128 x 128 lose (20.4).  Persistent
         // blocks that load a tile's first steps behind the epilogue before are no faster (that epilogue is 3 of 58 us at 2048 features).
         if (steps > 1) next_step(1);
+        if constexpr (SCALE && MODE == XE_OUT) factor = scale.get();
         if (steps > 0) {
             if (steps > 1) x_wait<NP>();
             else x_wait<0>();
@@ -610,6 +636,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
         // before is free.
         if (steps > 1) next_step(1);
         if (steps > 2) next_step(2);
+        if constexpr (SCALE && MODE == XE_OUT) factor = scale.get();
         int stage = 0;
         for (int s = 0; s < steps; ++s) {
             if (s + NS - 2 < steps) x_wait<(NS - 2) * NP>();
@@ -643,13 +670,17 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
         return mrow(i) < a.M && is_class(label[i], a.e.classes) && ln >= 0 && ln < cols ? (int)ln : -1;
     };
     if constexpr (MODE != XE_OUT) {
+        if constexpr (SCALE) {
+            scale.load(a.e, a.M);
+            factor = scale.get();
+        }
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const long m = mrow(i) < a.M ? mrow(i) : a.M - 1;
             label[i] = a.e.labels[m];
             if constexpr (MODE == XE_GRAD) {
                 lse[i] = a.e.lse[m];
-                up[i] = a.e.dloss[m];
+                up[i] = SCALE ? a.e.dloss[m] / factor : a.e.dloss[m];      // (exact where they differ by a power of two)
             }
         }
         if (tid < BN) s_bias[tid] = a.e.bias && n0 + tid < a.N ? a.e.bias[a.e.col0 + n0 + tid] : 0.f;
@@ -786,7 +817,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
                 float t = s_sum[tid];
 #pragma unroll
                 for (int w = 1; w < WM; ++w) t += s_sum[w * BN + tid];
-                a.e.dbias_part[mt * a.e.lddb + n0 + tid] = t;
+                a.e.dbias_part[mt * a.e.lddb + n0 + tid] = t * factor;
             }
         }
     } else {
@@ -806,7 +837,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
             // the quad c of row r with what is added to it; `there` columns of it and more
             auto quad = [&](int r, int c, long at, int there, float* f) {
                 const float4 v = mine[r * Q + (c ^ (r & (Q - 1)))];
-                f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+                f[0] = v.x * factor; f[1] = v.y * factor; f[2] = v.z * factor; f[3] = v.w * factor;
                 if (a.e.acc) {
                     const any_u32x4 o = raw_load<float, 4>(a.e.acc + at, there);
 #pragma unroll
@@ -1167,6 +1198,7 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
             b.B = wo; b.ldb = p.Cp; b.bplane = p.wplane;
             b.M = R; b.N = D; b.K = n;
             b.e.acc = c > 0 ? acc : nullptr;
+            b.e.labels = labels; b.e.dloss = dloss; b.e.classes = V; b.e.rows = R;
             if (F32 || p.zdx > 1 || c + 1 < p.pieces) b.e.out_f32 = acc;
             else b.e.out = (bf16_t*)dx;
             TSM_TRY((x_product<XE_OUT, X_GROWS, X_COLS, F32>(p.sizedx, b, p.zdx, "xent_dx", s)));
@@ -1178,6 +1210,7 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
             b.B = xo; b.ldb = p.Cp; b.bplane = p.xplane;
             b.M = n; b.N = D; b.K = R;
             b.kmask = mask;
+            b.e.labels = labels; b.e.dloss = dloss; b.e.classes = V; b.e.rows = R;
             T* out = (T*)dw + v0 * D;
             if (F32 || p.zdw > 1) b.e.out_f32 = p.zdw > 1 ? dwp : (float*)out;
             else b.e.out = (bf16_t*)out;

@@ -233,3 +233,36 @@ def test_several_pieces_of_the_classes():
     for got, want, size in ((dx, s @ w, mag @ w.abs()), (dw, s.t() @ x, mag.t() @ x.abs())):
         want, size = want.double().cpu().numpy(), size.double().cpu().numpy()
         within(got.np(), want, (2.0 ** -8 + 1e-4) * size + 2.0 ** -8 * np.abs(want), "gradient")
+
+
+@pytest.mark.parametrize("shape", [(200, 64, 5000), (1100, 264, 5000), (40, 72, 3001)])
+def test_one_dloss_for_all_rows_does_not_shift_the_gradients(shape):
+    """dloss half way between two bf16 values, the same in all rows: the gradients' size, by projection on the exact ones, is right.
+    What is rounded is G without dloss's mantissa; rounded so in 64 bits it says where the size has to be: off by p of the labels, because
+    p - 1 rounds to -1 where p is below 2^-9 (p is 3e-4 on average at 3001 classes, and the 26 rows' own average, weighted by their
+    |x|^2, is what it is: 5e-4).  A rounding of a result is at most 2^-8 of it, up as often as down: the projection adds up n of them,
+    n = (sum want^2)^2 / sum want^4, to a standard deviation of at most 2^-8 / sqrt(n); four of them are allowed.  With dloss itself
+    rounded the size would be off by 2^-8."""
+    R, D, V = shape
+    labels = _labels(R, V, 9, False)
+    labels[::3] = -1                                # the first row among them
+    d = B.XentDesc(rows=R, features=D, classes=V, dtype=CDT["bf16"])
+    x, xn = values((R, D), 0, "bf16")
+    w, wn = values((V, D), 1, "bf16", scale=1 / np.sqrt(D))
+    lab, up = torch.from_numpy(labels).cuda(), torch.full((R,), (1 + 2.0 ** -8) / 256, device="cuda")
+    up[0] = 0.0
+    loss, lse = torch.empty(R, device="cuda"), torch.empty(R, device="cuda")
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(V, device="cuda")
+    ws = scratch(B.tsm_xent_workspace_bytes(d))
+    B.tsm_xent_fwd(d, x, w, None, lab, loss, lse, ws)
+    B.tsm_xent_bwd(d, x, w, None, lab, lse, up, dx, dw, db, ws)
+    upn = up.double().cpu().numpy()
+    rdx, rdw, rdb = H.xent_bwd(xn, wn, None, labels, upn)
+    G = H.xent_grad(xn, wn, None, labels, upn)
+    rounded = torch.from_numpy(G / (1 + 2.0 ** -8)).to(torch.bfloat16).double().numpy() * (1 + 2.0 ** -8)
+    for got, want, like, what in ((dx, rdx, rounded @ wn, "dx"), (dw, rdw, rounded.T @ xn, "dw"), (db, rdb, rdb, "dbias")):
+        want = want.ravel()
+        size, right = (v.ravel() @ want / (want @ want) - 1 for v in (got.double().cpu().numpy(), like))
+        n = (want @ want) ** 2 / (want ** 2 @ want ** 2)
+        assert abs(size - right) < 4 * 2.0 ** -8 / np.sqrt(n), (what, size, right, n)
+        assert abs(size) < 2.0 ** -10, (what, size)
