@@ -10,7 +10,7 @@
 // bf16: G, but for a factor (XScale), is rounded once, to the type of the matrix cores' operands; lse, the losses, db (from G before that rounding) and
 // all sums are fp32.  fp32: x, w and G are cut into three bf16 parts each, exactly (8 + 8 + 8 bits), and a product is the sum of the
 // six largest part products (the method of Henry, Tang and Heinecke, "Leveraging the bfloat16 artificial intelligence datatype for
-// higher-precision computations", 2019; what is left out is at most 2^-24 of it), one after the other along K, the small parts first.
+// higher-precision computations", 2019; what is left out is at most 2^-24 of it), the small ones first.
 #include <algorithm>
 #include <type_traits>
 #include "internal.h"
@@ -39,7 +39,7 @@ struct XentEpi {
     long lddb;
     uint64_t* mask;          // bit r % 64 of word r / 64: row r has a label; nullable
     // OUT: [M][N]
-    const float* acc;        // fp32, added to the result, nullable
+    const float* acc;        // fp32 [splits][M][N], added to the result, nullable
     float* out_f32;          // [splits][M][N], or
     bf16_t* out;
 };
@@ -204,6 +204,11 @@ struct XOperand {
         const bool in = k < left && (KC || (mask >> k) & 1);
         x_load_lds16(x_rsrc(base + more), stage + i * (NT * 16) + wave_u * 1024, in ? off[i] : X_OOB, 0);
     }
+    // Whole fp32: the q-th of a lane's four reads of four values, two of either slice of 16 values.
+    __device__ __forceinline__ static uint32_t whole_at(int row0, int q, int lane) {
+        const int r = lane & 31, hi = lane >> 5;
+        return (row0 + r) * PITCH + (((q / 2 * 4 + hi * 2 + q % 2) ^ kswz(r)) * 16);
+    }
     // Where a lane reads the fragment of the 32 rows from row0 (a multiple of 32), K consecutive: of slice ks, else of slice 0.
     __device__ __forceinline__ static uint32_t frag_at(int row0, int ks, int lane) {
         if constexpr (KC) {
@@ -366,6 +371,64 @@ __device__ __forceinline__ void read_parts(const uint32_t (&a)[2], uint32_t b, x
     }
 }
 
+// fp32 operands that lie in LDS as they are (WHOLE): eight consecutive K of a lane, cut into their three parts in registers.
+struct XCut {
+    x_bf16x8 part[3];
+    __device__ __forceinline__ explicit XCut(const float (&v)[8]) {
+        float f[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) f[t] = v[t];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            uint32_t w[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                // (a finite value that would round to infinity is cut off instead)
+                constexpr float MOST = 0x1.fep127f;
+                w[t] = k == 0 ? pack_bf16x2(__builtin_amdgcn_fmed3f(f[2 * t], -MOST, MOST), __builtin_amdgcn_fmed3f(f[2 * t + 1], -MOST, MOST))
+                              : pack_bf16x2(f[2 * t], f[2 * t + 1]);
+                if (k < 2) {
+                    f[2 * t] -= __uint_as_float(w[t] << 16);
+                    f[2 * t + 1] -= __uint_as_float(w[t] & 0xffff0000u);
+                }
+            }
+            part[k] = __builtin_bit_cast(x_bf16x8, any_u32x4{w[0], w[1], w[2], w[3]});
+        }
+    }
+    __device__ __forceinline__ static XCut of(const x_bf16x8& lo, const x_bf16x8& up) {     // (two reads of four values)
+        const any_f32x4 l = __builtin_bit_cast(any_f32x4, lo), u = __builtin_bit_cast(any_f32x4, up);
+        const float f[8] = {l[0], l[1], l[2], l[3], u[0], u[1], u[2], u[3]};
+        return XCut(f);
+    }
+};
+// A slice of G's parts, 4096 bytes apart, and of a whole fp32 operand whose rows, of 256 bytes, are K.
+template <int KS>
+__device__ __forceinline__ void read_whole(uint32_t a, const uint32_t (&b)[4], x_bf16x8 (&fa)[3], float (&fb)[8]) {
+    asm volatile("ds_read_b128 %0, %11\n ds_read_b32 %3, %12 offset:%16\n ds_read_b32 %4, %13 offset:%16\n ds_read_b32 %5, %14 offset:%16\n"
+                 "ds_read_b32 %6, %15 offset:%16\n ds_read_b128 %1, %11 offset:4096\n ds_read_b32 %7, %12 offset:%17\n ds_read_b32 %8, %13 offset:%17\n"
+                 "ds_read_b32 %9, %14 offset:%17\n ds_read_b32 %10, %15 offset:%17\n ds_read_b128 %2, %11 offset:8192\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(fa[0]), "=&v"(fa[1]), "=&v"(fa[2]), "=&v"(fb[0]), "=&v"(fb[1]), "=&v"(fb[2]), "=&v"(fb[3]), "=&v"(fb[4]), "=&v"(fb[5]),
+                   "=&v"(fb[6]), "=&v"(fb[7])
+                 : "v"(a), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "n"(KS * 4096), "n"(KS * 4096 + 1024) : "memory");
+}
+// (G through the transposing read, rows of 128 bytes)
+template <int KS>
+__device__ __forceinline__ void read_whole_tr(uint32_t a, const uint32_t (&b)[4], x_bf16x8 (&fa)[3], float (&fb)[8]) {
+    x_s16x4 l[3], u[3];
+    constexpr int OFF = KS * 2048;
+    asm volatile("ds_read_b64_tr_b16 %0, %14 offset:%21\n ds_read_b64_tr_b16 %1, %14 offset:%22\n ds_read_b32 %6, %15 offset:%19\n"
+                 "ds_read_b32 %7, %16 offset:%19\n ds_read_b32 %8, %17 offset:%19\n ds_read_b32 %9, %18 offset:%19\n"
+                 "ds_read_b64_tr_b16 %2, %14 offset:%23\n ds_read_b64_tr_b16 %3, %14 offset:%24\n ds_read_b32 %10, %15 offset:%20\n"
+                 "ds_read_b32 %11, %16 offset:%20\n ds_read_b32 %12, %17 offset:%20\n ds_read_b32 %13, %18 offset:%20\n"
+                 "ds_read_b64_tr_b16 %4, %14 offset:%25\n ds_read_b64_tr_b16 %5, %14 offset:%26\n s_waitcnt lgkmcnt(0)"
+                 : "=&v"(l[0]), "=&v"(u[0]), "=&v"(l[1]), "=&v"(u[1]), "=&v"(l[2]), "=&v"(u[2]), "=&v"(fb[0]), "=&v"(fb[1]), "=&v"(fb[2]), "=&v"(fb[3]),
+                   "=&v"(fb[4]), "=&v"(fb[5]), "=&v"(fb[6]), "=&v"(fb[7])
+                 : "v"(a), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "n"(KS * 4096), "n"(KS * 4096 + 1024), "n"(OFF), "n"(OFF + 512), "n"(OFF + 4096),
+                   "n"(OFF + 4608), "n"(OFF + 8192), "n"(OFF + 8704) : "memory");
+#pragma unroll
+    for (int k = 0; k < 3; ++k) fa[k] = x_join(l[k], u[k]);
+}
+
 // Two words that the two halves of a wavefront hold of adjacent column quads, x of quads 0 | 1, y of quads 2 | 3: afterwards the lower
 // half has quads 0, 1 and the upper half quads 2, 3.
 __device__ __forceinline__ void swap_halves(uint32_t& x, uint32_t& y) {
@@ -390,15 +453,25 @@ __device__ __forceinline__ float sum32(float v) {
 // The shapes of a tile.  Large: eight wavefronts of 128 x 64, one block per CU, for whatever fills the chip with it.  Middle: four of
 // 64 x 64, two blocks per CU.  Small: four of 32 x 32, two blocks per CU, loads three steps ahead.  Deep: a small one by four groups of
 // wavefronts that take every fourth step of K each and add their sums up at the end, for fewer tiles than CUs.  Parts: for operands in three
-// parts, all of which a stage holds, so that each is loaded once for the six products (the others take the pairs of parts one after
-// the other along K): eight wavefronts of 64 x 32, one block per CU.
+// parts, all of which a stage holds, so that each is loaded once for the six products: eight wavefronts of 64 x 32, one block per CU.
+// fp32 operands of small and deep tiles lie in LDS whole and are cut where they are multiplied, each value by two wavefronts: that
+// saves the pass that cuts them, for products that wait for memory and on one another's steps anyway (us of a training pass: 15 x 772 x 69968,
+// where that pass was most of it, 683 -> 310, 157 x 3377 x 285, whose steps are few now, 242 -> 152).
 struct XBig { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NS = 2, KG = 1, BK = 64, PARTS = 1; };
 struct XMid { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, NS = 2, KG = 1, BK = 64, PARTS = 1; };
 struct XSmall { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 4, KG = 1, BK = 64, PARTS = 1; };
 struct XDeep { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 2, KG = 4, BK = 64, PARTS = 1; };
 struct XParts { static constexpr int BM = 128, BN = 128, WM = 2, WN = 4, NS = 2, KG = 1, BK = 32, PARTS = 3; };
-template <typename C> constexpr int x_stage() { return (C::BM + C::BN) * C::BK * 2 * C::PARTS; }
-template <typename C> constexpr int x_smem() { return C::KG * C::NS * x_stage<C>() + C::WN * C::BM * 8 + C::BN * 4; }   // stages, row statistics, biases
+// What a stage holds of each operand: parts of K steps each.  WHOLE: fp32 as it is, which to its loads is twice as many bf16 along K, or,
+// of the operand whose rows are K (OUT's second), along its columns; G is in parts.
+template <typename C, int MODE, bool SPLIT>
+struct XStage {
+    static constexpr bool WHOLE = SPLIT && C::PARTS == 1, WOUT = WHOLE && MODE == XE_OUT;
+    static constexpr int BK = WOUT ? 32 : C::BK, APARTS = WOUT ? 3 : C::PARTS, BPARTS = C::PARTS, BROWS = WOUT ? 2 * C::BN : C::BN;
+    static constexpr int NS = WOUT ? 3 : C::NS;
+    static constexpr int BYTES = (C::BM * APARTS + BROWS * BPARTS) * BK * 2;
+    static constexpr int SMEM = C::KG * NS * BYTES + C::WN * C::BM * 8 + C::BN * 4;       // stages, row statistics, biases
+};
 static constexpr int X_LAUNCH = 1 << 22;   // blocks of one launch, at most
 
 // SPLIT: operands in three parts.  DB: the column sums of G are wanted.
@@ -407,13 +480,14 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     constexpr int BM = C::BM, BN = C::BN, WM = C::WM, WN = C::WN, NT = WM * WN * 64, MI = BM / (WM * 32), NJ = BN / (WN * 32);
     constexpr bool BIG = NJ == 2;
     static_assert((BIG && (MI == 4 || MI == 2)) || (MI == 1 && NJ == 1 && BN == 64) || (C::PARTS == 3 && MI == 2 && NJ == 1 && SPLIT), "read_frags, read_step, read_parts");
-    constexpr int TM = BM / WM, TN = BN / WN, NS = C::NS, KG = C::KG, STAGE = x_stage<C>();
+    typedef XStage<C, MODE, SPLIT> S;
+    constexpr int TM = BM / WM, TN = BN / WN, NS = S::NS, KG = C::KG, STAGE = S::BYTES;
     static_assert(KG == 1 || (AKIND == X_ROWS && BKIND == X_ROWS), "groups skip steps");
-    constexpr int BK = C::BK, PARTS = C::PARTS;
-    constexpr bool PAIRS = SPLIT && PARTS == 1;                 // the parts one pair after the other
+    constexpr int BK = S::BK, PARTS = C::PARTS;
+    constexpr bool WHOLE = S::WHOLE, WOUT = S::WOUT;
     typedef XOperand<BM, AKIND, NT, BK> OpA;
-    typedef XOperand<BN, BKIND, NT, BK> OpB;
-    constexpr int NP = (OpA::PIECES + OpB::PIECES) * PARTS;
+    typedef XOperand<S::BROWS, BKIND, NT, BK> OpB;
+    constexpr int NP = OpA::PIECES * S::APARTS + OpB::PIECES * S::BPARTS;
     constexpr float L2E = 1.44269502f;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     float2* s_part = (float2*)(smem + KG * NS * STAGE);         // [WN][BM]; the column sums of G as floats [WM][BN]
@@ -436,10 +510,10 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     const long mt = band * BAND + rest % high, nt = rest / high;
     const long m0 = mt * BM, n0 = nt * BN;
     const long kb = z * a.ksplit, ke = kb + a.ksplit < a.K ? kb + a.ksplit : a.K;
-    const int ksteps = ke > kb ? (int)((ke - kb + BK - 1) / BK) : 0, steps = ksteps * (PAIRS ? 6 : 1);
+    const int steps = ke > kb ? (int)((ke - kb + BK - 1) / BK) : 0;
     OpA pa;
     OpB pb;
-    int kc = 0, pair = 0;                                       // of the step at the operands' windows
+    int kc = 0;                                                 // the step at the operands' windows
     auto load_step = [&](int stage) {
         unsigned char* st = smem + (group * NS + stage) * STAGE;
         const long l = ke - kb - (long)kc * BK;
@@ -450,31 +524,21 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
             mask = ((const __attribute__((address_space(4))) uint64_t*)a.kmask)[k / 64] >> (BK < 64 ? k % 64 : 0);
         }
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
+        for (int part = 0; part < S::APARTS; ++part) {
 #pragma unroll
             for (int q = 0; q < OpA::PIECES; ++q) pa.load(st + part * OpA::BYTES, q, left, ~0ull, wave_u, part * a.aplane * 2);
+            if (part < S::BPARTS)
 #pragma unroll
-            for (int q = 0; q < OpB::PIECES; ++q) pb.load(st + PARTS * OpA::BYTES + part * OpB::BYTES, q, left, mask, wave_u, part * a.bplane * 2);
+                for (int q = 0; q < OpB::PIECES; ++q) pb.load(st + S::APARTS * OpA::BYTES + part * OpB::BYTES, q, left, mask, wave_u, part * a.bplane * 2);
         }
     };
     auto next_step = [&](int stage) {
         if constexpr (KG > 1) {                                 // this group's next step: KG further on
-            for (kc += KG; PAIRS && kc >= ksteps;) {
-                kc -= ksteps;
-                ++pair;
-            }
-            pa.restart((PAIRS ? a.aplane * ((0x001102 >> (4 * pair)) & 3) : 0) + (long)kc * BK);
-            pb.restart((PAIRS ? a.bplane * ((0x010120 >> (4 * pair)) & 3) : 0) + (long)kc * BK);
-            load_step(stage);
-            return;
-        }
-        ++kc;
-        if (PAIRS && kc == ksteps) {                            // the next pair of parts: 2 0, 0 2, 1 1, 1 0, 0 1, 0 0
-            kc = 0;
-            ++pair;
-            pa.restart(a.aplane * ((0x001102 >> (4 * pair)) & 3));
-            pb.restart(a.bplane * ((0x010120 >> (4 * pair)) & 3));
+            kc += KG;
+            pa.restart((long)kc * BK);
+            pb.restart((long)kc * BK);
         } else {
+            ++kc;
             pa.advance();
             pb.advance();
         }
@@ -486,7 +550,19 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         if (OpA::KC ? q < BK / 16 : q < MI) aat[q] = lds0 + (OpA::KC ? OpA::frag_at(wm * TM, q, lane) : OpA::frag_at(wm * TM + q * 32, 0, lane));
-        if (OpB::KC ? q < BK / 16 : q < NJ) bat[q] = lds0 + PARTS * OpA::BYTES + (OpB::KC ? OpB::frag_at(wn * TN, q, lane) : OpB::frag_at(wn * TN + q * 32, 0, lane));
+        if (OpB::KC ? q < BK / 16 : q < NJ) bat[q] = lds0 + S::APARTS * OpA::BYTES + (OpB::KC ? OpB::frag_at(wn * TN, q, lane) : OpB::frag_at(wn * TN + q * 32, 0, lane));
+    }
+    if constexpr (WHOLE) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (OpA::KC && OpB::KC) {                           // two reads of four values per slice
+                aat[q] = lds0 + OpA::whole_at(wm * TM, q, lane);
+                bat[q] = lds0 + OpA::BYTES + OpB::whole_at(wn * TN, q, lane);
+            } else {                                            // rows 8 hi + q of the lane's column
+                const int k = 8 * hi + q, n = wn * TN + lo;
+                bat[q] = lds0 + S::APARTS * OpA::BYTES + k * OpB::PITCH + ((n / 8) ^ OpB::swz(k)) * 32 + n % 8 * 4;
+            }
+        }
     }
     x_f32x16 acc[MI][NJ];
 #pragma unroll
@@ -501,10 +577,14 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     if constexpr (SCALE && MODE == XE_OUT) scale.load(a.e, a.e.rows);      // (awaited behind the first steps' loads)
     if (steps > 0) {
         pa.init(a.A, a.lda, m0, a.M, kb, tid);
-        pb.init(a.B, a.ldb, n0, a.N, kb, tid);
-        if constexpr (PAIRS) pa.restart(a.aplane * 2);
+        pb.init(a.B, a.ldb, WOUT ? 2 * n0 : n0, WOUT ? 2 * a.N : a.N, kb, tid);
         if constexpr (KG == 1) load_step(0);
     }
+    constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};      // of three parts, the small products first
+    auto multiply_parts = [&](const x_bf16x8 (&fa)[3], const x_bf16x8 (&fb)[3]) {
+#pragma unroll
+        for (int k = 0; k < 6; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[PB[k]], fa[PA[k]], acc[0][0], 0, 0, 0);
+    };
     if constexpr (BIG) {
         x_bf16x8 af[2][MI], bf[2][NJ];
         auto read = [&](auto slice, int stage) {
@@ -579,8 +659,13 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
                 const uint32_t so = (group * NS + stage) * STAGE;
                 const uint32_t q[4] = {aat[0] + so, aat[1] + so, aat[2] + so, aat[3] + so}, b[4] = {bat[0] + so, bat[1] + so, bat[2] + so, bat[3] + so};
                 read_step(q, b, fa, fb);
+                if constexpr (WHOLE) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k], fa[k], acc[0][0], 0, 0, 0);
+                    for (int ks = 0; ks < 2; ++ks) multiply_parts(XCut::of(fa[2 * ks], fa[2 * ks + 1]).part, XCut::of(fb[2 * ks], fb[2 * ks + 1]).part);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k], fa[k], acc[0][0], 0, 0, 0);
+                }
             }
         }
         x_wait<0>();
@@ -621,7 +706,6 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
                     read_parts<OFF>(q, bat[0] + so, fa, fb);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};      // the small products first
 #pragma unroll
                 for (int k = 0; k < 6; ++k)
 #pragma unroll
@@ -635,7 +719,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
         // One barrier per step: in front of it every wavefront waits for its loads of this step, behind it the stage of the step
         // before is free.
         if (steps > 1) next_step(1);
-        if (steps > 2) next_step(2);
+        if (NS > 3 && steps > 2) next_step(2);
         if constexpr (SCALE && MODE == XE_OUT) factor = scale.get();
         int stage = 0;
         for (int s = 0; s < steps; ++s) {
@@ -643,15 +727,34 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
             else x_wait<0>();
             x_barrier();
             if (s + NS - 1 < steps) next_step(stage == 0 ? NS - 1 : stage - 1);
-            x_bf16x8 fa[4], fb[4];
             const uint32_t so = stage * STAGE;
-            const uint32_t q[4] = {aat[0] + so, aat[OpA::KC ? 1 : 0] + so, aat[OpA::KC ? 2 : 0] + so, aat[OpA::KC ? 3 : 0] + so};
-            const uint32_t b[4] = {bat[0] + so, bat[OpB::KC ? 1 : 0] + so, bat[OpB::KC ? 2 : 0] + so, bat[OpB::KC ? 3 : 0] + so};
-            if constexpr (OpA::KC && OpB::KC) read_step(q, b, fa, fb);
-            else if constexpr (OpA::KC) read_step(q, b[0], fa, fb);
-            else read_step(q[0], b[0], fa, fb);
+            if constexpr (WOUT) {
+                const uint32_t b[4] = {bat[0] + so, bat[1] + so, bat[2] + so, bat[3] + so};
+                auto slice = [&](auto number) {
+                    constexpr int ks = decltype(number)::value;
+                    x_bf16x8 fa[3];
+                    float fb[8];
+                    if constexpr (OpA::KC) read_whole<ks>(aat[ks] + so, b, fa, fb);
+                    else read_whole_tr<ks>(aat[0] + so, b, fa, fb);
+                    multiply_parts(fa, XCut(fb).part);
+                };
+                slice(std::integral_constant<int, 0>{});
+                slice(std::integral_constant<int, 1>{});
+            } else {
+                x_bf16x8 fa[4], fb[4];
+                const uint32_t q[4] = {aat[0] + so, aat[OpA::KC ? 1 : 0] + so, aat[OpA::KC ? 2 : 0] + so, aat[OpA::KC ? 3 : 0] + so};
+                const uint32_t b[4] = {bat[0] + so, bat[OpB::KC ? 1 : 0] + so, bat[OpB::KC ? 2 : 0] + so, bat[OpB::KC ? 3 : 0] + so};
+                if constexpr (OpA::KC && OpB::KC) read_step(q, b, fa, fb);
+                else if constexpr (OpA::KC) read_step(q, b[0], fa, fb);
+                else read_step(q[0], b[0], fa, fb);
+                if constexpr (WHOLE) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k], fa[k], acc[0][0], 0, 0, 0);
+                    for (int ks = 0; ks < 2; ++ks) multiply_parts(XCut::of(fa[2 * ks], fa[2 * ks + 1]).part, XCut::of(fb[2 * ks], fb[2 * ks + 1]).part);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k], fa[k], acc[0][0], 0, 0, 0);
+                }
+            }
             stage = stage + 1 == NS ? 0 : stage + 1;
         }
     }
@@ -839,7 +942,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
                 const float4 v = mine[r * Q + (c ^ (r & (Q - 1)))];
                 f[0] = v.x * factor; f[1] = v.y * factor; f[2] = v.z * factor; f[3] = v.w * factor;
                 if (a.e.acc) {
-                    const any_u32x4 o = raw_load<float, 4>(a.e.acc + at, there);
+                    const any_u32x4 o = raw_load<float, 4>(a.e.acc + z * a.M * a.N + at, there);
 #pragma unroll
                     for (int t = 0; t < 4; ++t) f[t] += raw_get<float>(o, t);
                 }
@@ -869,6 +972,19 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
                 }
             }
         }
+    }
+}
+
+// Rows of C fp32 values as rows of Cp, zero behind the C-th.  Two tensors in a launch.
+__global__ void __launch_bounds__(256) xent_pad_kernel(const float* __restrict__ in0, long rows0, float* __restrict__ out0, const float* __restrict__ in1,
+                                                       long rows1, float* __restrict__ out1, int C, int Cp) {
+    const long quads = (rows0 + rows1) * (Cp / 4);
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < quads; i += (long)gridDim.x * 256) {
+        const long row = i / (Cp / 4);
+        const int c = (int)(i % (Cp / 4)) * 4;
+        const bool second = row >= rows0;
+        const long r = second ? row - rows0 : row;
+        *(any_u32x4*)((second ? out1 : out0) + r * Cp + c) = raw_load<float, 4>((second ? in1 : in0) + r * C + c, C - c);
     }
 }
 
@@ -983,7 +1099,9 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float* __restrict_
 struct XentPlan {
     long piece, pieces;           // classes of a piece of G, number of pieces
     long Cp;                      // row pitch of x and w as operands
+    bool whole;                   // fp32 operands as they are (small tiles only)
     bool cut;                     // x and w are made into operands in the workspace
+    long pitch, depth;            // as the tiles see them: from row to row of x and w, features
     int size;                     // the tiles of s
     int sizedx, sizedw;           // of the two products that read G
     int zdx, zdw;                 // their splits of K
@@ -1011,8 +1129,8 @@ static int x_splits(int size, long M, long N, long K, bool parts) {
 
 // The largest tiles that fill half the chip, K split (split) or not, and are not more than half empty where the matrix is narrow.
 // us of the products with small, middle, large tiles: statistics of 1777 x 1000 x 32003 244, 150, 144, of 4 x 2048 x 65536 (w read from HBM)
-// 61, 69, 75, of 64 x 2048 x 400 17, 28, 50; dx of the first 231, 131 + 11, 110 + 18.  fp32, 2048 x 1024 x 10000: large tiles that took
-// the pairs of parts one after the other 288, middle ones that take them together 222.
+// 61, 69, 75, of 64 x 2048 x 400 17, 28, 50; dx of the first 231, 131 + 11, 110 + 18.  fp32, 2048 x 1024 x 10000: large tiles, with the
+// pairs of parts one after the other along K, 288, middle ones that take them together 222.
 static int x_size(long M, long N, long K, bool split, bool parts) {
     const long narrow = M < N ? M : N;
     for (int size = narrow > 128 && !parts ? X_BIG : narrow > 64 ? X_MID : X_SMALL; size > X_SMALL; --size)
@@ -1024,8 +1142,6 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     XentPlan p{};
     const long R = d->rows, D = d->features, V = d->classes;
     const int parts = d->dtype == TSM_F32 ? 3 : 1;
-    p.cut = parts > 1 || D % 8 != 0;
-    p.Cp = (D + 7) / 8 * 8;
     long piece = (long)(XENT_G_BYTES / (2 * parts)) / R / 1024 * 1024;
     if (piece < 1024) piece = 1024;
     if (piece > V) piece = V;
@@ -1033,6 +1149,12 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     p.pieces = (V + piece - 1) / piece;
     const bool f32 = parts == 3;
     p.size = x_size(R, piece, D, false, f32);
+    p.whole = f32 && p.size == X_SMALL;
+    p.cut = p.whole ? D % 4 != 0 : f32 || D % 8 != 0;
+    p.Cp = p.whole ? (D + 3) / 4 * 4 : (D + 7) / 8 * 8;
+    p.pitch = p.whole ? 2 * p.Cp : p.Cp;
+    p.depth = p.whole ? 2 * p.Cp : D;
+    const int copies = p.whole ? 2 : parts;                     // of two bytes
     const long t = x_tile(p.size);
     p.ntiles = (p.pieces - 1) * ((piece + t - 1) / t) + (V - (p.pieces - 1) * piece + t - 1) / t;
     p.mtiles = (R + t - 1) / t;
@@ -1042,15 +1164,17 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     p.gplane = (R + X_GTILE - 1) / X_GTILE * p.ldg;
     p.lddb = (piece + 7) / 8 * 8;
     Arena f(nullptr, 0);
-    p.o_x = f.used; f.take(p.cut ? (size_t)parts * p.xplane * 2 : 0);
-    p.o_w = f.used; f.take(p.cut ? (size_t)parts * p.wplane * 2 : 0);
+    p.o_x = f.used; f.take(p.cut ? (size_t)copies * p.xplane * 2 : 0);
+    p.o_w = f.used; f.take(p.cut ? (size_t)copies * p.wplane * 2 : 0);
     Arena b = f;
     p.o_part = f.used; f.take((size_t)p.ntiles * R * 8);
     p.o_picked = f.used; f.take((size_t)R * 4);
     p.fwd_bytes = f.used;
-    p.sizedx = x_size(R, D, V, p.pieces == 1, f32);
-    p.zdx = p.pieces > 1 ? 1 : x_splits(p.sizedx, R, D, V, f32);
-    p.sizedw = x_size(piece, D, R, true, f32);
+    // (where s has larger tiles, its operands are in parts, and a whole one is the caller's own)
+    const int least = f32 && !p.whole && D % 4 != 0 ? X_MID : X_SMALL;
+    p.sizedx = p.whole ? X_SMALL : std::max(least, x_size(R, D, piece, true, f32));
+    p.zdx = x_splits(p.sizedx, R, D, piece, f32);
+    p.sizedw = p.whole ? X_SMALL : std::max(least, x_size(piece, D, R, true, f32));
     p.zdw = x_splits(p.sizedw, piece, D, R, f32);
     p.o_G = b.used; b.take((size_t)parts * p.gplane * 2);
     p.o_acc = b.used; b.take((parts == 1 && p.pieces > 1) || p.zdx > 1 ? (size_t)p.zdx * R * D * 4 : 0);
@@ -1085,7 +1209,7 @@ static int x_launch(XentArgs a, int splits, const char* what, hipStream_t s) {
     a.ksplit = ((a.K + splits - 1) / splits + 63) / 64 * 64;
     for (a.job0 = 0; a.job0 < jobs; a.job0 += X_LAUNCH) {
         const long n = jobs - a.job0;
-        kernel<<<dim3((unsigned)(n < X_LAUNCH ? n : X_LAUNCH)), dim3(C::WM * C::WN * C::KG * 64), x_smem<C>(), s>>>(a);
+        kernel<<<dim3((unsigned)(n < X_LAUNCH ? n : X_LAUNCH)), dim3(C::WM * C::WN * C::KG * 64), XStage<C, MODE, SPLIT>::SMEM, s>>>(a);
         TSM_TRY(check_launch(what));
     }
     return TSM_OK;
@@ -1100,7 +1224,7 @@ static int x_product(int size, const XentArgs& a, int splits, const char* what, 
         if (size == X_MID) return x_launch<XMid, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     }
     if constexpr (MODE != XE_OUT)      // (us at 64 x 2048 x 400: 14.2 with small tiles, 10.3 with deep ones)
-        if (x_tiles(a.M, a.N, 64) <= 256 && a.K * (SPLIT ? 6 : 1) >= 512) return x_launch<XDeep, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+        if (x_tiles(a.M, a.N, 64) <= 256 && a.K >= 512) return x_launch<XDeep, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     return x_launch<XSmall, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
 }
 
@@ -1121,6 +1245,12 @@ static int x_operands(const XentPlan& p, const void* x, long R, const void* w, l
     *xo = (const bf16_t*)(ws + p.o_x);
     *wo = (const bf16_t*)(ws + p.o_w);
     const long rows = first ? R : 0, blocks = ((rows + n) * (p.Cp / 8) + 255) / 256;
+    if (sizeof(T) == 4 && p.whole) {
+        const long quads = (rows + n) * (p.Cp / 4);
+        xent_pad_kernel<<<dim3((unsigned)std::min((quads + 255) / 256, 8192L)), dim3(256), 0, s>>>((const float*)x, rows, (float*)(ws + p.o_x), (const float*)w, n,
+                                                                                                   (float*)(ws + p.o_w), C, (int)p.Cp);
+        return check_launch("xent_pad");
+    }
     xent_parts_kernel<T, sizeof(T) == 2 ? 1 : 3><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, s>>>(
         (const T*)x, rows, (bf16_t*)(ws + p.o_x), p.xplane, (const T*)w, n, (bf16_t*)(ws + p.o_w), p.wplane, C, (int)p.Cp);
     return check_launch("xent_parts");
@@ -1132,8 +1262,8 @@ static int xent_fwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
     constexpr bool F32 = sizeof(T) == 4;
     const long D = d->features, V = d->classes;
     XentArgs a{};
-    a.lda = a.ldb = p.Cp;
-    a.K = D;
+    a.lda = a.ldb = p.pitch;
+    a.K = p.depth;
     a.M = d->rows;
     a.aplane = p.xplane;
     a.bplane = p.wplane;
@@ -1174,9 +1304,9 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
         TSM_TRY(x_operands<T>(p, x, R, (const T*)w + v0 * D, n, (int)D, ws, c == 0, &xo, &wo, s));
         XentArgs a{};
         a.A = xo; a.B = wo;
-        a.lda = a.ldb = p.Cp;
+        a.lda = a.ldb = p.pitch;
         a.aplane = p.xplane; a.bplane = p.wplane;
-        a.M = R; a.N = n; a.K = D;
+        a.M = R; a.N = n; a.K = p.depth;
         a.e.bias = bias; a.e.labels = labels; a.e.classes = V; a.e.col0 = v0;
         a.e.lse = lse; a.e.dloss = dloss; a.e.G = G; a.e.ldg = p.ldg; a.e.gplane = p.gplane;
         a.e.mask = dw && c == 0 ? mask : nullptr;
@@ -1195,19 +1325,27 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
         if (dx) {
             XentArgs b{};
             b.A = G; b.lda = p.ldg; b.aplane = p.gplane;
-            b.B = wo; b.ldb = p.Cp; b.bplane = p.wplane;
+            b.B = wo; b.ldb = p.pitch; b.bplane = p.wplane;
+            if (F32 && p.sizedx == X_SMALL && !p.whole) {
+                b.B = (const bf16_t*)((const T*)w + v0 * D);
+                b.ldb = 2 * D;
+            }
             b.M = R; b.N = D; b.K = n;
             b.e.acc = c > 0 ? acc : nullptr;
             b.e.labels = labels; b.e.dloss = dloss; b.e.classes = V; b.e.rows = R;
             if (F32 || p.zdx > 1 || c + 1 < p.pieces) b.e.out_f32 = acc;
             else b.e.out = (bf16_t*)dx;
             TSM_TRY((x_product<XE_OUT, X_GROWS, X_COLS, F32>(p.sizedx, b, p.zdx, "xent_dx", s)));
-            if (p.zdx > 1) TSM_TRY(xent_join<T>(acc, p.zdx, R * D, dx, "xent_dx_join", s));
+            if (p.zdx > 1 && c + 1 == p.pieces) TSM_TRY(xent_join<T>(acc, p.zdx, R * D, dx, "xent_dx_join", s));      // (each has added up its pieces)
         }
         if (dw) {
             XentArgs b{};
             b.A = G; b.lda = p.ldg; b.aplane = p.gplane;
-            b.B = xo; b.ldb = p.Cp; b.bplane = p.xplane;
+            b.B = xo; b.ldb = p.pitch; b.bplane = p.xplane;
+            if (F32 && p.sizedw == X_SMALL && !p.whole) {
+                b.B = (const bf16_t*)x;
+                b.ldb = 2 * D;
+            }
             b.M = n; b.N = D; b.K = R;
             b.kmask = mask;
             b.e.labels = labels; b.e.dloss = dloss; b.e.classes = V; b.e.rows = R;

@@ -266,3 +266,38 @@ def test_one_dloss_for_all_rows_does_not_shift_the_gradients(shape):
         n = (want @ want) ** 2 / (want ** 2 @ want ** 2)
         assert abs(size - right) < 4 * 2.0 ** -8 / np.sqrt(n), (what, size, right, n)
         assert abs(size) < 2.0 ** -10, (what, size)
+
+
+@pytest.mark.parametrize("dtype,R,D,V", [("f32", 64, 8, 1500000), ("f32", 64, 6, 1500000), ("f32", 900, 72, 110000), ("f32", 900, 33, 110000),
+                                         ("bf16", 2600, 40, 110000), ("bf16", 1500, 260, 190000)])
+def test_pieces_of_very_many_classes(dtype, R, D, V):
+    """Few rows, past the classes of one piece of G: fp32 operands of small tiles, as they are and padded, and gradients of the rows whose
+    splits add up over the pieces.  The reference is on the GPU, in 64 bits.  Logits are below 30: 1e-5 covers 40 roundings of them, an
+    entry of G is 3e-5 of itself off, and a rounding to bf16; above: a sum of n terms in fp32 by (4 sqrt(n) + 16) units of the sum of
+    their sizes, which is 2.9e-4 of it for 1.5 million."""
+    d = B.XentDesc(rows=R, features=D, classes=V, dtype=CDT[dtype])
+    x, _ = values((R, D), 0, dtype)
+    w, _ = values((V, D), 1, dtype, scale=1.4 / np.sqrt(D))
+    b, _ = values((V,), 2, "f32")
+    lab = (torch.arange(R, device="cuda", dtype=torch.int64) * 23701 % V).int()
+    lab[5], lab[40] = V, -1
+    up, _ = values((R,), 3, "f32")
+    ws = scratch(B.tsm_xent_workspace_bytes(d))
+    loss, lse, dx, dw, db = (Guarded(s, t) for s, t in (((R,), torch.float32), ((R,), torch.float32), ((R, D), TDT[dtype]), ((V, D), TDT[dtype]), ((V,), torch.float32)))
+    B.tsm_xent_fwd(d, x, w, b, lab, loss.t, lse.t, ws)
+    B.tsm_xent_bwd(d, x, w, b, lab, lse.t, up, dx.t, dw.t, db.t, ws)
+    G = x.double() @ w.double().t() + b.double()
+    rlse = torch.logsumexp(G, 1)
+    ok = (lab >= 0) & (lab < V)
+    at, rows = torch.where(ok, lab, torch.zeros_like(lab)).long(), torch.arange(R, device="cuda")
+    within(lse.np(), rlse.cpu().numpy(), 1e-5, "lse")
+    within(loss.np(), torch.where(ok, rlse - G[rows, at], torch.zeros_like(rlse)).cpu().numpy(), 2e-5, "loss")
+    G.sub_(rlse[:, None]).exp_()
+    G[rows, at] -= 1
+    G.mul_(torch.where(ok, up, torch.zeros_like(up)).double()[:, None])
+    mag, half = G.abs(), HALF[dtype]
+    entry = 3e-5 + (half if dtype == "bf16" else 0)
+    for got, want, size, n in ((dx, G @ w.double(), mag @ w.double().abs(), V), (dw, G.t() @ x.double(), mag.t() @ x.double().abs(), R)):
+        want, size = want.cpu().numpy(), size.cpu().numpy()
+        within(got.np(), want, (entry + (4 * np.sqrt(n) + 16) * U) * size + half * np.abs(want) + 1e-30, "gradient")
+    within(db.np(), G.sum(0).cpu().numpy(), 5e-5 * mag.sum(0).cpu().numpy() + 1e-30, "dbias")
