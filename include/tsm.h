@@ -378,7 +378,8 @@ int tsm_resnet50_infer(const tsm_r50_desc* d, const void* clips, const float* pa
  * be h0: a stream's state, carried in place from call to call (T = 1: one new frame).
  * saved: caller-owned buffer of tsm_recur_saved_bytes(desc) bytes (0 up to 128 frames) in which the forward pass keeps
  * what the backward pass needs; NULL in the forward pass where none follows.  The backward pass takes the h0 that the
- * forward pass read.  Workspace: tsm_recur_workspace_bytes(desc), 0 for most shapes; NULL is accepted then.
+ * forward pass read.  Workspace: tsm_recur_workspace_bytes(desc), 0 for most shapes; NULL is accepted then.  Its
+ * contents do not matter, but one call at a time may use it: blocks of a call meet there.
  * Steps are joined as affine maps, in a fixed order.  Once a state of a column is infinite its later states are
  * infinite or NaN, which of the two depends on how its steps were joined.  No output may overlap an input or another
  * output (h_last == h0 aside): TSM_ERR_SHAPE.
@@ -429,7 +430,8 @@ int tsm_layernorm_bwd(const tsm_layernorm_desc* d, const void* x, const void* dy
  * loss, lse: fp32 [rows], per row; the mean of a batch is the caller's (dloss[r] = 1 / number of rows with a label).
  * dx, dw: the types of x and w, overwritten; dbias fp32; each may be NULL where it is not wanted, not all of them.
  * The backward pass forms the logits again, in pieces of the classes; lse is the forward pass's.  In TSM_BF16 the
- * entries of G are rounded to bf16 for the two products (dbias is summed before that), everything else is fp32.  In
+ * entries of G, without the mantissa that the dloss of all rows may share, are rounded to bf16 for the two products
+ * (dbias is summed before that), everything else is fp32.  In
  * TSM_F32 a product is the sum of six products of bf16 parts, good to 2^-24 of it for operands of 2^-110 and more; an
  * infinite operand makes the sums it enters NaN.
  * Logits of minus infinity (a bias that takes a class out) are classes without weight; where no class of a row is left
