@@ -1105,7 +1105,7 @@ struct XentPlan {
     int size;                     // the tiles of s
     int sizedx, sizedw;           // of the two products that read G
     int zdx, zdw;                 // their splits of K
-    long ntiles, mtiles;          // tiles of s: of all columns, of the rows
+    long ntiles, mtiles;          // tiles of s: of all columns, of the rows, at most
     long ldg, gplane, xplane, wplane, lddb;
     size_t fwd_bytes, bwd_bytes;
     size_t o_x, o_w, o_part, o_picked, o_G, o_acc, o_dw, o_dbias, o_mask;
@@ -1138,6 +1138,25 @@ static int x_size(long M, long N, long K, bool split, bool parts) {
     return X_SMALL;
 }
 
+// The columns of s that fill whole rounds of tiles, and the tiles of the rest: where the last round would be at most half full, smaller
+// ones that need one round of their own.  (A round of large, middle, small tiles at 1000 features: 36, 21, 9 us; in fp32 at 1024 41 for the
+// middle ones, 18 for deep ones.)
+struct XRest {
+    long columns;
+    int size;
+};
+static XRest x_rest(const XentPlan& p, long M, long N, long D, bool f32) {
+    const long t = x_tile(p.size), room = x_room(p.size, f32), mt = (M + t - 1) / t, whole = x_tiles(M, N, (int)t) / room * room / mt * t;
+    if (whole > 0 && whole < N && D >= 512 && !(f32 && D % 4 != 0))
+        for (int size = X_SMALL; size < p.size; ++size)
+            if (x_tiles(M, N - whole, x_tile(size)) <= (f32 ? 256 : 512)) return {whole, size};
+    return {N, p.size};
+}
+static long x_column_tiles(const XentPlan& p, long M, long N, long D, bool f32) {
+    const XRest r = x_rest(p, M, N, D, f32);
+    return (r.columns + x_tile(p.size) - 1) / x_tile(p.size) + (N - r.columns + x_tile(r.size) - 1) / x_tile(r.size);
+}
+
 static XentPlan xent_plan(const tsm_xent_desc* d) {
     XentPlan p{};
     const long R = d->rows, D = d->features, V = d->classes;
@@ -1156,8 +1175,10 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     p.depth = p.whole ? 2 * p.Cp : D;
     const int copies = p.whole ? 2 : parts;                     // of two bytes
     const long t = x_tile(p.size);
-    p.ntiles = (p.pieces - 1) * ((piece + t - 1) / t) + (V - (p.pieces - 1) * piece + t - 1) / t;
+    const long last = V - (p.pieces - 1) * piece;
+    p.ntiles = p.cut ? (p.pieces - 1) * x_column_tiles(p, R, piece, D, f32) + x_column_tiles(p, R, last, D, f32) : x_column_tiles(p, R, V, D, f32);
     p.mtiles = (R + t - 1) / t;
+    for (const long n : {piece, last}) p.mtiles = std::max(p.mtiles, (R + x_tile(x_rest(p, R, n, D, f32).size) - 1) / x_tile(x_rest(p, R, n, D, f32).size));
     p.xplane = R * p.Cp;
     p.wplane = piece * p.Cp;
     p.ldg = (piece + t - 1) / t * t * X_GTILE;
@@ -1256,6 +1277,19 @@ static int x_operands(const XentPlan& p, const void* x, long R, const void* w, l
     return check_launch("xent_parts");
 }
 
+// The same for columns `from` to n of a piece; whole fp32 operands are the caller's own.
+template <typename T>
+static void x_columns(const XentPlan& p, XentArgs& a, long from, long n, const void* x, const T* w, long D) {
+    a.N = n - from;
+    a.e.col0 += from;
+    a.B += from * p.pitch;
+    if (sizeof(T) == 4) {
+        a.A = (const bf16_t*)x;
+        a.B = (const bf16_t*)(w + from * D);
+        a.lda = a.ldb = a.K = 2 * D;
+    }
+}
+
 template <typename T>
 static int xent_fwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, const void* w, const float* bias, const int32_t* labels, float* loss,
                     float* lse, char* ws, hipStream_t s) {
@@ -1270,15 +1304,24 @@ static int xent_fwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
     a.e.picked = (float*)(ws + p.o_picked);
     a.e.bias = bias; a.e.labels = labels; a.e.classes = V;
     // (nothing of the pieces' size but the operands of w: where the caller's own serve, the classes go in one piece)
-    const long piece = p.cut ? p.piece : V, t = x_tile(p.size);
+    const long piece = p.cut ? p.piece : V;
     long tiles = 0;
     for (long v0 = 0; v0 < V; v0 += piece) {
-        a.N = V - v0 < piece ? V - v0 : piece;
-        a.e.col0 = v0;
-        a.e.part = (float2*)(ws + p.o_part) + tiles * a.M;
-        TSM_TRY(x_operands<T>(p, x, a.M, (const T*)w + v0 * D, a.N, (int)D, ws, v0 == 0, &a.A, &a.B, s));
-        TSM_TRY((x_product<XE_STATS, X_ROWS, X_ROWS, F32>(p.size, a, 1, "xent_stats", s)));
-        tiles += (a.N + t - 1) / t;
+        const long n = V - v0 < piece ? V - v0 : piece;
+        TSM_TRY(x_operands<T>(p, x, a.M, (const T*)w + v0 * D, n, (int)D, ws, v0 == 0, &a.A, &a.B, s));
+        const XRest rest = x_rest(p, a.M, n, D, F32);
+        XentArgs b = a;
+        b.N = rest.columns;
+        b.e.col0 = v0;
+        b.e.part = (float2*)(ws + p.o_part) + tiles * a.M;
+        TSM_TRY((x_product<XE_STATS, X_ROWS, X_ROWS, F32>(p.size, b, 1, "xent_stats", s)));
+        tiles += (b.N + x_tile(p.size) - 1) / x_tile(p.size);
+        if (b.N < n) {
+            x_columns<T>(p, b, b.N, n, x, (const T*)w + v0 * D, D);
+            b.e.part = (float2*)(ws + p.o_part) + tiles * a.M;
+            TSM_TRY((x_product<XE_STATS, X_ROWS, X_ROWS, F32>(rest.size, b, 1, "xent_stats_rest", s)));
+            tiles += (b.N + x_tile(rest.size) - 1) / x_tile(rest.size);
+        }
     }
     // few rows: four wavefronts each (4 rows x 1024 tiles: 65.0 -> 61.0 us for the whole call)
     const float2* part = (const float2*)(ws + p.o_part);
@@ -1310,17 +1353,29 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
         a.e.bias = bias; a.e.labels = labels; a.e.classes = V; a.e.col0 = v0;
         a.e.lse = lse; a.e.dloss = dloss; a.e.G = G; a.e.ldg = p.ldg; a.e.gplane = p.gplane;
         a.e.mask = dw && c == 0 ? mask : nullptr;
-        if (dbias) {
-            // one row tile: its sums are the result
-            a.e.dbias_part = p.mtiles == 1 ? dbias + v0 : dbp;
-            a.e.lddb = p.lddb;
-            TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, F32, true>(p.size, a, 1, "xent_grad", s)));
-            if (p.mtiles > 1) {
-                xent_colsum_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(dbp, p.mtiles, p.lddb, n, dbias + v0);
-                TSM_TRY(check_launch("xent_dbias"));
+        const XRest rest = x_rest(p, R, n, D, F32);
+        for (int part = 0; part < (rest.columns < n ? 2 : 1); ++part) {
+            const int size = part ? rest.size : p.size;
+            const long mtiles = (R + x_tile(size) - 1) / x_tile(size);
+            if (part) {
+                x_columns<T>(p, a, rest.columns, n, x, (const T*)w + v0 * D, D);
+                a.e.G += rest.columns / X_GCOLUMNS * (X_GTILE * X_GCOLUMNS);
+                a.e.mask = nullptr;
+            } else {
+                a.N = rest.columns;
             }
-        } else {
-            TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, F32>(p.size, a, 1, "xent_grad", s)));
+            if (dbias) {
+                // one row tile: its sums are the result
+                a.e.dbias_part = mtiles == 1 ? dbias + a.e.col0 : dbp;
+                a.e.lddb = p.lddb;
+                TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, F32, true>(size, a, 1, part ? "xent_grad_rest" : "xent_grad", s)));
+                if (mtiles > 1) {
+                    xent_colsum_kernel<<<dim3((unsigned)((a.N + 255) / 256)), dim3(256), 0, s>>>(dbp, mtiles, p.lddb, a.N, dbias + a.e.col0);
+                    TSM_TRY(check_launch("xent_dbias"));
+                }
+            } else {
+                TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, F32>(size, a, 1, part ? "xent_grad_rest" : "xent_grad", s)));
+            }
         }
         if (dx) {
             XentArgs b{};

@@ -301,3 +301,13 @@ def test_pieces_of_very_many_classes(dtype, R, D, V):
         want, size = want.cpu().numpy(), size.cpu().numpy()
         within(got.np(), want, (entry + (4 * np.sqrt(n) + 16) * U) * size + half * np.abs(want) + 1e-30, "gradient")
     within(db.np(), G.sum(0).cpu().numpy(), 5e-5 * mag.sum(0).cpu().numpy() + 1e-30, "dbias")
+
+
+@pytest.mark.parametrize("dtype,shape", [("bf16", (1030, 520, 14000)), ("bf16", (1030, 520, 20000)), ("f32", (512, 512, 8500)), ("f32", (400, 600, 9001))])
+@pytest.mark.parametrize("biased,ignored", [(False, False), (True, True)])
+def test_classes_behind_the_last_whole_round_of_tiles(shape, dtype, biased, ignored):
+    """Sizes at which the last classes go to smaller tiles than the others: small, middle, and fp32 operands as they are."""
+    R, D, V = shape
+    labels = _labels(R, V, 4, ignored)
+    inputs, outs = _run(R, D, V, dtype, values((V,), 2, "f32") if biased else None, labels)
+    _check(inputs, outs, labels, dtype)
