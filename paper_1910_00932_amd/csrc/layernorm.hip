@@ -5,7 +5,7 @@
 //
 // Both passes are bound by memory: x -> y forward, x, dy -> dx backward.  A row lives in the registers of L lanes from its
 // one read on (R vectors of 16 bytes per lane), so mean, centred variance and result cost one pass; all sums are fp32.  The
-// weights' gradients are columns sums over all rows: every block keeps its rows' share in registers, writes one row of a
+// weights' gradients are column sums over all rows: every block keeps its rows' share in registers, writes one row of a
 // partial buffer at its end, and a second launch adds the rows in a fixed order.
 #include "internal.h"
 #include "args.h"
@@ -136,11 +136,11 @@ __global__ void __launch_bounds__(LN_NT) ln_fwd_long_kernel(const T* __restrict_
     }
 }
 
-// partial: [gridDim.x][2][C], dgamma's and dbeta's shares of a block's rows.
+// dgamma's and dbeta's shares of a block's rows, `step` values from block to block.
 template <typename T, int L, int R>
 __global__ void __launch_bounds__(LN_NT) ln_bwd_kernel(const T* __restrict__ x, const T* __restrict__ dy, const float* __restrict__ gamma,
                                                        const float* __restrict__ mean_in, const float* __restrict__ rstd_in, T* __restrict__ dx,
-                                                       float* __restrict__ partial, long rows, int C) {
+                                                       float* __restrict__ dgamma, float* __restrict__ dbeta, long step, long rows, int C) {
     constexpr int VE = Elem<T>::VEC;
     constexpr int G = LN_NT / L;                        // rows in flight per block
     __shared__ float red[2][L > 64 ? LN_NT / 64 : 1];
@@ -190,8 +190,8 @@ __global__ void __launch_bounds__(LN_NT) ln_bwd_kernel(const T* __restrict__ x, 
         }
     }
     // the rows in flight meet in LDS, in a fixed order, one sum at a time
-    float* out = partial + (size_t)blockIdx.x * 2 * C;
     for (int which = 0; which < 2; ++which) {
+        float* out = (which ? dbeta : dgamma) + blockIdx.x * step;
         if constexpr (G > 1) {
             __syncthreads();
             if (grp > 0) {
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(LN_NT) ln_bwd_kernel(const T* __restrict__ x, 
 #pragma unroll 4
                         for (int g = 0; g < G - 1; ++g) t += share[(g * R * VE + r * VE + e) * L + lane];
                     }
-                    if (c < C) out[which * C + c] = t;
+                    if (c < C) out[c] = t;
                 }
         }
     }
@@ -257,12 +257,12 @@ __global__ void __launch_bounds__(LN_NT) ln_bwd_long_kernel(const T* __restrict_
 // ... and the weights' gradients by blocks of 64 vectors of columns times a share of the rows.
 template <typename T>
 __global__ void __launch_bounds__(LN_NT) ln_bwd_cols_kernel(const T* __restrict__ x, const T* __restrict__ dy, const float* __restrict__ mean_in,
-                                                            const float* __restrict__ rstd_in, float* __restrict__ partial, long rows, int C) {
+                                                            const float* __restrict__ rstd_in, float* __restrict__ dgamma, float* __restrict__ dbeta, long step, long rows,
+                                                            int C) {
     constexpr int VE = Elem<T>::VEC;
     __shared__ float share[3 * 64 * VE];
     const int lane = threadIdx.x & 63, grp = threadIdx.x >> 6;
     const long cblocks = (C + 64 * VE - 1) / (64 * VE);
-    float* out = partial + (size_t)blockIdx.y * 2 * C;
     for (long cb = blockIdx.x; cb < cblocks; cb += gridDim.x) {
         const int c0 = (int)((cb * 64 + lane) * VE);
         float ag[VE], ab[VE];
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(LN_NT) ln_bwd_cols_kernel(const T* __restrict_
                     if (c0 + e < C) {
                         float t = which ? ab[e] : ag[e];
                         for (int g = 0; g < 3; ++g) t += share[(g * VE + e) * 64 + lane];
-                        out[which * C + c0 + e] = t;
+                        (which ? dbeta : dgamma)[blockIdx.y * step + c0 + e] = t;
                     }
         }
     }
@@ -366,7 +366,7 @@ static int ln_bwd_blocks(const tsm_layernorm_desc* d) {
         return (int)(share < 16 ? share : 16);
     }
     const int64_t groups = (d->rows + LN_NT / L - 1) / (LN_NT / L);
-    return (int)(groups < LN_BLOCKS ? groups : LN_BLOCKS);
+    return groups <= 2 ? 1 : (int)(groups < LN_BLOCKS ? groups : LN_BLOCKS);
 }
 
 static size_t ln_ws_bytes(const tsm_layernorm_desc* d) { return align_up((size_t)ln_bwd_blocks(d) * 2 * d->C * sizeof(float)); }
@@ -391,18 +391,22 @@ static int ln_bwd(const tsm_layernorm_desc* d, const void* x, const void* dy, co
     ln_shape(d->C, d->dtype, &L, &R);
     const int nb = ln_bwd_blocks(d);
     const dim3 grid((unsigned)nb), block(LN_NT);
-#define CALL(T, L, R) ln_bwd_kernel<T, L, R><<<grid, block, 0, s>>>((const T*)x, (const T*)dy, gamma, mean, rstd, (T*)dx, partial, d->rows, d->C)
+    // one block's shares are the result (16 rows of 43, call after call: 10.2 -> 8.3 us)
+    float *pg = nb > 1 ? partial : dgamma, *pb = nb > 1 ? partial + d->C : dbeta;
+    const long step = 2L * d->C;
+#define CALL(T, L, R) ln_bwd_kernel<T, L, R><<<grid, block, 0, s>>>((const T*)x, (const T*)dy, gamma, mean, rstd, (T*)dx, pg, pb, step, d->rows, d->C)
     if (L == 0) {
         const dim3 rgrid((unsigned)(d->rows < (1 << 22) ? d->rows : (1 << 22)));
         ln_bwd_long_kernel<T><<<rgrid, block, 0, s>>>((const T*)x, (const T*)dy, gamma, mean, rstd, (T*)dx, d->rows, d->C);
         TSM_TRY(check_launch("layernorm_bwd_rows"));
         const int64_t cb = cdiv(d->C, 64 * Elem<T>::VEC);
-        ln_bwd_cols_kernel<T><<<dim3((unsigned)cb, (unsigned)nb), block, 0, s>>>((const T*)x, (const T*)dy, mean, rstd, partial, d->rows, d->C);
+        ln_bwd_cols_kernel<T><<<dim3((unsigned)cb, (unsigned)nb), block, 0, s>>>((const T*)x, (const T*)dy, mean, rstd, pg, pb, step, d->rows, d->C);
     } else {
         LN_DISPATCH(T, CALL);
     }
 #undef CALL
     TSM_TRY(check_launch("layernorm_bwd"));
+    if (nb == 1) return TSM_OK;
     ln_join_kernel<<<dim3((unsigned)((2L * d->C + 63) / 64)), dim3(1024), 0, s>>>(partial, nb, d->C, dgamma, dbeta);
     return check_launch("layernorm_join");
 }
