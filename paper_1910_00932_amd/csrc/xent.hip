@@ -53,7 +53,7 @@ struct XentArgs {
     XentEpi e;
 };
 
-enum { X_SMALL = 0, X_MID = 1, X_BIG = 2 };      // tiles of 64, 128, 256
+enum { X_TINY = 0, X_SMALL = 1, X_MID = 2, X_BIG = 3 };      // tiles of 32 (s in fp32 only), 64, 128, 256
 enum { XE_STATS = 0, XE_GRAD = 1, XE_OUT = 2 };
 
 __device__ __forceinline__ bool is_class(int label, long classes) { return label >= 0 && label < classes; }
@@ -456,12 +456,15 @@ __device__ __forceinline__ float sum32(float v) {
 // parts, all of which a stage holds, so that each is loaded once for the six products: eight wavefronts of 64 x 32, one block per CU.
 // fp32 operands of small and deep tiles lie in LDS whole and are cut where they are multiplied, each value by two wavefronts: that
 // saves the pass that cuts them, for products that wait for memory and on one another's steps anyway (us of a training pass: 15 x 772 x 69968,
-// where that pass was most of it, 683 -> 310, 157 x 3377 x 285, whose steps are few now, 242 -> 152).
-struct XBig { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NS = 2, KG = 1, BK = 64, PARTS = 1; };
-struct XMid { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, NS = 2, KG = 1, BK = 64, PARTS = 1; };
-struct XSmall { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 4, KG = 1, BK = 64, PARTS = 1; };
-struct XDeep { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 2, KG = 4, BK = 64, PARTS = 1; };
-struct XParts { static constexpr int BM = 128, BN = 128, WM = 2, WN = 4, NS = 2, KG = 1, BK = 32, PARTS = 3; };
+// where that pass was most of it, 683 -> 310, 157 x 3377 x 285, whose steps are few now, 242 -> 152).  Tiny, for the fewest tiles in fp32:
+// sixteen wavefronts take steps of a tile of 32 x 32 straight from memory, which spreads the cutting over more CUs (152 -> 102; in bf16, where
+// nothing is cut, rows of 16-byte reads cost what that saves: 64 x 2048 x 400 34.1 and 36.5).
+struct XBig { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NS = 2, KG = 1, BK = 64, PARTS = 1; static constexpr bool DIRECT = false; };
+struct XMid { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, NS = 2, KG = 1, BK = 64, PARTS = 1; static constexpr bool DIRECT = false; };
+struct XSmall { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 4, KG = 1, BK = 64, PARTS = 1; static constexpr bool DIRECT = false; };
+struct XDeep { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 2, KG = 4, BK = 64, PARTS = 1; static constexpr bool DIRECT = false; };
+struct XTiny { static constexpr int BM = 32, BN = 32, WM = 1, WN = 1, NS = 1, KG = 16, BK = 64, PARTS = 1; static constexpr bool DIRECT = true; };
+struct XParts { static constexpr int BM = 128, BN = 128, WM = 2, WN = 4, NS = 2, KG = 1, BK = 32, PARTS = 3; static constexpr bool DIRECT = false; };
 // What a stage holds of each operand: parts of K steps each.  WHOLE: fp32 as it is, which to its loads is twice as many bf16 along K, or,
 // of the operand whose rows are K (OUT's second), along its columns; G is in parts.
 template <typename C, int MODE, bool SPLIT>
@@ -470,7 +473,8 @@ struct XStage {
     static constexpr int BK = WOUT ? 32 : C::BK, APARTS = WOUT ? 3 : C::PARTS, BPARTS = C::PARTS, BROWS = WOUT ? 2 * C::BN : C::BN;
     static constexpr int NS = WOUT ? 3 : C::NS;
     static constexpr int BYTES = (C::BM * APARTS + BROWS * BPARTS) * BK * 2;
-    static constexpr int SMEM = C::KG * NS * BYTES + C::WN * C::BM * 8 + C::BN * 4;       // stages, row statistics, biases
+    static constexpr int STAGES = C::DIRECT ? (C::KG - 1) * C::BM * C::BN * 4 : C::KG * NS * BYTES;      // (direct: the groups' sums)
+    static constexpr int SMEM = STAGES + C::WN * C::BM * 8 + C::BN * 4;       // stages, row statistics, biases
 };
 static constexpr int X_LAUNCH = 1 << 22;   // blocks of one launch, at most
 
@@ -479,10 +483,10 @@ template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
 __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(XentArgs a) {
     constexpr int BM = C::BM, BN = C::BN, WM = C::WM, WN = C::WN, NT = WM * WN * 64, MI = BM / (WM * 32), NJ = BN / (WN * 32);
     constexpr bool BIG = NJ == 2;
-    static_assert((BIG && (MI == 4 || MI == 2)) || (MI == 1 && NJ == 1 && BN == 64) || (C::PARTS == 3 && MI == 2 && NJ == 1 && SPLIT), "read_frags, read_step, read_parts");
+    static_assert((BIG && (MI == 4 || MI == 2)) || (MI == 1 && NJ == 1 && (BN == 64 || C::DIRECT)) || (C::PARTS == 3 && MI == 2 && NJ == 1 && SPLIT), "read_frags, read_step, read_parts");
     typedef XStage<C, MODE, SPLIT> S;
     constexpr int TM = BM / WM, TN = BN / WN, NS = S::NS, KG = C::KG, STAGE = S::BYTES;
-    static_assert(KG == 1 || (AKIND == X_ROWS && BKIND == X_ROWS), "groups skip steps");
+    static_assert(KG == 1 || (AKIND == X_ROWS && BKIND == X_ROWS && MODE != XE_OUT), "groups skip steps");
     constexpr int BK = S::BK, PARTS = C::PARTS;
     constexpr bool WHOLE = S::WHOLE, WOUT = S::WOUT;
     typedef XOperand<BM, AKIND, NT, BK> OpA;
@@ -490,8 +494,8 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     constexpr int NP = OpA::PIECES * S::APARTS + OpB::PIECES * S::BPARTS;
     constexpr float L2E = 1.44269502f;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    float2* s_part = (float2*)(smem + KG * NS * STAGE);         // [WN][BM]; the column sums of G as floats [WM][BN]
-    float* s_bias = (float*)(smem + KG * NS * STAGE + WN * BM * 8);     // [BN]
+    float2* s_part = (float2*)(smem + S::STAGES);               // [WN][BM]; the column sums of G as floats [WM][BN]
+    float* s_bias = (float*)(smem + S::STAGES + WN * BM * 8);   // [BN]
     const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT), tid = threadIdx.x % NT;      // within the group
     const int lane = tid & 63, wave = tid >> 6, hi = lane >> 5, lo = lane & 31;
     const int wave_u = __builtin_amdgcn_readfirstlane(wave);
@@ -575,7 +579,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     XScale scale;
     float factor = 1.f;
     if constexpr (SCALE && MODE == XE_OUT) scale.load(a.e, a.e.rows);      // (awaited behind the first steps' loads)
-    if (steps > 0) {
+    if (!C::DIRECT && steps > 0) {
         pa.init(a.A, a.lda, m0, a.M, kb, tid);
         pb.init(a.B, a.ldb, WOUT ? 2 * n0 : n0, WOUT ? 2 * a.N : a.N, kb, tid);
         if constexpr (KG == 1) load_step(0);
@@ -584,6 +588,23 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     auto multiply_parts = [&](const x_bf16x8 (&fa)[3], const x_bf16x8 (&fb)[3]) {
 #pragma unroll
         for (int k = 0; k < 6; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[PB[k]], fa[PA[k]], acc[0][0], 0, 0, 0);
+    };
+    auto join_groups = [&]() {                                  // the sums of all groups, in the first one
+        float4* sums = (float4*)smem;                           // [KG - 1][4][NT]
+        if (group > 0) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                sums[((group - 1) * 4 + r) * NT + tid] = make_float4(acc[0][0][4 * r], acc[0][0][4 * r + 1], acc[0][0][4 * r + 2], acc[0][0][4 * r + 3]);
+        }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll 3
+        for (int g = 0; g < KG - 1; ++g)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float4 o = sums[(g * 4 + r) * NT + tid];
+                acc[0][0][4 * r] += o.x; acc[0][0][4 * r + 1] += o.y; acc[0][0][4 * r + 2] += o.z; acc[0][0][4 * r + 3] += o.w;
+            }
     };
     if constexpr (BIG) {
         x_bf16x8 af[2][MI], bf[2][NJ];
@@ -646,6 +667,35 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
             __builtin_amdgcn_sched_barrier(0);
             if (s + 1 < steps) read(S0{}, nxt);
         }
+    } else if constexpr (C::DIRECT) {
+        static_assert(WHOLE, "fp32");
+        // a wavefront's fragments come from memory as they are, those of its next step before this one's are multiplied
+        const __amdgpu_buffer_rsrc_t ra = x_rsrc((const void*)OpA::uniform((uint64_t)(a.A + m0 * a.lda))), rb = x_rsrc((const void*)OpA::uniform((uint64_t)(a.B + n0 * a.ldb)));
+        const uint32_t rowa = m0 + lo < a.M ? (uint32_t)(lo * a.lda * 2) : X_OOB, rowb = n0 + lo < a.N ? (uint32_t)(lo * a.ldb * 2) : X_OOB;
+        x_bf16x8 fa[2][4], fb[2][4];
+        auto fetch = [&](int s, int f) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {                       // two reads of four values per slice
+                const long k = (long)s * BK + q / 2 * 32 + hi * 16 + q % 2 * 8;
+                const uint32_t out = k < a.K ? 0 : X_OOB;
+                fa[f][q] = __builtin_bit_cast(x_bf16x8, __builtin_amdgcn_raw_buffer_load_b128(ra, (int)((rowa + (uint32_t)(k * 2)) | out | (rowa & X_OOB)), 0, 0));
+                fb[f][q] = __builtin_bit_cast(x_bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rb, (int)((rowb + (uint32_t)(k * 2)) | out | (rowb & X_OOB)), 0, 0));
+            }
+        };
+        auto take = [&](int f) {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) multiply_parts(XCut::of(fa[f][2 * ks], fa[f][2 * ks + 1]).part, XCut::of(fb[f][2 * ks], fb[f][2 * ks + 1]).part);
+        };
+        if (group < steps) fetch(group, 0);
+        for (int s = group; s < steps; s += 2 * KG) {
+            if (s + KG < steps) fetch(s + KG, 1);
+            take(0);
+            if (s + KG < steps) {
+                if (s + 2 * KG < steps) fetch(s + 2 * KG, 0);
+                take(1);
+            }
+        }
+        join_groups();
     } else if constexpr (KG > 1) {
         kc = group - KG;
         if (group < steps) next_step(0);
@@ -670,21 +720,7 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
         }
         x_wait<0>();
         x_barrier();
-        float4* sums = (float4*)smem;                           // [KG - 1][4][NT]
-        if (group > 0) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                sums[((group - 1) * 4 + r) * NT + tid] = make_float4(acc[0][0][4 * r], acc[0][0][4 * r + 1], acc[0][0][4 * r + 2], acc[0][0][4 * r + 3]);
-        }
-        __syncthreads();
-        if (group > 0) return;                                  // (barriers are among the wavefronts that are left)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int g = 0; g < KG - 1; ++g) {
-                const float4 o = sums[(g * 4 + r) * NT + tid];
-                acc[0][0][4 * r] += o.x; acc[0][0][4 * r + 1] += o.y; acc[0][0][4 * r + 2] += o.z; acc[0][0][4 * r + 3] += o.w;
-            }
+        join_groups();
     } else if constexpr (PARTS > 1) {
         static_assert(NS == 2, "two stages");
         for (int s = 0; s < steps; ++s) {                       // (three stages instead of two: the same time)
@@ -759,6 +795,8 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
         }
     }
 
+    if (KG > 1 && group > 0) return;                            // (barriers are among the wavefronts that are left)
+
     // ---- epilogue: this lane has rows mrow(i), columns nw + ncol(j, q) .. + 3
     const int wrow = wm * TM + lo;
     auto mrow = [&](int i) { return m0 + wrow + i * 32; };
@@ -789,7 +827,10 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
         if (tid < BN) s_bias[tid] = a.e.bias && n0 + tid < a.N ? a.e.bias[a.e.col0 + n0 + tid] : 0.f;
         if (MODE == XE_GRAD && a.e.mask && nt == 0 && tid < BM) {
             const uint64_t b = __ballot(m0 + tid < a.M && is_class(a.e.labels[m0 + tid < a.M ? m0 + tid : 0], a.e.classes));
-            if (lane == 0) a.e.mask[(m0 + tid) / 64] = b;
+            if (lane == 0) {
+                if (BM >= 64) a.e.mask[(m0 + tid) / 64] = b;
+                else ((uint32_t*)a.e.mask)[m0 / 32] = (uint32_t)b;
+            }
         }
         __syncthreads();
 #pragma unroll
@@ -1115,7 +1156,7 @@ static constexpr size_t XENT_G_BYTES = (size_t)512 << 20;   // of a piece of G, 
 
 static long x_tiles(long M, long N, int t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }
 
-static int x_tile(int size) { return size == X_BIG ? 256 : size == X_MID ? 128 : 64; }
+static int x_tile(int size) { return size == X_BIG ? 256 : size == X_MID ? 128 : size == X_SMALL ? 64 : 32; }
 static int x_room(int size, bool parts) { return size == X_BIG || (size == X_MID && parts) ? 256 : 512; }      // blocks that run at one time
 
 // Splits of K that fill the chip, each of 512 products per result at least (fp32: of parts).
@@ -1168,7 +1209,8 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     p.pieces = (V + piece - 1) / piece;
     const bool f32 = parts == 3;
     p.size = x_size(R, piece, D, false, f32);
-    p.whole = f32 && p.size == X_SMALL;
+    if (f32 && p.size == X_SMALL && x_tiles(R, V, 32) <= 256) p.size = X_TINY;
+    p.whole = f32 && p.size <= X_SMALL;
     p.cut = p.whole ? D % 4 != 0 : f32 || D % 8 != 0;
     p.Cp = p.whole ? (D + 3) / 4 * 4 : (D + 7) / 8 * 8;
     p.pitch = p.whole ? 2 * p.Cp : p.Cp;
@@ -1181,7 +1223,7 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     for (const long n : {piece, last}) p.mtiles = std::max(p.mtiles, (R + x_tile(x_rest(p, R, n, D, f32).size) - 1) / x_tile(x_rest(p, R, n, D, f32).size));
     p.xplane = R * p.Cp;
     p.wplane = piece * p.Cp;
-    p.ldg = (piece + t - 1) / t * t * X_GTILE;
+    p.ldg = (piece + std::max(t, 64L) - 1) / std::max(t, 64L) * std::max(t, 64L) * X_GTILE;
     p.gplane = (R + X_GTILE - 1) / X_GTILE * p.ldg;
     p.lddb = (piece + 7) / 8 * 8;
     Arena f(nullptr, 0);
@@ -1244,6 +1286,8 @@ static int x_product(int size, const XentArgs& a, int splits, const char* what, 
         if (size == X_BIG) return x_launch<XBig, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
         if (size == X_MID) return x_launch<XMid, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     }
+    if constexpr (MODE != XE_OUT && SPLIT)
+        if (size == X_TINY) return x_launch<XTiny, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     if constexpr (MODE != XE_OUT)      // (us at 64 x 2048 x 400: 14.2 with small tiles, 10.3 with deep ones)
         if (x_tiles(a.M, a.N, 64) <= 256 && a.K >= 512) return x_launch<XDeep, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     return x_launch<XSmall, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
