@@ -480,7 +480,7 @@ static constexpr int X_LAUNCH = 1 << 22;   // blocks of one launch, at most
 
 // SPLIT: operands in three parts.  DB: the column sums of G are wanted.
 template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
-__global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(XentArgs a) {
+__device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njobs) {
     constexpr int BM = C::BM, BN = C::BN, WM = C::WM, WN = C::WN, NT = WM * WN * 64, MI = BM / (WM * 32), NJ = BN / (WN * 32);
     constexpr bool BIG = NJ == 2;
     static_assert((BIG && (MI == 4 || MI == 2)) || (MI == 1 && NJ == 1 && (BN == 64 || C::DIRECT)) || (C::PARTS == 3 && MI == 2 && NJ == 1 && SPLIT), "read_frags, read_step, read_parts");
@@ -506,9 +506,8 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     // of 2, 4, 8, 16, 32 row tiles: dw 4.23, 4.19, 4.42, 4.98, 5.24 ms of 8192 x 2048 x 131072, statistics, with the final loop, at 4, 8, 16 3.61, 3.66, 3.76).
     constexpr int BAND = 4;
     const long mtiles = (a.M + BM - 1) / BM, ntiles = (a.N + BN - 1) / BN, tiles = mtiles * ntiles;
-    const int njobs = gridDim.x;
-    const int xcd = blockIdx.x & 7;
-    const long job = a.job0 + xcd * (njobs / 8) + (xcd < njobs % 8 ? xcd : njobs % 8) + (blockIdx.x >> 3), tile = job % tiles, z = job / tiles;
+    const int xcd = block & 7;
+    const long job = a.job0 + xcd * (njobs / 8) + (xcd < njobs % 8 ? xcd : njobs % 8) + (block >> 3), tile = job % tiles, z = job / tiles;
     const long band = tile / (BAND * ntiles), rest = tile - band * BAND * ntiles;
     const long high = mtiles - band * BAND < BAND ? mtiles - band * BAND : BAND;
     const long mt = band * BAND + rest % high, nt = rest / high;
@@ -1016,6 +1015,17 @@ __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(X
     }
 }
 
+template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
+__global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(XentArgs a) {
+    xent_tile<C, MODE, AKIND, BKIND, SPLIT, DB>(a, blockIdx.x, gridDim.x);
+}
+// The two products that read G, where both have small tiles: dx by the first nx blocks, dw by the others.
+template <bool SPLIT>
+__global__ void __launch_bounds__(XSmall::WM * XSmall::WN * 64) xent_both_kernel(XentArgs dx, XentArgs dw, int nx) {
+    if ((int)blockIdx.x < nx) xent_tile<XSmall, XE_OUT, X_GROWS, X_COLS, SPLIT, false>(dx, blockIdx.x, nx);
+    else xent_tile<XSmall, XE_OUT, X_GCOLS, X_COLS, SPLIT, false>(dw, blockIdx.x - nx, gridDim.x - nx);
+}
+
 // Rows of C fp32 values as rows of Cp, zero behind the C-th.  Two tensors in a launch.
 __global__ void __launch_bounds__(256) xent_pad_kernel(const float* __restrict__ in0, long rows0, float* __restrict__ out0, const float* __restrict__ in1,
                                                        long rows1, float* __restrict__ out1, int C, int Cp) {
@@ -1259,6 +1269,8 @@ static int xent_check(const tsm_xent_desc* d, const char* who) {
 
 static size_t xent_ws(const XentPlan& p) { return p.fwd_bytes > p.bwd_bytes ? p.fwd_bytes : p.bwd_bytes; }
 
+static long x_ksplit(long K, int splits) { return ((K + splits - 1) / splits + 63) / 64 * 64; }
+
 template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
 static int x_launch(XentArgs a, int splits, const char* what, hipStream_t s) {
     auto kernel = xent_tile_kernel<C, MODE, AKIND, BKIND, SPLIT, DB>;
@@ -1269,7 +1281,7 @@ static int x_launch(XentArgs a, int splits, const char* what, hipStream_t s) {
         configured = true;
     }
     const long jobs = x_tiles(a.M, a.N, C::BM) * splits;
-    a.ksplit = ((a.K + splits - 1) / splits + 63) / 64 * 64;
+    a.ksplit = x_ksplit(a.K, splits);
     for (a.job0 = 0; a.job0 < jobs; a.job0 += X_LAUNCH) {
         const long n = jobs - a.job0;
         kernel<<<dim3((unsigned)(n < X_LAUNCH ? n : X_LAUNCH)), dim3(C::WM * C::WN * C::KG * 64), XStage<C, MODE, SPLIT>::SMEM, s>>>(a);
@@ -1291,6 +1303,23 @@ static int x_product(int size, const XentArgs& a, int splits, const char* what, 
     if constexpr (MODE != XE_OUT)      // (us at 64 x 2048 x 400: 14.2 with small tiles, 10.3 with deep ones)
         if (x_tiles(a.M, a.N, 64) <= 256 && a.K >= 512) return x_launch<XDeep, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     return x_launch<XSmall, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+}
+
+// dx and dw in one launch, which small ones would otherwise wait for each other's.
+template <bool SPLIT>
+static int x_both(XentArgs dx, int zdx, XentArgs dw, int zdw, const char* what, hipStream_t s) {
+    auto kernel = xent_both_kernel<SPLIT>;
+    static bool configured = false;
+    if (!configured) {
+        if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
+            return fail(TSM_ERR_LAUNCH, "%s: cannot raise dynamic LDS limit", what);
+        configured = true;
+    }
+    const long nx = x_tiles(dx.M, dx.N, XSmall::BM) * zdx, nw = x_tiles(dw.M, dw.N, XSmall::BM) * zdw;
+    dx.ksplit = x_ksplit(dx.K, zdx);
+    dw.ksplit = x_ksplit(dw.K, zdw);
+    kernel<<<dim3((unsigned)(nx + nw)), dim3(XSmall::WM * XSmall::WN * 64), XStage<XSmall, XE_OUT, SPLIT>::SMEM, s>>>(dx, dw, (int)nx);
+    return check_launch(what);
 }
 
 template <typename T>
@@ -1421,39 +1450,46 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
                 TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, F32>(size, a, 1, part ? "xent_grad_rest" : "xent_grad", s)));
             }
         }
+        XentArgs gx{}, gw{};
+        gx.A = gw.A = G;
+        gx.lda = gw.lda = p.ldg;
+        gx.aplane = gw.aplane = p.gplane;
+        gx.e.labels = gw.e.labels = labels;
+        gx.e.dloss = gw.e.dloss = dloss;
+        gx.e.classes = gw.e.classes = V;
+        gx.e.rows = gw.e.rows = R;
+        gx.ldb = gw.ldb = p.pitch;
+        T* out = (T*)dw + v0 * D;
         if (dx) {
-            XentArgs b{};
-            b.A = G; b.lda = p.ldg; b.aplane = p.gplane;
-            b.B = wo; b.ldb = p.pitch; b.bplane = p.wplane;
+            gx.B = wo; gx.bplane = p.wplane;
             if (F32 && p.sizedx == X_SMALL && !p.whole) {
-                b.B = (const bf16_t*)((const T*)w + v0 * D);
-                b.ldb = 2 * D;
+                gx.B = (const bf16_t*)((const T*)w + v0 * D);
+                gx.ldb = 2 * D;
             }
-            b.M = R; b.N = D; b.K = n;
-            b.e.acc = c > 0 ? acc : nullptr;
-            b.e.labels = labels; b.e.dloss = dloss; b.e.classes = V; b.e.rows = R;
-            if (F32 || p.zdx > 1 || c + 1 < p.pieces) b.e.out_f32 = acc;
-            else b.e.out = (bf16_t*)dx;
-            TSM_TRY((x_product<XE_OUT, X_GROWS, X_COLS, F32>(p.sizedx, b, p.zdx, "xent_dx", s)));
-            if (p.zdx > 1 && c + 1 == p.pieces) TSM_TRY(xent_join<T>(acc, p.zdx, R * D, dx, "xent_dx_join", s));      // (each has added up its pieces)
+            gx.M = R; gx.N = D; gx.K = n;
+            gx.e.acc = c > 0 ? acc : nullptr;
+            if (F32 || p.zdx > 1 || c + 1 < p.pieces) gx.e.out_f32 = acc;
+            else gx.e.out = (bf16_t*)dx;
         }
         if (dw) {
-            XentArgs b{};
-            b.A = G; b.lda = p.ldg; b.aplane = p.gplane;
-            b.B = xo; b.ldb = p.pitch; b.bplane = p.xplane;
+            gw.B = xo; gw.bplane = p.xplane;
             if (F32 && p.sizedw == X_SMALL && !p.whole) {
-                b.B = (const bf16_t*)x;
-                b.ldb = 2 * D;
+                gw.B = (const bf16_t*)x;
+                gw.ldb = 2 * D;
             }
-            b.M = n; b.N = D; b.K = R;
-            b.kmask = mask;
-            b.e.labels = labels; b.e.dloss = dloss; b.e.classes = V; b.e.rows = R;
-            T* out = (T*)dw + v0 * D;
-            if (F32 || p.zdw > 1) b.e.out_f32 = p.zdw > 1 ? dwp : (float*)out;
-            else b.e.out = (bf16_t*)out;
-            TSM_TRY((x_product<XE_OUT, X_GCOLS, X_COLS, F32>(p.sizedw, b, p.zdw, "xent_dw", s)));
-            if (p.zdw > 1) TSM_TRY(xent_join<T>(dwp, p.zdw, n * D, out, "xent_dw_join", s));
+            gw.M = n; gw.N = D; gw.K = R;
+            gw.kmask = mask;
+            if (F32 || p.zdw > 1) gw.e.out_f32 = p.zdw > 1 ? dwp : (float*)out;
+            else gw.e.out = (bf16_t*)out;
         }
+        if (dx && dw && p.sizedx == X_SMALL && p.sizedw == X_SMALL && x_tiles(R, D, 64) * p.zdx + x_tiles(n, D, 64) * p.zdw <= X_LAUNCH) {
+            TSM_TRY((x_both<F32>(gx, p.zdx, gw, p.zdw, "xent_dx_dw", s)));
+        } else {
+            if (dx) TSM_TRY((x_product<XE_OUT, X_GROWS, X_COLS, F32>(p.sizedx, gx, p.zdx, "xent_dx", s)));
+            if (dw) TSM_TRY((x_product<XE_OUT, X_GCOLS, X_COLS, F32>(p.sizedw, gw, p.zdw, "xent_dw", s)));
+        }
+        if (dx && p.zdx > 1 && c + 1 == p.pieces) TSM_TRY(xent_join<T>(acc, p.zdx, R * D, dx, "xent_dx_join", s));      // (each has added up its pieces)
+        if (dw && p.zdw > 1) TSM_TRY(xent_join<T>(dwp, p.zdw, n * D, out, "xent_dw_join", s));
     }
     return TSM_OK;
 }
