@@ -53,7 +53,7 @@ struct XentArgs {
     XentEpi e;
 };
 
-enum { X_TINY = 0, X_SMALL = 1, X_MID = 2, X_BIG = 3 };      // tiles of 32 (s in fp32 only), 64, 128, 256
+enum { X_TINY = 0, X_SMALL = 1, X_MID = 2, X_BIG = 3 };      // tiles of 32 (of s only), 64, 128, 256
 enum { XE_STATS = 0, XE_GRAD = 1, XE_OUT = 2 };
 
 __device__ __forceinline__ bool is_class(int label, long classes) { return label >= 0 && label < classes; }
@@ -131,7 +131,7 @@ struct XOperand {
     static constexpr int RPP = KC ? NT / KV : NT / (ROWS / 8);// rows of the LDS image per pass
     static constexpr int PITCH = KC ? BK * 2 : ROWS * 2;      // its bytes
     uint32_t off[PIECES];         // byte offset in the step's window of this thread's pieces
-    int kfirst;                   // KC: K of the piece, else K of the thread's row in a pass
+    int kfirst;                   // KC: K of the first piece, else K of the thread's row in a pass
     const char *base, *base0;     // of the step's window, of the first one of the first part
     long step;                    // bytes from one step to the next
     int part, part0;              // G: steps into a block (X_GROWS), into 256 rows (X_GCOLS)
@@ -154,7 +154,7 @@ struct XOperand {
             const long pitch = KIND == X_GROWS ? X_GCOLUMNS : ld;
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
-                off[i] = row0 + i * RPP + r < rows ? (uint32_t)((i * RPP + r) * pitch * 2 + kv * 16) : X_OOB;
+                off[i] = row0 + i * RPP + r < rows ? (uint32_t)((i * RPP + r) * pitch * 2 + (kv ^ kswz(i * RPP)) * 16) : X_OOB;
             base0 = (const char*)(KIND == X_GROWS ? p + row0 / X_GTILE * ld + row0 % X_GTILE * X_GCOLUMNS + k0 * X_GTILE : p + row0 * ld + k0);
             step = KIND == X_GROWS ? (X_GTILE * X_GCOLUMNS - (X_GCOLUMNS - BK)) * 2 : BK * 2;      // (into the next block)
         } else {
@@ -200,7 +200,7 @@ struct XOperand {
     // Piece i of the step at the window, `more` bytes behind it: left = K from its start to the end; mask: bit k clear for rows k that
     // count as zero.
     __device__ __forceinline__ void load(unsigned char* stage, int i, int left, uint64_t mask, int wave_u, long more = 0) const {
-        const int k = KC ? kfirst : i * RPP + kfirst;
+        const int k = KC ? kfirst ^ kswz(i * RPP) * 8 : i * RPP + kfirst;
         const bool in = k < left && (KC || (mask >> k) & 1);
         x_load_lds16(x_rsrc(base + more), stage + i * (NT * 16) + wave_u * 1024, in ? off[i] : X_OOB, 0);
     }
@@ -456,14 +456,15 @@ __device__ __forceinline__ float sum32(float v) {
 // parts, all of which a stage holds, so that each is loaded once for the six products: eight wavefronts of 64 x 32, one block per CU.
 // fp32 operands of small and deep tiles lie in LDS whole and are cut where they are multiplied, each value by two wavefronts: that
 // saves the pass that cuts them, for products that wait for memory and on one another's steps anyway (us of a training pass: 15 x 772 x 69968,
-// where that pass was most of it, 683 -> 310, 157 x 3377 x 285, whose steps are few now, 242 -> 152).  Tiny, for the fewest tiles in fp32:
-// sixteen wavefronts take steps of a tile of 32 x 32 straight from memory, which spreads the cutting over more CUs (152 -> 102; in bf16, where
-// nothing is cut, rows of 16-byte reads cost what that saves: 64 x 2048 x 400 34.1 and 36.5).
+// where that pass was most of it, 683 -> 310, 157 x 3377 x 285, whose steps are few now, 242 -> 152).  Tiny, for the fewest tiles: eight
+// wavefronts take every eighth step of a tile of 32 x 32 (128 x 2048 x 1000 34.4 -> 28.1); in fp32 sixteen take theirs straight from memory,
+// which spreads the cutting over more CUs (152 -> 102; in bf16 the rows of 16-byte reads cost what that saves).
 struct XBig { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NS = 2, KG = 1, BK = 64, PARTS = 1; static constexpr bool DIRECT = false; };
 struct XMid { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, NS = 2, KG = 1, BK = 64, PARTS = 1; static constexpr bool DIRECT = false; };
 struct XSmall { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 4, KG = 1, BK = 64, PARTS = 1; static constexpr bool DIRECT = false; };
 struct XDeep { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, NS = 2, KG = 4, BK = 64, PARTS = 1; static constexpr bool DIRECT = false; };
-struct XTiny { static constexpr int BM = 32, BN = 32, WM = 1, WN = 1, NS = 1, KG = 16, BK = 64, PARTS = 1; static constexpr bool DIRECT = true; };
+struct XTiny { static constexpr int BM = 32, BN = 32, WM = 1, WN = 1, NS = 2, KG = 8, BK = 64, PARTS = 1; static constexpr bool DIRECT = false; };
+struct XTinyWhole { static constexpr int BM = 32, BN = 32, WM = 1, WN = 1, NS = 1, KG = 16, BK = 64, PARTS = 1; static constexpr bool DIRECT = true; };
 struct XParts { static constexpr int BM = 128, BN = 128, WM = 2, WN = 4, NS = 2, KG = 1, BK = 32, PARTS = 3; static constexpr bool DIRECT = false; };
 // What a stage holds of each operand: parts of K steps each.  WHOLE: fp32 as it is, which to its loads is twice as many bf16 along K, or,
 // of the operand whose rows are K (OUT's second), along its columns; G is in parts.
@@ -483,7 +484,7 @@ template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
 __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njobs) {
     constexpr int BM = C::BM, BN = C::BN, WM = C::WM, WN = C::WN, NT = WM * WN * 64, MI = BM / (WM * 32), NJ = BN / (WN * 32);
     constexpr bool BIG = NJ == 2;
-    static_assert((BIG && (MI == 4 || MI == 2)) || (MI == 1 && NJ == 1 && (BN == 64 || C::DIRECT)) || (C::PARTS == 3 && MI == 2 && NJ == 1 && SPLIT), "read_frags, read_step, read_parts");
+    static_assert((BIG && (MI == 4 || MI == 2)) || (MI == 1 && NJ == 1) || (C::PARTS == 3 && MI == 2 && NJ == 1 && SPLIT), "read_frags, read_step, read_parts");
     typedef XStage<C, MODE, SPLIT> S;
     constexpr int TM = BM / WM, TN = BN / WN, NS = S::NS, KG = C::KG, STAGE = S::BYTES;
     static_assert(KG == 1 || (AKIND == X_ROWS && BKIND == X_ROWS && MODE != XE_OUT), "groups skip steps");
@@ -1019,11 +1020,27 @@ template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
 __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(XentArgs a) {
     xent_tile<C, MODE, AKIND, BKIND, SPLIT, DB>(a, blockIdx.x, gridDim.x);
 }
-// The two products that read G, where both have small tiles: dx by the first nx blocks, dw by the others.
+// out[c] = sum of the rows of part [rows][ld]
+__device__ __forceinline__ void column_sum(const float* __restrict__ part, long rows, long ld, long n, float* __restrict__ out, long block) {
+    const long c = block * 256 + threadIdx.x;
+    if (c >= n) return;
+    float s = 0.f;
+#pragma unroll 8
+    for (long r = 0; r < rows; ++r) s += part[r * ld + c];
+    out[c] = s;
+}
+struct XColumns {
+    const float* part;
+    long rows, ld, n;
+    float* out;
+};
+// The two products that read G, where both have small tiles: dx by the first nx blocks, dw by nw, the sums of dbias by any others.
 template <bool SPLIT>
-__global__ void __launch_bounds__(XSmall::WM * XSmall::WN * 64) xent_both_kernel(XentArgs dx, XentArgs dw, int nx) {
-    if ((int)blockIdx.x < nx) xent_tile<XSmall, XE_OUT, X_GROWS, X_COLS, SPLIT, false>(dx, blockIdx.x, nx);
-    else xent_tile<XSmall, XE_OUT, X_GCOLS, X_COLS, SPLIT, false>(dw, blockIdx.x - nx, gridDim.x - nx);
+__global__ void __launch_bounds__(XSmall::WM * XSmall::WN * 64) xent_both_kernel(XentArgs dx, XentArgs dw, int nx, int nw, XColumns sums) {
+    const int b = blockIdx.x;
+    if (b < nx) xent_tile<XSmall, XE_OUT, X_GROWS, X_COLS, SPLIT, false>(dx, b, nx);
+    else if (b < nx + nw) xent_tile<XSmall, XE_OUT, X_GCOLS, X_COLS, SPLIT, false>(dw, b - nx, nw);
+    else column_sum(sums.part, sums.rows, sums.ld, sums.n, sums.out, b - nx - nw);
 }
 
 // Rows of C fp32 values as rows of Cp, zero behind the C-th.  Two tensors in a launch.
@@ -1125,16 +1142,9 @@ __global__ void __launch_bounds__(256) xent_finish_kernel(const float2* __restri
     }
 }
 
-// out[c] = sum of the rows of part [rows][ld]
 __global__ void __launch_bounds__(256) xent_colsum_kernel(const float* __restrict__ part, long rows, long ld, long n, float* __restrict__ out) {
-    const long c = (long)blockIdx.x * 256 + threadIdx.x;
-    if (c >= n) return;
-    float s = 0.f;
-#pragma unroll 8
-    for (long r = 0; r < rows; ++r) s += part[r * ld + c];
-    out[c] = s;
+    column_sum(part, rows, ld, n, out, blockIdx.x);
 }
-
 // out = sum of the splits' results, rounded once
 template <typename T>
 __global__ void __launch_bounds__(256) xent_join_kernel(const float* __restrict__ part, int splits, long n, T* __restrict__ out) {
@@ -1219,7 +1229,7 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     p.pieces = (V + piece - 1) / piece;
     const bool f32 = parts == 3;
     p.size = x_size(R, piece, D, false, f32);
-    if (f32 && p.size == X_SMALL && x_tiles(R, V, 32) <= 256) p.size = X_TINY;
+    if ((f32 || D >= 512) && p.size == X_SMALL && x_tiles(R, V, 32) <= 256) p.size = X_TINY;
     p.whole = f32 && p.size <= X_SMALL;
     p.cut = p.whole ? D % 4 != 0 : f32 || D % 8 != 0;
     p.Cp = p.whole ? (D + 3) / 4 * 4 : (D + 7) / 8 * 8;
@@ -1298,16 +1308,16 @@ static int x_product(int size, const XentArgs& a, int splits, const char* what, 
         if (size == X_BIG) return x_launch<XBig, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
         if (size == X_MID) return x_launch<XMid, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     }
-    if constexpr (MODE != XE_OUT && SPLIT)
-        if (size == X_TINY) return x_launch<XTiny, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+    if constexpr (MODE != XE_OUT)
+        if (size == X_TINY) return x_launch<typename std::conditional<SPLIT, XTinyWhole, XTiny>::type, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     if constexpr (MODE != XE_OUT)      // (us at 64 x 2048 x 400: 14.2 with small tiles, 10.3 with deep ones)
         if (x_tiles(a.M, a.N, 64) <= 256 && a.K >= 512) return x_launch<XDeep, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
     return x_launch<XSmall, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
 }
 
-// dx and dw in one launch, which small ones would otherwise wait for each other's.
+// dx, dw and what is left of dbias in one launch: small ones would otherwise wait for one another's.
 template <bool SPLIT>
-static int x_both(XentArgs dx, int zdx, XentArgs dw, int zdw, const char* what, hipStream_t s) {
+static int x_both(XentArgs dx, int zdx, XentArgs dw, int zdw, const XColumns& sums, const char* what, hipStream_t s) {
     auto kernel = xent_both_kernel<SPLIT>;
     static bool configured = false;
     if (!configured) {
@@ -1318,7 +1328,7 @@ static int x_both(XentArgs dx, int zdx, XentArgs dw, int zdw, const char* what, 
     const long nx = x_tiles(dx.M, dx.N, XSmall::BM) * zdx, nw = x_tiles(dw.M, dw.N, XSmall::BM) * zdw;
     dx.ksplit = x_ksplit(dx.K, zdx);
     dw.ksplit = x_ksplit(dw.K, zdw);
-    kernel<<<dim3((unsigned)(nx + nw)), dim3(XSmall::WM * XSmall::WN * 64), XStage<XSmall, XE_OUT, SPLIT>::SMEM, s>>>(dx, dw, (int)nx);
+    kernel<<<dim3((unsigned)(nx + nw + (sums.n + 255) / 256)), dim3(XSmall::WM * XSmall::WN * 64), XStage<XSmall, XE_OUT, SPLIT>::SMEM, s>>>(dx, dw, (int)nx, (int)nw, sums);
     return check_launch(what);
 }
 
@@ -1426,6 +1436,8 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
         a.e.bias = bias; a.e.labels = labels; a.e.classes = V; a.e.col0 = v0;
         a.e.lse = lse; a.e.dloss = dloss; a.e.G = G; a.e.ldg = p.ldg; a.e.gplane = p.gplane;
         a.e.mask = dw && c == 0 ? mask : nullptr;
+        const bool both = dx && dw && p.sizedx == X_SMALL && p.sizedw == X_SMALL && x_tiles(R, D, 64) * p.zdx + x_tiles(n, D, 64) * p.zdw + n / 256 < X_LAUNCH;
+        XColumns sums{};
         const XRest rest = x_rest(p, R, n, D, F32);
         for (int part = 0; part < (rest.columns < n ? 2 : 1); ++part) {
             const int size = part ? rest.size : p.size;
@@ -1442,7 +1454,9 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
                 a.e.dbias_part = mtiles == 1 ? dbias + a.e.col0 : dbp;
                 a.e.lddb = p.lddb;
                 TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, F32, true>(size, a, 1, part ? "xent_grad_rest" : "xent_grad", s)));
-                if (mtiles > 1) {
+                if (mtiles > 1 && both && rest.columns == n) {
+                    sums = XColumns{dbp, mtiles, p.lddb, n, dbias + v0};
+                } else if (mtiles > 1) {
                     xent_colsum_kernel<<<dim3((unsigned)((a.N + 255) / 256)), dim3(256), 0, s>>>(dbp, mtiles, p.lddb, a.N, dbias + a.e.col0);
                     TSM_TRY(check_launch("xent_dbias"));
                 }
@@ -1482,8 +1496,8 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
             if (F32 || p.zdw > 1) gw.e.out_f32 = p.zdw > 1 ? dwp : (float*)out;
             else gw.e.out = (bf16_t*)out;
         }
-        if (dx && dw && p.sizedx == X_SMALL && p.sizedw == X_SMALL && x_tiles(R, D, 64) * p.zdx + x_tiles(n, D, 64) * p.zdw <= X_LAUNCH) {
-            TSM_TRY((x_both<F32>(gx, p.zdx, gw, p.zdw, "xent_dx_dw", s)));
+        if (both) {
+            TSM_TRY((x_both<F32>(gx, p.zdx, gw, p.zdw, sums, "xent_dx_dw", s)));
         } else {
             if (dx) TSM_TRY((x_product<XE_OUT, X_GROWS, X_COLS, F32>(p.sizedx, gx, p.zdx, "xent_dx", s)));
             if (dw) TSM_TRY((x_product<XE_OUT, X_GCOLS, X_COLS, F32>(p.sizedw, gw, p.zdw, "xent_dw", s)));
