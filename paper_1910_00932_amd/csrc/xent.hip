@@ -1228,7 +1228,9 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     p.piece = piece;
     p.pieces = (V + piece - 1) / piece;
     const bool f32 = parts == 3;
-    p.size = x_size(R, piece, D, false, f32);
+    // fp32 of few rows or classes: cutting x and w first costs more than larger tiles save (us of a pass of 100 x 3000 x 20000 with middle and
+    // small tiles 921, 610, of 192 x 1024 x 30000 461, 435, of 256 x 1024 x 30000 513, 555)
+    p.size = f32 && std::min(R, V) <= 192 ? X_SMALL : x_size(R, piece, D, false, f32);
     if ((f32 || D >= 512) && p.size == X_SMALL && x_tiles(R, V, 32) <= 256) p.size = X_TINY;
     p.whole = f32 && p.size <= X_SMALL;
     p.cut = p.whole ? D % 4 != 0 : f32 || D % 8 != 0;
