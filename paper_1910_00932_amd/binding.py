@@ -151,9 +151,9 @@ def _ptr(t):
     return t.data_ptr()
 
 
-def _stream(stream):
+def _stream(stream, dev=None):
     if stream is None:      # (torch.cuda.current_stream() builds a Stream object for it: 2.5 us of a small call)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if dev is None else dev)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
@@ -353,16 +353,15 @@ def _device():
     try:
         return torch.cuda.current_device()
     except RuntimeError:        # no GPU: no tensor is on it
-        return -1
+        return -2
 
 
 def _arg(t, n, dtype, name, dev, at_least=False):
     """The pointer of a tensor of n values of a torch dtype on the current device, dev; None stays None."""
-    if t is None or isinstance(t, int):
+    if t is None or t.__class__ is int:
         return t
     # (one condition for what is right: these checks run before every launch)
-    if (t.numel() == n or (at_least and t.numel() > n)) and t.dtype is dtype and t.is_contiguous() and \
-            t.get_device() == dev:
+    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and (t.numel() == n or (at_least and t.numel() > n)):
         return t.data_ptr()
     _ptr(t)
     if t.dtype != dtype or t.numel() != n:
@@ -395,7 +394,7 @@ def tsm_recur_fwd(desc, x, g, h0, y, h_last, saved, ws, stream=None):
     dev = _device()
     _check(lib().tsm_recur_fwd(ctypes.addressof(desc), _arg(x, n, dt, "x", dev), _arg(g, n, dt, "g", dev), _arg(h0, m, f, "h0", dev),
                                _arg(y, n, dt, "y", dev), _arg(h_last, m, f, "h_last", dev),
-                               _saved(saved, desc), p, nb, _stream(stream)))
+                               _saved(saved, desc), p, nb, _stream(stream, dev)))
 
 
 def tsm_recur_bwd(desc, x, g, h0, saved, dy, dh_last, dx, dg, dh0, ws, stream=None):
@@ -406,7 +405,7 @@ def tsm_recur_bwd(desc, x, g, h0, saved, dy, dh_last, dx, dg, dh0, ws, stream=No
     _check(lib().tsm_recur_bwd(ctypes.addressof(desc), _arg(x, n, dt, "x", dev), _arg(g, n, dt, "g", dev), _arg(h0, m, f, "h0", dev),
                                _saved(saved, desc),
                                _arg(dy, n, dt, "dy", dev), _arg(dh_last, m, f, "dh_last", dev), _arg(dx, n, dt, "dx", dev),
-                               _arg(dg, n, dt, "dg", dev), _arg(dh0, m, f, "dh0", dev), p, nb, _stream(stream)))
+                               _arg(dg, n, dt, "dg", dev), _arg(dh0, m, f, "dh0", dev), p, nb, _stream(stream, dev)))
 
 
 def tsm_layernorm_workspace_bytes(desc):
@@ -418,7 +417,7 @@ def tsm_layernorm_fwd(desc, x, gamma, beta, y, mean, rstd, stream=None):
     dev = _device()
     _check(lib().tsm_layernorm_fwd(ctypes.addressof(desc), _arg(x, n, dt, "x", dev), _arg(gamma, c, f, "gamma", dev),
                                    _arg(beta, c, f, "beta", dev), _arg(y, n, dt, "y", dev), _arg(mean, r, f, "mean", dev, True),
-                                   _arg(rstd, r, f, "rstd", dev, True), _stream(stream)))
+                                   _arg(rstd, r, f, "rstd", dev, True), _stream(stream, dev)))
 
 
 def tsm_layernorm_bwd(desc, x, dy, gamma, mean, rstd, dx, dgamma, dbeta, ws, stream=None):
@@ -428,7 +427,7 @@ def tsm_layernorm_bwd(desc, x, dy, gamma, mean, rstd, dx, dgamma, dbeta, ws, str
     _check(lib().tsm_layernorm_bwd(ctypes.addressof(desc), _arg(x, n, dt, "x", dev), _arg(dy, n, dt, "dy", dev),
                                    _arg(gamma, c, f, "gamma", dev), _arg(mean, r, f, "mean", dev, True), _arg(rstd, r, f, "rstd", dev, True),
                                    _arg(dx, n, dt, "dx", dev), _arg(dgamma, c, f, "dgamma", dev), _arg(dbeta, c, f, "dbeta", dev), p, nb,
-                                   _stream(stream)))
+                                   _stream(stream, dev)))
 
 
 def tsm_xent_workspace_bytes(desc):
@@ -441,7 +440,7 @@ def tsm_xent_fwd(desc, x, w, bias, labels, loss, lse, ws, stream=None):
     dev = _device()
     _check(lib().tsm_xent_fwd(ctypes.addressof(desc), _arg(x, r * d, dt, "x", dev), _arg(w, v * d, dt, "w", dev),
                               _arg(bias, v, f, "bias", dev), _arg(labels, r, torch.int32, "labels", dev), _arg(loss, r, f, "loss", dev),
-                              _arg(lse, r, f, "lse", dev), p, nb, _stream(stream)))
+                              _arg(lse, r, f, "lse", dev), p, nb, _stream(stream, dev)))
 
 
 def tsm_xent_bwd(desc, x, w, bias, labels, lse, dloss, dx, dw, dbias, ws, stream=None):
@@ -451,4 +450,4 @@ def tsm_xent_bwd(desc, x, w, bias, labels, lse, dloss, dx, dw, dbias, ws, stream
     _check(lib().tsm_xent_bwd(ctypes.addressof(desc), _arg(x, r * d, dt, "x", dev), _arg(w, v * d, dt, "w", dev),
                               _arg(bias, v, f, "bias", dev), _arg(labels, r, torch.int32, "labels", dev), _arg(lse, r, f, "lse", dev),
                               _arg(dloss, r, f, "dloss", dev), _arg(dx, r * d, dt, "dx", dev), _arg(dw, v * d, dt, "dw", dev),
-                              _arg(dbias, v, f, "dbias", dev), p, nb, _stream(stream)))
+                              _arg(dbias, v, f, "dbias", dev), p, nb, _stream(stream, dev)))
