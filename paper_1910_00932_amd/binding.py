@@ -370,13 +370,24 @@ def _arg(t, n, dtype, name, dev, at_least=False):
     raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, t.get_device(), dev))
 
 
-def _saved(t, desc):
+def _buffer(t, name, dev):
+    """The pointer of a caller's buffer on the current device, dev, and its bytes."""
+    if t is None:
+        return None, 0
+    p = _ptr(t)
+    if t.get_device() != dev:
+        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, t.get_device(), dev))
+    return p, t.numel() * t.element_size()
+
+
+def _saved(t, desc, dev):
     if t is None or isinstance(t, int):
         return t
+    p, got = _buffer(t, "saved", dev)
     n = tsm_recur_saved_bytes(desc)
-    if t.numel() * t.element_size() < n:
-        raise ValueError("saved: expected at least %d bytes, got %d" % (n, t.numel() * t.element_size()))
-    return _ptr(t)
+    if got < n:
+        raise ValueError("saved: expected at least %d bytes, got %d" % (n, got))
+    return p
 
 
 def tsm_recur_saved_bytes(desc):
@@ -390,20 +401,20 @@ def tsm_recur_workspace_bytes(desc):
 def tsm_recur_fwd(desc, x, g, h0, y, h_last, saved, ws, stream=None):
     m = desc.N * desc.C * desc.H * desc.W
     n, dt, f = m * desc.T, _TORCH_DTYPE.get(desc.dtype), torch.float32
-    p, nb = _ws(ws)
     dev = _device()
+    p, nb = _buffer(ws, "the workspace", dev)
     _check(lib().tsm_recur_fwd(ctypes.addressof(desc), _arg(x, n, dt, "x", dev), _arg(g, n, dt, "g", dev), _arg(h0, m, f, "h0", dev),
                                _arg(y, n, dt, "y", dev), _arg(h_last, m, f, "h_last", dev),
-                               _saved(saved, desc), p, nb, _stream(stream, dev)))
+                               _saved(saved, desc, dev), p, nb, _stream(stream, dev)))
 
 
 def tsm_recur_bwd(desc, x, g, h0, saved, dy, dh_last, dx, dg, dh0, ws, stream=None):
     m = desc.N * desc.C * desc.H * desc.W
     n, dt, f = m * desc.T, _TORCH_DTYPE.get(desc.dtype), torch.float32
-    p, nb = _ws(ws)
     dev = _device()
+    p, nb = _buffer(ws, "the workspace", dev)
     _check(lib().tsm_recur_bwd(ctypes.addressof(desc), _arg(x, n, dt, "x", dev), _arg(g, n, dt, "g", dev), _arg(h0, m, f, "h0", dev),
-                               _saved(saved, desc),
+                               _saved(saved, desc, dev),
                                _arg(dy, n, dt, "dy", dev), _arg(dh_last, m, f, "dh_last", dev), _arg(dx, n, dt, "dx", dev),
                                _arg(dg, n, dt, "dg", dev), _arg(dh0, m, f, "dh0", dev), p, nb, _stream(stream, dev)))
 
@@ -422,8 +433,8 @@ def tsm_layernorm_fwd(desc, x, gamma, beta, y, mean, rstd, stream=None):
 
 def tsm_layernorm_bwd(desc, x, dy, gamma, mean, rstd, dx, dgamma, dbeta, ws, stream=None):
     n, r, c, dt, f = desc.rows * desc.C, desc.rows, desc.C, _TORCH_DTYPE.get(desc.dtype), torch.float32
-    p, nb = _ws(ws)
     dev = _device()
+    p, nb = _buffer(ws, "the workspace", dev)
     _check(lib().tsm_layernorm_bwd(ctypes.addressof(desc), _arg(x, n, dt, "x", dev), _arg(dy, n, dt, "dy", dev),
                                    _arg(gamma, c, f, "gamma", dev), _arg(mean, r, f, "mean", dev, True), _arg(rstd, r, f, "rstd", dev, True),
                                    _arg(dx, n, dt, "dx", dev), _arg(dgamma, c, f, "dgamma", dev), _arg(dbeta, c, f, "dbeta", dev), p, nb,
@@ -436,8 +447,8 @@ def tsm_xent_workspace_bytes(desc):
 
 def tsm_xent_fwd(desc, x, w, bias, labels, loss, lse, ws, stream=None):
     r, d, v, dt, f = desc.rows, desc.features, desc.classes, _TORCH_DTYPE.get(desc.dtype), torch.float32
-    p, nb = _ws(ws)
     dev = _device()
+    p, nb = _buffer(ws, "the workspace", dev)
     _check(lib().tsm_xent_fwd(ctypes.addressof(desc), _arg(x, r * d, dt, "x", dev), _arg(w, v * d, dt, "w", dev),
                               _arg(bias, v, f, "bias", dev), _arg(labels, r, torch.int32, "labels", dev), _arg(loss, r, f, "loss", dev),
                               _arg(lse, r, f, "lse", dev), p, nb, _stream(stream, dev)))
@@ -445,8 +456,8 @@ def tsm_xent_fwd(desc, x, w, bias, labels, loss, lse, ws, stream=None):
 
 def tsm_xent_bwd(desc, x, w, bias, labels, lse, dloss, dx, dw, dbias, ws, stream=None):
     r, d, v, dt, f = desc.rows, desc.features, desc.classes, _TORCH_DTYPE.get(desc.dtype), torch.float32
-    p, nb = _ws(ws)
     dev = _device()
+    p, nb = _buffer(ws, "the workspace", dev)
     _check(lib().tsm_xent_bwd(ctypes.addressof(desc), _arg(x, r * d, dt, "x", dev), _arg(w, v * d, dt, "w", dev),
                               _arg(bias, v, f, "bias", dev), _arg(labels, r, torch.int32, "labels", dev), _arg(lse, r, f, "lse", dev),
                               _arg(dloss, r, f, "dloss", dev), _arg(dx, r * d, dt, "dx", dev), _arg(dw, v * d, dt, "dw", dev),
