@@ -151,9 +151,15 @@ def _ptr(t):
     return t.data_ptr()
 
 
+# The handle of a device's current stream.  torch.cuda.current_stream() builds a Stream object for it (2.5 us of a small call); what saves
+# that is private to torch, and a torch without it goes the public way.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream, dev=None):
-    if stream is None:      # (torch.cuda.current_stream() builds a Stream object for it: 2.5 us of a small call)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if dev is None else dev)
+    if stream is None:
+        dev = torch.cuda.current_device() if dev is None else dev
+        return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 

@@ -77,3 +77,27 @@ def test_a_saved_buffer_on_another_device_is_refused(here, call):
         _calls(near, far)[call]()
     with pytest.raises(ValueError, match="saved: expected at least 64 bytes, got 63"):
         _calls(near, Tensor(63, torch.uint8))[call]()
+
+
+@pytest.mark.parametrize("private", [True, False])
+def test_current_stream_with_and_without_torchs_private_call(monkeypatch, private):
+    """What a torch without the private call offers is asked in its place; without a device given, about the current one."""
+    class Stream:
+        def __init__(self, dev):
+            self.cuda_stream = 1000 + dev
+
+    def handle(dev):
+        return 1000 + dev
+
+    def gone(dev):
+        raise AssertionError("not in this torch")
+    if private:
+        monkeypatch.setattr(B, "_raw_stream", handle)
+        monkeypatch.setattr(torch.cuda, "current_stream", gone)
+    else:
+        monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+        monkeypatch.setattr(B, "_raw_stream", None, raising=False)
+        monkeypatch.setattr(torch.cuda, "current_stream", Stream)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    assert B._stream(None) == 1003 and B._stream(None, 1) == 1001
+    assert B._stream(77) == 77 and B._stream(Stream(5)) == 1005
