@@ -58,8 +58,6 @@ enum { XE_STATS = 0, XE_GRAD = 1, XE_OUT = 2 };
 
 __device__ __forceinline__ bool is_class(int label, long classes) { return label >= 0 && label < classes; }
 
-// exp(v - m) with exp(-inf - -inf) = 0: a column without any weight
-__device__ __forceinline__ float exp_below(float v, float m) { return v == -__builtin_inff() && v == m ? 0.f : __expf(v - m); }
 // joins (m, s) with (m2, s2)
 __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float s2) {
     const float t = fmaxf(m, m2);
