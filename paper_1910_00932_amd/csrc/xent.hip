@@ -32,6 +32,7 @@ struct XentEpi {
     long col0, classes;
     // GRAD
     const float *lse, *dloss;     // (dloss for OUT too, with labels and classes)
+    const float* scale;      // GRAD and OUT, bf16: XScale's factor, where a wavefront does not look for it itself
     long rows;               // OUT: of the whole pass
     bf16_t* G;               // in blocks (X_GROWS): ldg elements per 256 rows, gplane from one part to the next
     long ldg, gplane;
@@ -66,24 +67,64 @@ __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float
 }
 
 // The factor in [1, 2) that bf16 G leaves out of dloss, and what reads G puts back: the mantissa of the first ordinary dloss among the
-// first 64 rows with a label, the same in every tile.  A mean's dloss is one number for all rows, and the entry of a row's label, by far
+// rows with a label, the same in every tile.  A mean's dloss is one number for all rows, and the entry of a row's label, by far
 // its largest, is almost that number: rounded with it, all of them would be off alike, by up to 2^-9 of the whole gradient.
+// Of up to 512 rows every wavefront looks for itself, 64 at a time, most often once; of more, a launch of one block does (us of a training
+// pass without and with it: 128 x 2048 x 1000 29 to 30 and 33 to 34, 1777 x 1000 x 32003 535 and 541), which passes over any number of rows.
+__device__ __forceinline__ bool ordinary(float v) {
+    const uint32_t exponent = (__float_as_uint(v) >> 23) & 0xff;
+    return exponent != 0 && exponent != 0xff;
+}
+__device__ __forceinline__ float mantissa(float v) { return __uint_as_float((__float_as_uint(v) & 0x7fffffu) | 0x3f800000u); }
+static constexpr int X_SCALE_ROWS = 512, X_SCALE_TURN = 4;      // rows that a wavefront looks through; rows per thread and turn of the launch
 struct XScale {
     float up;
-    bool ok;
-    __device__ __forceinline__ void load(const XentEpi& e, long M) {
-        const int lane = threadIdx.x & 63;
-        const long r = lane < M ? lane : M - 1;
-        up = e.dloss[r];
-        ok = is_class(e.labels[r], e.classes);
+    bool ok, found;
+    __device__ __forceinline__ void rows(const XentEpi& e, long from, long M) {
+        const long r = from + (threadIdx.x & 63), at = r < M ? r : M - 1;       // (the last one again)
+        up = e.dloss[at];
+        ok = is_class(e.labels[at], e.classes);
     }
-    __device__ __forceinline__ float get() const {
-        const uint32_t bits = __float_as_uint(up), exponent = (bits >> 23) & 0xff;
-        const uint64_t rows = __ballot(ok && exponent != 0 && exponent != 0xff);
-        const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)bits, rows ? __builtin_ctzll(rows) : 0);
-        return rows ? __uint_as_float((first & 0x7fffffu) | 0x3f800000u) : 1.f;
+    __device__ __forceinline__ void load(const XentEpi& e, long M) {            // ahead of get()
+        found = e.scale != nullptr;
+        if (found) up = *(const __attribute__((address_space(4))) float*)e.scale;
+        else rows(e, 0, M);
+    }
+    __device__ __forceinline__ float get(const XentEpi& e, long M) {
+        if (found) return up;
+        uint64_t count = __ballot(ok && ordinary(up));
+        for (long from = 64; count == 0 && from < M; from += 64) {
+            rows(e, from, M);
+            count = __ballot(ok && ordinary(up));
+        }
+        const float first = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(up), count ? __builtin_ctzll(count) : 0));
+        return count ? mantissa(first) : 1.f;
     }
 };
+__global__ void __launch_bounds__(1024) xent_scale_kernel(const float* __restrict__ dloss, const int32_t* __restrict__ labels, int rows, long classes,
+                                                          float* __restrict__ scale) {
+    __shared__ int s_first;
+    if (threadIdx.x == 0) s_first = rows;
+    __syncthreads();
+    for (long base = 0; base < rows; base += 1024 * X_SCALE_TURN) {
+        bool use[X_SCALE_TURN];
+#pragma unroll
+        for (int i = 0; i < X_SCALE_TURN; ++i) {
+            const long r = base + i * 1024 + threadIdx.x, at = r < rows ? r : rows - 1;
+            use[i] = is_class(labels[at], classes) && ordinary(dloss[at]) && r < rows;
+        }
+#pragma unroll
+        for (int i = 0; i < X_SCALE_TURN; ++i)
+            if (use[i]) {
+                atomicMin(&s_first, (int)(base + i * 1024 + threadIdx.x));
+                break;
+            }
+        __syncthreads();
+        if (s_first < rows) break;                              // (the same for all: the next turn writes behind another barrier)
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *scale = s_first < rows ? mantissa(dloss[s_first]) : 1.f;
+}
 
 // ---- tiles: BM x BN results of wavefronts that share the operands through LDS ---------------------------------------------
 // Operands come 64 steps of K at a time (32 for those in three parts), straight from memory into an LDS stage while another is
@@ -643,7 +684,7 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
         // stages of 32 K, up to four steps ahead, gained nothing (18.0 against 17.6), four wavefronts of 128 x 128 lose (20.4).  Persistent
         // blocks that load a tile's first steps behind the epilogue before are no faster (that epilogue is 3 of 58 us at 2048 features).
         if (steps > 1) next_step(1);
-        if constexpr (SCALE && MODE == XE_OUT) factor = scale.get();
+        if constexpr (SCALE && MODE == XE_OUT) factor = scale.get(a.e, a.e.rows);
         if (steps > 0) {
             if (steps > 1) x_wait<NP>();
             else x_wait<0>();
@@ -754,7 +795,7 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
         // before is free.
         if (steps > 1) next_step(1);
         if (NS > 3 && steps > 2) next_step(2);
-        if constexpr (SCALE && MODE == XE_OUT) factor = scale.get();
+        if constexpr (SCALE && MODE == XE_OUT) factor = scale.get(a.e, a.e.rows);
         int stage = 0;
         for (int s = 0; s < steps; ++s) {
             if (s + NS - 2 < steps) x_wait<(NS - 2) * NP>();
@@ -811,7 +852,7 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
     if constexpr (MODE != XE_OUT) {
         if constexpr (SCALE) {
             scale.load(a.e, a.M);
-            factor = scale.get();
+            factor = scale.get(a.e, a.M);
         }
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
@@ -1167,7 +1208,7 @@ struct XentPlan {
     long ntiles, mtiles;          // tiles of s: of all columns, of the rows, at most
     long ldg, gplane, xplane, wplane, lddb;
     size_t fwd_bytes, bwd_bytes;
-    size_t o_x, o_w, o_part, o_picked, o_G, o_acc, o_dw, o_dbias, o_mask;
+    size_t o_x, o_w, o_part, o_picked, o_G, o_acc, o_dw, o_dbias, o_mask, o_scale;
 };
 
 static constexpr size_t XENT_G_BYTES = (size_t)512 << 20;   // of a piece of G, at most (a piece has 1024 classes at least)
@@ -1264,6 +1305,7 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     p.o_dw = b.used; b.take(p.zdw > 1 ? (size_t)p.zdw * piece * D * 4 : 0);
     p.o_dbias = b.used; b.take((size_t)p.mtiles * p.lddb * 4);
     p.o_mask = b.used; b.take((size_t)(R + 255) / 256 * 4 * 8);
+    p.o_scale = b.used; b.take(f32 || R <= X_SCALE_ROWS ? 0 : 4);
     p.bwd_bytes = b.used;
     return p;
 }
@@ -1424,6 +1466,12 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
     // fp32 results are added up where they go
     float *acc = F32 && p.zdx == 1 ? (float*)dx : (float*)(ws + p.o_acc), *dwp = (float*)(ws + p.o_dw), *dbp = (float*)(ws + p.o_dbias);
     uint64_t* mask = (uint64_t*)(ws + p.o_mask);
+    const float* scale = nullptr;
+    if (!F32 && R > X_SCALE_ROWS) {
+        scale = (const float*)(ws + p.o_scale);
+        xent_scale_kernel<<<dim3(1), dim3(1024), 0, s>>>(dloss, labels, d->rows, V, (float*)(ws + p.o_scale));
+        TSM_TRY(check_launch("xent_scale"));
+    }
     const bf16_t *xo, *wo;
     for (long c = 0; c < p.pieces; ++c) {
         const long v0 = c * p.piece, n = V - v0 < p.piece ? V - v0 : p.piece;
@@ -1434,7 +1482,7 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
         a.aplane = p.xplane; a.bplane = p.wplane;
         a.M = R; a.N = n; a.K = p.depth;
         a.e.bias = bias; a.e.labels = labels; a.e.classes = V; a.e.col0 = v0;
-        a.e.lse = lse; a.e.dloss = dloss; a.e.G = G; a.e.ldg = p.ldg; a.e.gplane = p.gplane;
+        a.e.lse = lse; a.e.dloss = dloss; a.e.scale = scale; a.e.G = G; a.e.ldg = p.ldg; a.e.gplane = p.gplane;
         a.e.mask = dw && c == 0 ? mask : nullptr;
         const bool both = dx && dw && p.sizedx == X_SMALL && p.sizedw == X_SMALL && x_tiles(R, D, 64) * p.zdx + x_tiles(n, D, 64) * p.zdw + n / 256 < X_LAUNCH;
         XColumns sums{};
@@ -1470,6 +1518,7 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
         gx.aplane = gw.aplane = p.gplane;
         gx.e.labels = gw.e.labels = labels;
         gx.e.dloss = gw.e.dloss = dloss;
+        gx.e.scale = gw.e.scale = scale;
         gx.e.classes = gw.e.classes = V;
         gx.e.rows = gw.e.rows = R;
         gx.ldb = gw.ldb = p.pitch;

@@ -311,3 +311,63 @@ def test_classes_behind_the_last_whole_round_of_tiles(shape, dtype, biased, igno
     labels = _labels(R, V, 4, ignored)
     inputs, outs = _run(R, D, V, dtype, values((V,), 2, "f32") if biased else None, labels)
     _check(inputs, outs, labels, dtype)
+
+
+@pytest.mark.parametrize("shape,lead", [((200, 64, 3001), 64), ((300, 264, 5000), 130), ((512, 72, 3001), 390), ((640, 72, 3001), 513), ((4500, 64, 3001), 4200), ((9000, 48, 3001), 8400)])
+def test_rows_in_front_that_count_for_nothing_do_not_shift_the_gradients(shape, lead):
+    """A batch whose leading rows have no label, or a dloss of zero, and whose other rows share one dloss half way between two bf16
+    values.  Bounds as in test_one_dloss_for_all_rows_does_not_shift_the_gradients: G without dloss's mantissa, rounded in 64 bits, says
+    where the size has to be, but for the projection's share of the results' rounding; with dloss itself rounded it would be off by 2^-8."""
+    R, D, V = shape
+    labels = _labels(R, V, 9, False)
+    labels[:lead:2] = -1
+    d = B.XentDesc(rows=R, features=D, classes=V, dtype=CDT["bf16"])
+    x, xn = values((R, D), 0, "bf16")
+    w, wn = values((V, D), 1, "bf16", scale=1 / np.sqrt(D))
+    lab, up = torch.from_numpy(labels).cuda(), torch.full((R,), (1 + 2.0 ** -8) / 256, device="cuda")
+    up[1:lead:2] = 0.0
+    loss, lse = torch.empty(R, device="cuda"), torch.empty(R, device="cuda")
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(V, device="cuda")
+    ws = scratch(B.tsm_xent_workspace_bytes(d))
+    B.tsm_xent_fwd(d, x, w, None, lab, loss, lse, ws)
+    B.tsm_xent_bwd(d, x, w, None, lab, lse, up, dx, dw, db, ws)
+    xn, labels, upn = xn[lead:], labels[lead:], up.double().cpu().numpy()[lead:]       # (the rows in front add nothing)
+    assert not bool(dx[:lead].any())
+    rdx, rdw, rdb = H.xent_bwd(xn, wn, None, labels, upn)
+    G = H.xent_grad(xn, wn, None, labels, upn)
+    rounded = torch.from_numpy(G / (1 + 2.0 ** -8)).to(torch.bfloat16).double().numpy() * (1 + 2.0 ** -8)
+    for got, want, like, what in ((dx[lead:], rdx, rounded @ wn, "dx"), (dw, rdw, rounded.T @ xn, "dw"), (db, rdb, rdb, "dbias")):
+        want = want.ravel()
+        size, right = (v.ravel() @ want / (want @ want) - 1 for v in (got.double().cpu().numpy(), like))
+        n = (want @ want) ** 2 / (want ** 2 @ want ** 2)
+        assert abs(size - right) < 4 * 2.0 ** -8 / np.sqrt(n), (what, size, right, n)
+        assert abs(size) < 2.0 ** -10, (what, size)
+
+
+def test_dloss_of_the_first_row_that_counts_in_a_graph():
+    """The factor follows the inputs of a replay: labels and dloss change between them."""
+    R, D, V = 700, 72, 300
+    d = B.XentDesc(rows=R, features=D, classes=V, dtype=CDT["bf16"])
+    x, _ = values((R, D), 0, "bf16")
+    w, _ = values((V, D), 1, "bf16", scale=1 / np.sqrt(D))
+    full = torch.from_numpy(_labels(R, V, 9, False)).cuda()
+    lab, up = full.clone(), torch.ones(R, device="cuda")
+    loss, lse = torch.empty(R, device="cuda"), torch.empty(R, device="cuda")
+    outs = [torch.empty_like(x), torch.empty_like(w), torch.empty(V, device="cuda")]
+    eager = [torch.empty_like(t) for t in outs]
+    ws, ws2 = scratch(B.tsm_xent_workspace_bytes(d)), scratch(B.tsm_xent_workspace_bytes(d))
+    B.tsm_xent_fwd(d, x, w, None, lab, loss, lse, ws)
+    B.tsm_xent_bwd(d, x, w, None, lab, lse, up, *outs, ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.tsm_xent_bwd(d, x, w, None, lab, lse, up, *outs, ws)
+    for lead, size in ((0, 1.75 / 700), (100, (1 + 2.0 ** -8) / 256), (690, 0.3), (700, 1.0)):
+        lab.copy_(full)
+        lab[:lead] = -1
+        up.fill_(size)
+        g.replay()
+        B.tsm_xent_bwd(d, x, w, None, lab, lse, up, *eager, ws2)
+        torch.cuda.synchronize()
+        for a, b in zip(outs, eager):
+            assert torch.equal(a, b), lead
