@@ -96,3 +96,42 @@ def test_statistics_are_optional_and_bits_repeat():
         y = Guarded((77, C), torch.bfloat16)
         B.tsm_layernorm_fwd(d, xd, gd, bd, y.t, None, None)
         assert np.array_equal(y.np(), a[0])
+
+
+@pytest.mark.parametrize("dtype,C,x0,spread", [("f32", 1 << 23, 0.3, 0.0), ("f32", 3 << 21, 1.0, 0.1), ("bf16", (1 << 24) + 1, 0.3, 0.02)])
+def test_sums_over_very_long_rows(dtype, C, x0, spread):
+    """Values of one sign, or one value, in which every rounding of a long sum leans the same way.  A value is among at most n = 400
+    additions in turn -- 8 of a vector, 64, 64 and up to 256 of them, the wavefront's and the block's -- and the sums are off by n units of
+    2^-24 of their magnitudes, whatever C.  As above, xhat is off by c = n units of mean |x|, and a unit of |x|, times rstd."""
+    rng = np.random.default_rng(5)
+    t = torch.from_numpy((x0 + spread * rng.standard_normal((1, C))).astype(np.float32)).to(TDT[dtype])
+    x, g, b = t.double().numpy(), np.full(C, 0.75), np.full(C, 0.5)
+    dyt = torch.from_numpy((0.3 + spread * rng.standard_normal((1, C))).astype(np.float32)).to(TDT[dtype])
+    dy = dyt.double().numpy()
+    d = B.LayerNormDesc(rows=1, C=C, dtype=CDT[dtype], eps=EPS)
+    xd, dyd, gd, bd = t.cuda(), dyt.cuda(), torch.full((C,), 0.75, device="cuda"), torch.full((C,), 0.5, device="cuda")
+    y, mean, rstd = Guarded((1, C), TDT[dtype]), Guarded((1,), torch.float32), Guarded((1,), torch.float32)
+    B.tsm_layernorm_fwd(d, xd, gd, bd, y.t, mean.t, rstd.t)
+    n = 400
+    rmean = x.mean()
+    var = ((x - rmean) ** 2).mean()
+    rrstd = (var + EPS) ** -0.5
+    m = n * U * np.abs(x).mean() + U * abs(rmean)
+    c = m + U * np.abs(x).max()
+    rel = ((n + 4) * U * var + 2 * c * np.sqrt(var) + c ** 2) / (var + EPS) + 4 * U
+    within(mean.np(), np.array([rmean]), m, "mean")
+    within(rstd.np(), np.array([rrstd]), rel * rrstd, "rstd")
+    xhat = (x - rmean) * rrstd
+    exh = c * rrstd + (rel + 4 * U) * (np.abs(xhat) + c * rrstd)
+    ry = xhat * g + b
+    within(y.np(), ry, g * exh + 4 * U * (np.abs(g * xhat) + np.abs(b)) + HALF[dtype] * np.abs(ry), "y")
+    dx, dg, db = Guarded((1, C), TDT[dtype]), Guarded((C,), torch.float32), Guarded((C,), torch.float32)
+    B.tsm_layernorm_bwd(d, xd, dyd, gd, mean.t, rstd.t, dx.t, dg.t, db.t, scratch(B.tsm_layernorm_workspace_bytes(d)))
+    v = dy * g
+    m1, m2 = v.mean(), (v * xhat).mean()
+    rdx = rrstd * (v - m1 - xhat * m2)
+    e1 = (n + 2) * U * np.abs(v).mean()
+    e2 = (n + 4) * U * np.abs(v * xhat).mean() + (np.abs(v) * exh).mean()
+    size = np.abs(v) + np.abs(v).mean() + np.abs(xhat) * (abs(m2) + e2)
+    bound = rrstd * (e1 + np.abs(xhat) * e2 + exh * (abs(m2) + e2) + 8 * U * size) + rel * rrstd * size
+    within(dx.np(), rdx, bound + HALF[dtype] * np.abs(rdx), "dx")
