@@ -7,6 +7,7 @@
 // one read on (R vectors of 16 bytes per lane), so mean, centred variance and result cost one pass; all sums are fp32.  The
 // weights' gradients are column sums over all rows: every block keeps its rows' share in registers, writes one row of a
 // partial buffer at its end, and a second launch adds the rows in a fixed order.
+#include <algorithm>
 #include "internal.h"
 #include "args.h"
 #include "vec_any.h"
@@ -325,30 +326,35 @@ __global__ void __launch_bounds__(LN_NT) ln_bwd_cols_kernel(const T* __restrict_
     }
 }
 
-// dgamma, dbeta = the sums of the partial rows: 64 columns x 16 row lanes per block.
+// dgamma, dbeta = the sums of the partial rows: 64 columns x 16 row lanes per block and turn.
 __global__ void __launch_bounds__(1024) ln_join_kernel(const float* __restrict__ partial, int nrows, int C, float* __restrict__ dgamma,
                                                        float* __restrict__ dbeta) {
     __shared__ float red[16][64];
     const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-    const long w = (long)blockIdx.x * 64 + tx, w2 = 2L * C;
-    float s = 0.f;
-    if (w < w2)
+    const long w2 = 2L * C;
+    for (long w0 = blockIdx.x * 64L; w0 < w2; w0 += gridDim.x * 64L) {
+        const long w = w0 + tx;
+        float s = 0.f;
+        if (w < w2)
 #pragma unroll 4
-        for (int r = ty; r < nrows; r += 16) s += partial[(size_t)r * w2 + w];
-    red[ty][tx] = s;
-    __syncthreads();
-    if (ty == 0 && w < w2) {
-        float t = 0.f;
+            for (int r = ty; r < nrows; r += 16) s += partial[(size_t)r * w2 + w];
+        if (w0 != blockIdx.x * 64L) __syncthreads();            // (the turn before has been read)
+        red[ty][tx] = s;
+        __syncthreads();
+        if (ty == 0 && w < w2) {
+            float t = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) t += red[r][tx];
-        if (w < C) dgamma[w] = t;
-        else dbeta[w - C] = t;
+            for (int r = 0; r < 16; ++r) t += red[r][tx];
+            if (w < C) dgamma[w] = t;
+            else dbeta[w - C] = t;
+        }
     }
 }
 
 // ---- host --------------------------------------------------------------------------------
 // Blocks keep gamma and beta over their rows (200704 x 256 bf16: 512 52, 1024 37, 2048 36, 4096 48, 8192 67 us).
 static constexpr int LN_FWD_BLOCKS = 2048;
+static constexpr long LN_JOIN_BLOCKS = 1 << 16;      // (2^32 threads are more than a launch has: 2 x 2^27 columns in one turn)
 static constexpr int LN_BLOCKS = 512;     // of the backward pass: two per CU, each writes one partial row (25088 x 2048 bf16: 256 73, 512 56, 1024 63 us)
 
 // Lanes and vectors per lane of a row; 0 lanes: the row exceeds a block's registers.  Few vectors per lane keep many rows in
@@ -434,7 +440,7 @@ static int ln_bwd(const tsm_layernorm_desc* d, const void* x, const void* dy, co
 #undef CALL
     TSM_TRY(check_launch("layernorm_bwd"));
     if (nb == 1) return TSM_OK;
-    ln_join_kernel<<<dim3((unsigned)((2L * d->C + 63) / 64)), dim3(1024), 0, s>>>(partial, nb, d->C, dgamma, dbeta);
+    ln_join_kernel<<<dim3((unsigned)std::min((2L * d->C + 63) / 64, LN_JOIN_BLOCKS)), dim3(1024), 0, s>>>(partial, nb, d->C, dgamma, dbeta);
     return check_launch("layernorm_join");
 }
 

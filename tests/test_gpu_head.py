@@ -303,3 +303,35 @@ def test_binding_refuses_other_sizes_types_and_devices(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     with pytest.raises(ValueError, match="current device"):
         B.tsm_layernorm_fwd(h.ln, h.f, h.gamma, h.beta, o["z"], None, None, stream=0)
+
+
+def test_layernorm_weight_gradients_of_very_long_rows():
+    """2 x 2^27 sums of partial rows, as many threads as no launch has.  Bounds: dgamma and dbeta are sums of 33 terms, of which dgamma's are
+    off by 4 units; dx as in the layer norm's own tests, with chains of 400 additions."""
+    rows, C = 33, 1 << 27
+    x, dy = (torch.randn(rows, C, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    gamma = torch.randn(C, device="cuda")
+    mean, rstd = torch.linspace(-0.5, 0.5, rows, device="cuda"), torch.linspace(0.5, 2.0, rows, device="cuda")
+    dx, dg, db = torch.empty_like(x), torch.full((C,), float("nan"), device="cuda"), torch.full((C,), float("nan"), device="cuda")
+    d = B.LayerNormDesc(rows=rows, C=C, dtype=B.TSM_BF16, eps=EPS)
+    B.tsm_layernorm_bwd(d, x, dy, gamma, mean, rstd, dx, dg, db, scratch(B.tsm_layernorm_workspace_bytes(d)))
+    s1, s2, a1, a2 = (torch.zeros(rows, dtype=torch.float64, device="cuda") for _ in range(4))
+    m, r = mean.double()[:, None], rstd.double()[:, None]
+    step = 1 << 23
+    for c in range(0, C, step):
+        up = dy[:, c:c + step].double()
+        xhat = (x[:, c:c + step].double() - m) * r
+        prod, v = up * xhat, up * gamma[c:c + step].double()
+        assert bool(((dg[c:c + step].double() - prod.sum(0)).abs() <= 68 * U * prod.abs().sum(0)).all()), c
+        assert bool(((db[c:c + step].double() - up.sum(0)).abs() <= 64 * U * up.abs().sum(0)).all()), c
+        s1 += v.sum(1)
+        s2 += (v * xhat).sum(1)
+        a1 += v.abs().sum(1)
+        a2 += (v * xhat).abs().sum(1)
+    s1, s2, a1, a2 = s1[:, None] / C, s2[:, None] / C, a1[:, None] / C, a2[:, None] / C
+    for c in (0, C // 2, C - 5000):
+        v = dy[:, c:c + 5000].double() * gamma[c:c + 5000].double()
+        xhat = (x[:, c:c + 5000].double() - m) * r
+        want = r * (v - s1 - xhat * s2)
+        bound = r * (402 * U * a1 + xhat.abs() * 408 * U * a2 + 8 * U * (v.abs() + a1 + xhat.abs() * a2))
+        within(dx[:, c:c + 5000].double().cpu().numpy(), want.cpu().numpy(), (bound + HALF["bf16"] * want.abs()).cpu().numpy(), "dx %d" % c)
