@@ -354,6 +354,9 @@ __global__ void __launch_bounds__(1024) ln_join_kernel(const float* __restrict__
 // ---- host --------------------------------------------------------------------------------
 // Blocks keep gamma and beta over their rows (200704 x 256 bf16: 512 52, 1024 37, 2048 36, 4096 48, 8192 67 us).
 static constexpr int LN_FWD_BLOCKS = 2048;
+// Rows that a thread adds up in turn for dgamma and dbeta, at most; of more rows there are more blocks and partial rows.  (512 blocks for all: 2^26
+// rows of 8 channels, 8192 in turn, lose 1.2e-4 of a sum of one sign, and twice that of twice the rows.)
+static constexpr int64_t LN_CHAIN = 512;
 static constexpr long LN_JOIN_BLOCKS = 1 << 16;      // (2^32 threads are more than a launch has: 2 x 2^27 columns in one turn)
 static constexpr int LN_BLOCKS = 512;     // of the backward pass: two per CU, each writes one partial row (25088 x 2048 bf16: 256 73, 512 56, 1024 63 us)
 
@@ -394,12 +397,10 @@ static int ln_check(const tsm_layernorm_desc* d, const char* who) {
 static int ln_bwd_blocks(const tsm_layernorm_desc* d) {
     int L, R;
     ln_shape(d->C, d->dtype, &L, &R);
-    if (L == 0) {   // row shares of ln_bwd_cols_kernel
-        const int64_t share = (d->rows + 31) / 32;
-        return (int)(share < 16 ? share : 16);
-    }
+    if (L == 0)     // row shares of ln_bwd_cols_kernel, by four wavefronts each
+        return (int)std::min(std::max(std::min((d->rows + 31) / 32, (int64_t)16), (d->rows + 4 * LN_CHAIN - 1) / (4 * LN_CHAIN)), (int64_t)65535);
     const int64_t groups = (d->rows + LN_NT / L - 1) / (LN_NT / L);
-    return groups <= 2 ? 1 : (int)(groups < LN_BLOCKS ? groups : LN_BLOCKS);
+    return groups <= 2 ? 1 : (int)std::min(std::max(std::min(groups, (int64_t)LN_BLOCKS), (groups + LN_CHAIN - 1) / LN_CHAIN), (int64_t)1 << 22);
 }
 
 static size_t ln_ws_bytes(const tsm_layernorm_desc* d) { return align_up((size_t)ln_bwd_blocks(d) * 2 * d->C * sizeof(float)); }

@@ -135,3 +135,24 @@ def test_sums_over_very_long_rows(dtype, C, x0, spread):
     size = np.abs(v) + np.abs(v).mean() + np.abs(xhat) * (abs(m2) + e2)
     bound = rrstd * (e1 + np.abs(xhat) * e2 + exh * (abs(m2) + e2) + 8 * U * size) + rel * rrstd * size
     within(dx.np(), rdx, bound + HALF[dtype] * np.abs(rdx), "dx")
+
+
+@pytest.mark.parametrize("rows,C", [(1 << 26, 8), (90001, 4100)])
+def test_weight_gradients_of_very_many_rows(rows, C):
+    """One value in all rows, so that every rounding of a long sum leans the same way.  A term of dbeta is among at most 512 additions of its
+    thread, 16 of its block, and n / 16 and 16 of the n blocks' sums, of which a block has 512 times 16 or, of rows past the registers, 512
+    times 4 rows: as many units of 2^-24.  dgamma's terms are off by a few units more."""
+    d = B.LayerNormDesc(rows=rows, C=C, dtype=B.TSM_F32, eps=EPS)
+    x = torch.full((rows, C), 0.75, device="cuda")
+    dy = torch.full((rows, C), 0.2385874, device="cuda")
+    gamma = torch.ones(C, device="cuda")
+    mean, rstd = torch.full((rows,), 0.25, device="cuda"), torch.full((rows,), 1.7, device="cuda")
+    dx, dg, db = torch.empty_like(x), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    B.tsm_layernorm_bwd(d, x, dy, gamma, mean, rstd, dx, dg, db, scratch(B.tsm_layernorm_workspace_bytes(d)))
+    blocks = rows / 512 / (4 if C > 4096 else 16)
+    k = 512 + 16 + max(blocks, 512) / 16 + 16
+    up = float(dy[0, 0])
+    want = rows * up
+    within(db.double().cpu().numpy(), np.full(C, want), k * U * want, "dbeta")
+    want = rows * up * 0.5 * float(rstd[0])
+    within(dg.double().cpu().numpy(), np.full(C, want), (k + 8) * U * want, "dgamma")
