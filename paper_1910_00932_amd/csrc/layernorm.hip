@@ -11,6 +11,7 @@
 #include "internal.h"
 #include "args.h"
 #include "vec_any.h"
+#include "long_sum.h"
 
 namespace tsm {
 
@@ -94,27 +95,8 @@ __global__ void __launch_bounds__(LN_NT) ln_fwd_kernel(const T* __restrict__ x, 
     }
 }
 
-// A thread's sum over a row of any length: what it adds goes up a level after 64 additions, and again after 64 of those, so that none of 2^30
-// values is the last of more than some 400 in turn.  (One register for all lets a row of 2^23 times 0.3 lose 3e-4 of its mean, of 2^25 1e-3,
-// and the variance with it.)
-struct LnLongSum {
-    float s0 = 0.f, s1 = 0.f, s2 = 0.f;
-    int n = 0;
-    __device__ __forceinline__ void add(float v) {
-        s0 += v;
-        if ((++n & 63) == 0) {
-            s1 += s0;
-            s0 = 0.f;
-            if ((n & 4095) == 0) {
-                s2 += s1;
-                s1 = 0.f;
-            }
-        }
-    }
-    __device__ __forceinline__ float get() const { return s0 + (s1 + s2); }
-};
-
-// Rows longer than the registers of a block: one block per row, which reads it three times (from L2 after the first).
+// Rows longer than the registers of a block: one block per row, which reads it three times (from L2 after the first).  (One register for a
+// thread's share lets a row of 2^23 times 0.3 lose 3e-4 of its mean, of 2^25 1e-3, and the variance with it.)
 template <typename T>
 __global__ void __launch_bounds__(LN_NT) ln_fwd_long_kernel(const T* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ beta,
                                                             T* __restrict__ y, float* __restrict__ mean_out, float* __restrict__ rstd_out,
@@ -123,7 +105,7 @@ __global__ void __launch_bounds__(LN_NT) ln_fwd_long_kernel(const T* __restrict_
     __shared__ float red[2][LN_NT / 64];
     for (long row = blockIdx.x; row < rows; row += gridDim.x) {
         const T* xr = x + row * C;
-        LnLongSum s;
+        LongSum s;
         for (int c0 = threadIdx.x * VE; c0 < C; c0 += LN_NT * VE) {
             const auto raw = raw_load<T, VE>(xr + c0, C - c0);
             float t = 0.f;
@@ -132,7 +114,7 @@ __global__ void __launch_bounds__(LN_NT) ln_fwd_long_kernel(const T* __restrict_
             s.add(t);
         }
         const float mean = ln_sum<LN_NT>(s.get(), red[0]) / (float)C;
-        LnLongSum q;
+        LongSum q;
         for (int c0 = threadIdx.x * VE; c0 < C; c0 += LN_NT * VE) {
             const auto raw = raw_load<T, VE>(xr + c0, C - c0);
             float t = 0.f;
@@ -253,7 +235,7 @@ __global__ void __launch_bounds__(LN_NT) ln_bwd_long_kernel(const T* __restrict_
     __shared__ float red[2][LN_NT / 64];
     for (long row = blockIdx.x; row < rows; row += gridDim.x) {
         const float mean = mean_in[row], rstd = rstd_in[row];
-        LnLongSum s1, s2;
+        LongSum s1, s2;
         for (int c0 = threadIdx.x * VE; c0 < C; c0 += LN_NT * VE) {
             const auto rx = raw_load<T, VE>(x + row * C + c0, C - c0);
             const auto rd = raw_load<T, VE>(dy + row * C + c0, C - c0);

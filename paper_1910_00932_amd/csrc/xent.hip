@@ -16,6 +16,7 @@
 #include "internal.h"
 #include "args.h"
 #include "vec_any.h"
+#include "long_sum.h"
 
 namespace tsm {
 
@@ -1059,14 +1060,18 @@ template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
 __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(XentArgs a) {
     xent_tile<C, MODE, AKIND, BKIND, SPLIT, DB>(a, blockIdx.x, gridDim.x);
 }
-// out[c] = sum of the rows of part [rows][ld]
+// out[c] = sum of the rows of part [rows][ld], eight and then any number of them at a time
 __device__ __forceinline__ void column_sum(const float* __restrict__ part, long rows, long ld, long n, float* __restrict__ out, long block) {
     const long c = block * 256 + threadIdx.x;
     if (c >= n) return;
-    float s = 0.f;
-#pragma unroll 8
-    for (long r = 0; r < rows; ++r) s += part[r * ld + c];
-    out[c] = s;
+    LongSum s;
+    for (long r = 0; r < rows; r += 8) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t += r + i < rows ? part[(r + i) * ld + c] : 0.f;
+        s.add(t);
+    }
+    out[c] = s.get();
 }
 struct XColumns {
     const float* part;

@@ -371,3 +371,21 @@ def test_dloss_of_the_first_row_that_counts_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(outs, eager):
             assert torch.equal(a, b), lead
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_bias_gradient_of_very_many_rows(dtype):
+    """One value in all rows, so that every rounding of a long sum leans the same way: x and the logits are zero, p is 1/2, and G of the class
+    that no row has is dloss / 2, of the other minus that.  A term is among some 12 additions of its tile, 8 and 64 and 64 of the tiles' sums
+    and at most 64 behind those: k = 212 units of 2^-24; p and G are off by 16 (two exponentials' and a logarithm's)."""
+    R, D, V = 1 << 24, 1, 2
+    d = B.XentDesc(rows=R, features=D, classes=V, dtype=CDT[dtype])
+    x, w = torch.zeros(R, D, dtype=TDT[dtype], device="cuda"), torch.ones(V, D, dtype=TDT[dtype], device="cuda")
+    lab, up = torch.ones(R, dtype=torch.int32, device="cuda"), torch.full((R,), 0.4771748, device="cuda")
+    loss, lse, db = torch.empty(R, device="cuda"), torch.empty(R, device="cuda"), torch.empty(V, device="cuda")
+    ws = torch.empty(B.tsm_xent_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    B.tsm_xent_fwd(d, x, w, None, lab, loss, lse, ws)
+    B.tsm_xent_bwd(d, x, w, None, lab, lse, up, None, None, db, ws)
+    want = np.array([0.5, -0.5]) * R * float(up[0])
+    within(db.double().cpu().numpy(), want, (212 + 16) * U * np.abs(want), "dbias")
+    within(loss[::4097].double().cpu().numpy(), np.full(R // 4097 + 1, np.log(2.0)), 16 * U, "loss")
