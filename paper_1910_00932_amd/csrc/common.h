@@ -5,6 +5,7 @@
 #include <stddef.h>
 #include <stdio.h>
 #include "../../include/tsm.h"
+#include "per_device.h"
 
 namespace tsm {
 
@@ -13,6 +14,8 @@ void set_error(const char* fmt, ...);
 int fail(int code, const char* fmt, ...);
 // Checks the launch error state of the calling thread after a kernel launch.
 int check_launch(const char* what);
+// Raises a kernel's limit of dynamic LDS to what a CU has, on the current device; once: of this kernel.
+int raise_lds_limit(const void* kernel, OncePerDevice& once, const char* what);
 bool profiling_active();   // per-launch timing is on (every launch must then stay on the profiled stream)
 
 #define TSM_TRY(expr)                 \

@@ -645,12 +645,8 @@ static int ks_launch(KsArgs& a, hipStream_t s) {
     constexpr size_t smem = (size_t)KS * (TM + TN) * 128 + TM * sizeof(KsRow) + 2 * KS * TN * sizeof(float);
     static_assert(smem <= 160 * 1024, "LDS budget");
     auto kern = ksplit_kernel<T, MI, NJ, KS, DGRAD, RAG>;
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "ksplit: cannot raise dynamic LDS limit");
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kern, lds, "ksplit"));
     a.mtiles = ks_classes(a, DGRAD, TM);
     a.ntiles = (a.Cd + TN - 1) / TN;
     a.by_n = a.w_bytes > a.src_bytes;

@@ -2505,12 +2505,8 @@ static int launch_igemm(IgemmArgs& a, const char* name, hipStream_t s) {
     a.ntiles = (a.Cd + BN - 1) / BN;
     size_t smem = (size_t)2 * (BM + BN) * LDK * sizeof(bf16_t) + (size_t)2 * BM * sizeof(RowInfo);
     auto kern = igemm_kernel<BM, BN, WM, WN, DGRAD, PF, MINB>;
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "igemm: cannot raise dynamic LDS limit");
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kern, lds, "igemm"));
     const int grid = igemm_grid(mtiles, a.Cd, BN, MINB);
     hipLaunchKernelGGL(kern, dim3(grid), dim3(256), smem, s, a);
     return check_launch(name);   // class names carry the tile shape so that they map one-to-one onto kernel symbols
@@ -2523,12 +2519,8 @@ static int launch_igemm_ring_s(IgemmArgs& a, const char* name, hipStream_t s) {
     constexpr size_t smem = ring_smem(BM, BN, WM, WN, STREAM);   // operand stages, staging tile of one epilogue pass, statistics slots, two row buffers
     static_assert(smem <= 160 * 1024, "LDS budget");
     auto kern = igemm_ring_kernel<BM, BN, WM, WN, DGRAD, STREAM, CADD, MBITS>;
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "igemm: cannot raise dynamic LDS limit");
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kern, lds, "igemm"));
     const int grid = igemm_grid(mtiles, a.Cd, BN, 1);
     hipLaunchKernelGGL(kern, dim3(grid), dim3(WM * WN * 64), smem, s, a);
     return check_launch(name);
@@ -2643,12 +2635,8 @@ static bool c64_eligible(const IgemmArgs& a) {
 template <bool DGRAD, bool STREAM>
 static int launch_c64_s(IgemmArgs& a, hipStream_t s) {
     auto kern = conv3x3_c64_kernel<DGRAD, STREAM>;
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "conv3x3_c64: cannot raise dynamic LDS limit");
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kern, lds, "conv3x3_c64"));
     const long rows = (long)a.F * a.Hd * a.Wd;
     const int grid = igemm_grid((int)((rows + C64_BM - 1) / C64_BM), 64, 64, 1);
     hipLaunchKernelGGL(kern, dim3(grid), dim3(512), C64_SMEM, s, a);
@@ -2839,12 +2827,8 @@ static bool stem_eligible(const IgemmArgs& a) {
 template <bool STREAM>
 static int launch_stem_pw(IgemmArgs& a, hipStream_t s) {
     auto kern = stem_pw_kernel<STREAM>;
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "stem_pw: cannot raise dynamic LDS limit");
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kern, lds, "stem_pw"));
     const long rows = (long)a.F * a.Hd * a.Wd;
     const int grid = igemm_grid((int)((rows + STEM_BM - 1) / STEM_BM), 64, 64, 1);
     hipLaunchKernelGGL(kern, dim3(grid), dim3(512), SPW_SMEM, s, a);
@@ -2854,12 +2838,8 @@ static int launch_stem_pw(IgemmArgs& a, hipStream_t s) {
 template <bool STREAM>
 static int launch_stem_s(IgemmArgs& a, hipStream_t s) {
     auto kern = stem_s2d_kernel<STREAM>;
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "stem_s2d: cannot raise dynamic LDS limit");
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kern, lds, "stem_s2d"));
     const long rows = (long)a.F * a.Hd * a.Wd;
     const int grid = igemm_grid((int)((rows + STEM_BM - 1) / STEM_BM), 64, 64, 1);
     hipLaunchKernelGGL(kern, dim3(grid), dim3(512), STEM_SMEM, s, a);
@@ -2899,12 +2879,8 @@ static bool pw_fwd_eligible(const IgemmArgs& a) {
 template <int KC, bool STREAM, bool AFF = false>
 static int launch_pw_fwd(IgemmArgs& a, hipStream_t s) {
     auto kern = pw_fwd_kernel<KC, STREAM, AFF>;
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "pw_fwd: cannot raise dynamic LDS limit");
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kern, lds, "pw_fwd"));
     const long rows = (long)a.F * a.Hd * a.Wd;
     const int grid = igemm_grid((int)((rows + 255) / 256), a.Cd, 128, 1);      // as the general kernel with 256 x 128 tiles
     if (grid % (a.Cd / PwD<KC>::NB) != 0) return fail(TSM_ERR_LAUNCH, "pw_fwd: grid does not split over the parts of the result");
@@ -2925,12 +2901,8 @@ static bool pw_dgrad_eligible(const IgemmArgs& a) {
 template <int KC, bool STREAM, bool CADD = false>
 static int launch_pw_dgrad(IgemmArgs& a, hipStream_t s) {
     auto kern = pw_dgrad_kernel<KC, STREAM, CADD>;
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "pw_dgrad: cannot raise dynamic LDS limit");
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kern, lds, "pw_dgrad"));
     const long rows = (long)a.F * a.Hd * a.Wd;
     const int grid = igemm_grid((int)((rows + 255) / 256), a.Cd, 128, 1);      // as the general kernel with 256 x 128 tiles
     if (grid % (a.Cd / PwD<KC>::NB) != 0) return fail(TSM_ERR_LAUNCH, "pw_dgrad: grid does not split over the parts of the result");
@@ -3652,12 +3624,8 @@ static int launch_wgrad_tr(WgradArgs& a, int Cout, int blocks_per_cu, const char
     const dim3 grid((unsigned)((grouped ? (a.nchunks + 7) / 8 * 8 : a.nchunks) * tiles));
     auto kern = wgrad_tr_kernel<BCO, BCI, WM, WN, AFF>;
     const size_t smem = (size_t)2 * WMK * (BCO * 2 + BCI * 2) + (size_t)2 * NT * sizeof(PixInfo);
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "wgrad: cannot raise dynamic LDS limit");
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kern, lds, "wgrad"));
     hipLaunchKernelGGL(kern, grid, dim3(NT), smem, s, a);
     return check_launch(name);
 }
@@ -3764,12 +3732,8 @@ static int launch_fused_tail(const TailArgs& a, long rows, hipStream_t s) {
     auto kern = fused_tail_kernel<MID, STREAM>;
     constexpr size_t smem = (size_t)2 * (256 + 128) * BK * sizeof(bf16_t) + (size_t)128 * (128 + 8) * sizeof(bf16_t) +
                             (size_t)256 * sizeof(RowInfo) + (size_t)10 * MID * sizeof(float);
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "fused_tail: cannot raise dynamic LDS limit");
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kern, lds, "fused_tail"));
     const int grid = igemm_grid((int)((rows + 255) / 256), 64, 64, 1);
     hipLaunchKernelGGL(kern, dim3(grid), dim3(512), smem, s, a);
     return check_launch(MID == 64 ? "fused_tail_64" : "fused_tail_128");

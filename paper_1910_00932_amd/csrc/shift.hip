@@ -32,6 +32,13 @@ int fail(int code, const char* fmt, ...) {
     return code;
 }
 
+int raise_lds_limit(const void* kernel, OncePerDevice& once, const char* what) {
+    int dev = 0;
+    const bool ok = hipGetDevice(&dev) == hipSuccess &&
+                    once(dev, [&] { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess; });
+    return ok ? TSM_OK : fail(TSM_ERR_LAUNCH, "%s: cannot raise dynamic LDS limit", what);
+}
+
 // ---- optional per-launch timing (measurement aid) ----------------------------------
 // While enabled, a HIP event is recorded on the profiled stream after every kernel
 // launch that goes through check_launch(); the time between consecutive events is

@@ -1331,12 +1331,8 @@ static long x_ksplit(long K, int splits) { return ((K + splits - 1) / splits + 6
 template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
 static int x_launch(XentArgs a, int splits, const char* what, hipStream_t s) {
     auto kernel = xent_tile_kernel<C, MODE, AKIND, BKIND, SPLIT, DB>;
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "%s: cannot raise dynamic LDS limit", what);
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kernel, lds, what));
     const long jobs = x_tiles(a.M, a.N, C::BM) * splits;
     a.ksplit = x_ksplit(a.K, splits);
     for (a.job0 = 0; a.job0 < jobs; a.job0 += X_LAUNCH) {
@@ -1366,12 +1362,8 @@ static int x_product(int size, const XentArgs& a, int splits, const char* what, 
 template <bool SPLIT>
 static int x_both(XentArgs dx, int zdx, XentArgs dw, int zdw, const XColumns& sums, const char* what, hipStream_t s) {
     auto kernel = xent_both_kernel<SPLIT>;
-    static bool configured = false;
-    if (!configured) {
-        if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-            return fail(TSM_ERR_LAUNCH, "%s: cannot raise dynamic LDS limit", what);
-        configured = true;
-    }
+    static OncePerDevice lds;
+    TSM_TRY(raise_lds_limit((const void*)kernel, lds, what));
     const long nx = x_tiles(dx.M, dx.N, XSmall::BM) * zdx, nw = x_tiles(dw.M, dw.N, XSmall::BM) * zdw;
     dx.ksplit = x_ksplit(dx.K, zdx);
     dw.ksplit = x_ksplit(dw.K, zdw);
