@@ -70,8 +70,8 @@ __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float
 // The factor in [1, 2) that bf16 G leaves out of dloss, and what reads G puts back: the mantissa of the first ordinary dloss among the
 // rows with a label, the same in every tile.  A mean's dloss is one number for all rows, and the entry of a row's label, by far
 // its largest, is almost that number: rounded with it, all of them would be off alike, by up to 2^-9 of the whole gradient.
-// Of up to 512 rows every wavefront looks for itself, 64 at a time, most often once; of more, a launch of one block does (us of a training
-// pass without and with it: 128 x 2048 x 1000 29 to 30 and 33 to 34, 1777 x 1000 x 32003 535 and 541), which passes over any number of rows.
+// Of up to 512 rows every wavefront looks for itself, 64 at a time, most often once; of more, a launch of one block does (4.7 us at 1777 rows,
+// 5.3 at 8192; a pass of 128 x 2048 x 1000, 29 us, would be 3 to 4 longer with it), which passes over any number of rows.
 __device__ __forceinline__ bool ordinary(float v) {
     const uint32_t exponent = (__float_as_uint(v) >> 23) & 0xff;
     return exponent != 0 && exponent != 0xff;
@@ -115,11 +115,13 @@ __global__ void __launch_bounds__(1024) xent_scale_kernel(const float* __restric
             use[i] = is_class(labels[at], classes) && ordinary(dloss[at]) && r < rows;
         }
 #pragma unroll
-        for (int i = 0; i < X_SCALE_TURN; ++i)
-            if (use[i]) {
-                atomicMin(&s_first, (int)(base + i * 1024 + threadIdx.x));
+        for (int i = 0; i < X_SCALE_TURN; ++i) {
+            const uint64_t count = __ballot(use[i]);
+            if (count) {                                        // the wavefront's first; one LDS access for all of it
+                if ((threadIdx.x & 63) == 0) atomicMin(&s_first, (int)(base + i * 1024 + threadIdx.x + __builtin_ctzll(count)));
                 break;
             }
+        }
         __syncthreads();
         if (s_first < rows) break;                              // (the same for all: the next turn writes behind another barrier)
         __syncthreads();
