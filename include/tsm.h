@@ -431,7 +431,10 @@ int tsm_layernorm_bwd(const tsm_layernorm_desc* d, const void* x, const void* dy
  * dx, dw: the types of x and w, overwritten; dbias fp32; each may be NULL where it is not wanted, not all of them.
  * The backward pass forms the logits again, in pieces of the classes; lse is the forward pass's.  In TSM_BF16 the
  * entries of G, without the mantissa that the dloss of all rows may share, are rounded to bf16 for the two products
- * (dbias is summed before that), everything else is fp32.  In
+ * where there are more than 64 rows and more than 64 classes: a gradient is then off by up to 1.2 times what its own
+ * rounding costs (0.0017 of its norm), and the probability of a row's label counts as zero in it where it is below
+ * 2^-9.  Up to 64 rows or classes G keeps 16 bits, and in TSM_F32, which is how to have it in full, all of them
+ * (dbias is summed before that rounding), everything else is fp32.  In
  * TSM_F32 a product is the sum of six products of bf16 parts, good to 2^-24 of it for operands of 2^-110 and more; an
  * infinite operand makes the sums it enters NaN.
  * Logits of minus infinity (a bias that takes a class out) are classes without weight; where no class of a row is left

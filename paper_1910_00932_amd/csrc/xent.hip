@@ -7,8 +7,8 @@
 // joined over the tiles) and the label's logit.  Backward: s is formed again in pieces of the classes, a piece of G lives in the
 // workspace for the two products that read it.  Four products of rows x features x classes in all, on the bf16 matrix cores.
 //
-// bf16: G, but for a factor (XScale), is rounded once, to the type of the matrix cores' operands; lse, the losses, db (from G before that rounding) and
-// all sums are fp32.  fp32: x, w and G are cut into three bf16 parts each, exactly (8 + 8 + 8 bits), and a product is the sum of the
+// bf16: G, but for a factor (XScale), is rounded once, to the type of the matrix cores' operands, or of few rows or classes cut into two parts
+// (X_GTWO); lse, the losses, db (from G before that) and all sums are fp32.  fp32: x, w and G are cut into three bf16 parts each, exactly (8 + 8 + 8 bits), and a product is the sum of the
 // six largest part products (the method of Henry, Tang and Heinecke, "Leveraging the bfloat16 artificial intelligence datatype for
 // higher-precision computations", 2019; what is left out is at most 2^-24 of it), the small ones first.
 #include <algorithm>
@@ -67,7 +67,7 @@ __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float
     m = t;
 }
 
-// The factor in [1, 2) that bf16 G leaves out of dloss, and what reads G puts back: the mantissa of the first ordinary dloss among the
+// The factor in [1, 2) that bf16 G of one part leaves out of dloss, and what reads G puts back: the mantissa of the first ordinary dloss among the
 // rows with a label, the same in every tile.  A mean's dloss is one number for all rows, and the entry of a row's label, by far
 // its largest, is almost that number: rounded with it, all of them would be off alike, by up to 2^-9 of the whole gradient.
 // Of up to 512 rows every wavefront looks for itself, 64 at a time, most often once; of more, a launch of one block does (4.7 us at 1777 rows,
@@ -521,9 +521,10 @@ struct XStage {
 };
 static constexpr int X_LAUNCH = 1 << 22;   // blocks of one launch, at most
 
-// SPLIT: operands in three parts.  DB: the column sums of G are wanted.
-template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
+// GP: the parts of G, 3 for fp32, whose operands are in three parts too (SPLIT), 2 or 1 for bf16.  DB: the column sums of G are wanted.
+template <typename C, int MODE, int AKIND, int BKIND, int GP, bool DB>
 __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njobs) {
+    constexpr bool SPLIT = GP == 3, TWICE = GP == 2 && MODE == XE_OUT;      // TWICE: every step of K once per part of G
     constexpr int BM = C::BM, BN = C::BN, WM = C::WM, WN = C::WN, NT = WM * WN * 64, MI = BM / (WM * 32), NJ = BN / (WN * 32);
     constexpr bool BIG = NJ == 2;
     static_assert((BIG && (MI == 4 || MI == 2)) || (MI == 1 && NJ == 1) || (C::PARTS == 3 && MI == 2 && NJ == 1 && SPLIT), "read_frags, read_step, read_parts");
@@ -556,10 +557,11 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
     const long mt = band * BAND + rest % high, nt = rest / high;
     const long m0 = mt * BM, n0 = nt * BN;
     const long kb = z * a.ksplit, ke = kb + a.ksplit < a.K ? kb + a.ksplit : a.K;
-    const int steps = ke > kb ? (int)((ke - kb + BK - 1) / BK) : 0;
+    const int steps = ke > kb ? (int)((ke - kb + BK - 1) / BK) * (TWICE ? 2 : 1) : 0;
     OpA pa;
     OpB pb;
     int kc = 0;                                                 // the step at the operands' windows
+    int part0 = TWICE ? 1 : 0;                                  // the part of A that it takes, of those the first
     auto load_step = [&](int stage) {
         unsigned char* st = smem + (group * NS + stage) * STAGE;
         const long l = ke - kb - (long)kc * BK;
@@ -572,7 +574,7 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
 #pragma unroll
         for (int part = 0; part < S::APARTS; ++part) {
 #pragma unroll
-            for (int q = 0; q < OpA::PIECES; ++q) pa.load(st + part * OpA::BYTES, q, left, ~0ull, wave_u, part * a.aplane * 2);
+            for (int q = 0; q < OpA::PIECES; ++q) pa.load(st + part * OpA::BYTES, q, left, ~0ull, wave_u, (part0 + part) * a.aplane * 2);
             if (part < S::BPARTS)
 #pragma unroll
                 for (int q = 0; q < OpB::PIECES; ++q) pb.load(st + S::APARTS * OpA::BYTES + part * OpB::BYTES, q, left, mask, wave_u, part * a.bplane * 2);
@@ -583,7 +585,10 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
             kc += KG;
             pa.restart((long)kc * BK);
             pb.restart((long)kc * BK);
+        } else if (TWICE && part0 == 1) {                       // the same K of the large part (B comes from L2 this time)
+            part0 = 0;
         } else {
+            if (TWICE) part0 = 1;
             ++kc;
             pa.advance();
             pb.advance();
@@ -617,7 +622,7 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    constexpr bool SCALE = !SPLIT && MODE != XE_STATS;
+    constexpr bool SCALE = GP == 1 && MODE != XE_STATS;
     XScale scale;
     float factor = 1.f;
     if constexpr (SCALE && MODE == XE_OUT) scale.load(a.e, a.e.rows);      // (awaited behind the first steps' loads)
@@ -969,7 +974,6 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
                     if (lo == 31) s_sum[wm * BN + wn * TN + ncol(j, r / 4) + r % 4] = t;
                 }
         }
-        constexpr int GPARTS = SPLIT ? 3 : 1;
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -980,14 +984,18 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
 #pragma unroll
                     for (int t = 0; t < 8; ++t) f[t] = acc[i][j][4 * q + t];
 #pragma unroll
-                    for (int part = 0; part < GPARTS; ++part) {
+                    for (int part = 0; part < GP; ++part) {
                         uint32_t w[4];
 #pragma unroll
                         for (int t = 0; t < 4; ++t) {
                             w[t] = pack_bf16x2(f[2 * t], f[2 * t + 1]);
-                            if (part + 1 < GPARTS) {
+                            if (part + 1 < GP) {
                                 f[2 * t] -= __uint_as_float(w[t] << 16);
                                 f[2 * t + 1] -= __uint_as_float(w[t] & 0xffff0000u);
+                                if (GP == 2) {                          // (what is infinite or NaN is so in its first part alone)
+                                    f[2 * t] = f[2 * t] == f[2 * t] ? f[2 * t] : 0.f;
+                                    f[2 * t + 1] = f[2 * t + 1] == f[2 * t + 1] ? f[2 * t + 1] : 0.f;
+                                }
                             }
                         }
                         swap_halves(w[0], w[2]);
@@ -1058,9 +1066,9 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
     }
 }
 
-template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
+template <typename C, int MODE, int AKIND, int BKIND, int GP, bool DB>
 __global__ void __launch_bounds__(C::WM * C::WN * C::KG * 64) xent_tile_kernel(XentArgs a) {
-    xent_tile<C, MODE, AKIND, BKIND, SPLIT, DB>(a, blockIdx.x, gridDim.x);
+    xent_tile<C, MODE, AKIND, BKIND, GP, DB>(a, blockIdx.x, gridDim.x);
 }
 // out[c] = sum of the rows of part [rows][ld], eight and then any number of them at a time
 __device__ __forceinline__ void column_sum(const float* __restrict__ part, long rows, long ld, long n, float* __restrict__ out, long block) {
@@ -1081,11 +1089,11 @@ struct XColumns {
     float* out;
 };
 // The two products that read G, where both have small tiles: dx by the first nx blocks, dw by nw, the sums of dbias by any others.
-template <bool SPLIT>
+template <int GP>
 __global__ void __launch_bounds__(XSmall::WM * XSmall::WN * 64) xent_both_kernel(XentArgs dx, XentArgs dw, int nx, int nw, XColumns sums) {
     const int b = blockIdx.x;
-    if (b < nx) xent_tile<XSmall, XE_OUT, X_GROWS, X_COLS, SPLIT, false>(dx, b, nx);
-    else if (b < nx + nw) xent_tile<XSmall, XE_OUT, X_GCOLS, X_COLS, SPLIT, false>(dw, b - nx, nw);
+    if (b < nx) xent_tile<XSmall, XE_OUT, X_GROWS, X_COLS, GP, false>(dx, b, nx);
+    else if (b < nx + nw) xent_tile<XSmall, XE_OUT, X_GCOLS, X_COLS, GP, false>(dw, b - nx, nw);
     else column_sum(sums.part, sums.rows, sums.ld, sums.n, sums.out, b - nx - nw);
 }
 
@@ -1205,6 +1213,7 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float* __restrict_
 // ---- host --------------------------------------------------------------------------------
 struct XentPlan {
     long piece, pieces;           // classes of a piece of G, number of pieces
+    int gparts;                   // bf16 parts of G
     long Cp;                      // row pitch of x and w as operands
     bool whole;                   // fp32 operands as they are (small tiles only)
     bool cut;                     // x and w are made into operands in the workspace
@@ -1218,6 +1227,12 @@ struct XentPlan {
     size_t o_x, o_w, o_part, o_picked, o_G, o_acc, o_dw, o_dbias, o_mask, o_scale;
 };
 
+// In bf16 G is one bf16 number per entry, or two, of 16 bits in all.  With few rows or classes a gradient is made of few entries, whose
+// roundings do not average: of one row it is off by up to 2.0 times what the rounding of the results costs (1 x 76 x 3: 0.0033 of its norm, with
+// two parts 0.0016), of more than 64 rows and classes by 1.0 to 1.2 times.  And there the second part costs little, since the products wait
+// for what they read (us of a pass with one part and two: 64 x 2048 x 400 29 and 29, 8192 x 2048 x 10 67 and 67, 4 x 2048 x 65536 223 and
+// 242, 64 x 2048 x 65536 240 and 270), where those of 1777 x 1000 x 32003, 235 of 538 us, would take twice as long.
+static constexpr int X_GTWO = 64;
 static constexpr size_t XENT_G_BYTES = (size_t)512 << 20;   // of a piece of G, at most (a piece has 1024 classes at least)
 
 static long x_tiles(long M, long N, int t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }
@@ -1268,7 +1283,8 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     XentPlan p{};
     const long R = d->rows, D = d->features, V = d->classes;
     const int parts = d->dtype == TSM_F32 ? 3 : 1;
-    long piece = (long)(XENT_G_BYTES / (2 * parts)) / R / 1024 * 1024;
+    p.gparts = parts == 3 ? 3 : std::min(R, V) <= X_GTWO ? 2 : 1;
+    long piece = (long)(XENT_G_BYTES / (2 * p.gparts)) / R / 1024 * 1024;
     if (piece < 1024) piece = 1024;
     if (piece > V) piece = V;
     p.piece = piece;
@@ -1307,12 +1323,12 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     p.zdx = x_splits(p.sizedx, R, D, piece, f32);
     p.sizedw = p.whole ? X_SMALL : std::max(least, x_size(piece, D, R, true, f32));
     p.zdw = x_splits(p.sizedw, piece, D, R, f32);
-    p.o_G = b.used; b.take((size_t)parts * p.gplane * 2);
+    p.o_G = b.used; b.take((size_t)p.gparts * p.gplane * 2);
     p.o_acc = b.used; b.take((parts == 1 && p.pieces > 1) || p.zdx > 1 ? (size_t)p.zdx * R * D * 4 : 0);
     p.o_dw = b.used; b.take(p.zdw > 1 ? (size_t)p.zdw * piece * D * 4 : 0);
     p.o_dbias = b.used; b.take((size_t)p.mtiles * p.lddb * 4);
     p.o_mask = b.used; b.take((size_t)(R + 255) / 256 * 4 * 8);
-    p.o_scale = b.used; b.take(f32 || R <= X_SCALE_ROWS ? 0 : 4);
+    p.o_scale = b.used; b.take(p.gparts > 1 || R <= X_SCALE_ROWS ? 0 : 4);
     p.bwd_bytes = b.used;
     return p;
 }
@@ -1330,46 +1346,47 @@ static size_t xent_ws(const XentPlan& p) { return p.fwd_bytes > p.bwd_bytes ? p.
 
 static long x_ksplit(long K, int splits) { return ((K + splits - 1) / splits + 63) / 64 * 64; }
 
-template <typename C, int MODE, int AKIND, int BKIND, bool SPLIT, bool DB>
+template <typename C, int MODE, int AKIND, int BKIND, int GP, bool DB>
 static int x_launch(XentArgs a, int splits, const char* what, hipStream_t s) {
-    auto kernel = xent_tile_kernel<C, MODE, AKIND, BKIND, SPLIT, DB>;
+    auto kernel = xent_tile_kernel<C, MODE, AKIND, BKIND, GP, DB>;
     static OncePerDevice lds;
     TSM_TRY(raise_lds_limit((const void*)kernel, lds, what));
     const long jobs = x_tiles(a.M, a.N, C::BM) * splits;
     a.ksplit = x_ksplit(a.K, splits);
     for (a.job0 = 0; a.job0 < jobs; a.job0 += X_LAUNCH) {
         const long n = jobs - a.job0;
-        kernel<<<dim3((unsigned)(n < X_LAUNCH ? n : X_LAUNCH)), dim3(C::WM * C::WN * C::KG * 64), XStage<C, MODE, SPLIT>::SMEM, s>>>(a);
+        kernel<<<dim3((unsigned)(n < X_LAUNCH ? n : X_LAUNCH)), dim3(C::WM * C::WN * C::KG * 64), XStage<C, MODE, GP == 3>::SMEM, s>>>(a);
         TSM_TRY(check_launch(what));
     }
     return TSM_OK;
 }
 
-template <int MODE, int AKIND, int BKIND, bool SPLIT, bool DB = false>
+template <int MODE, int AKIND, int BKIND, int GP, bool DB = false>
 static int x_product(int size, const XentArgs& a, int splits, const char* what, hipStream_t s) {
+    constexpr bool SPLIT = GP == 3;
     if constexpr (SPLIT) {
-        if (size == X_MID) return x_launch<XParts, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
-    } else {
-        if (size == X_BIG) return x_launch<XBig, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
-        if (size == X_MID) return x_launch<XMid, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+        if (size == X_MID) return x_launch<XParts, MODE, AKIND, BKIND, GP, DB>(a, splits, what, s);
+    } else if constexpr (GP == 1 || MODE == XE_OUT) {           // (two parts: s is at most 64 rows or columns, and has small tiles)
+        if (size == X_BIG) return x_launch<XBig, MODE, AKIND, BKIND, GP, DB>(a, splits, what, s);
+        if (size == X_MID) return x_launch<XMid, MODE, AKIND, BKIND, GP, DB>(a, splits, what, s);
     }
     if constexpr (MODE != XE_OUT)
-        if (size == X_TINY) return x_launch<typename std::conditional<SPLIT, XTinyWhole, XTiny>::type, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+        if (size == X_TINY) return x_launch<typename std::conditional<SPLIT, XTinyWhole, XTiny>::type, MODE, AKIND, BKIND, GP, DB>(a, splits, what, s);
     if constexpr (MODE != XE_OUT)      // (us at 64 x 2048 x 400: 14.2 with small tiles, 10.3 with deep ones)
-        if (x_tiles(a.M, a.N, 64) <= 256 && a.K >= 512) return x_launch<XDeep, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
-    return x_launch<XSmall, MODE, AKIND, BKIND, SPLIT, DB>(a, splits, what, s);
+        if (x_tiles(a.M, a.N, 64) <= 256 && a.K >= 512) return x_launch<XDeep, MODE, AKIND, BKIND, GP, DB>(a, splits, what, s);
+    return x_launch<XSmall, MODE, AKIND, BKIND, GP, DB>(a, splits, what, s);
 }
 
 // dx, dw and what is left of dbias in one launch: small ones would otherwise wait for one another's.
-template <bool SPLIT>
+template <int GP>
 static int x_both(XentArgs dx, int zdx, XentArgs dw, int zdw, const XColumns& sums, const char* what, hipStream_t s) {
-    auto kernel = xent_both_kernel<SPLIT>;
+    auto kernel = xent_both_kernel<GP>;
     static OncePerDevice lds;
     TSM_TRY(raise_lds_limit((const void*)kernel, lds, what));
     const long nx = x_tiles(dx.M, dx.N, XSmall::BM) * zdx, nw = x_tiles(dw.M, dw.N, XSmall::BM) * zdw;
     dx.ksplit = x_ksplit(dx.K, zdx);
     dw.ksplit = x_ksplit(dw.K, zdw);
-    kernel<<<dim3((unsigned)(nx + nw + (sums.n + 255) / 256)), dim3(XSmall::WM * XSmall::WN * 64), XStage<XSmall, XE_OUT, SPLIT>::SMEM, s>>>(dx, dw, (int)nx, (int)nw, sums);
+    kernel<<<dim3((unsigned)(nx + nw + (sums.n + 255) / 256)), dim3(XSmall::WM * XSmall::WN * 64), XStage<XSmall, XE_OUT, GP == 3>::SMEM, s>>>(dx, dw, (int)nx, (int)nw, sums);
     return check_launch(what);
 }
 
@@ -1438,12 +1455,12 @@ static int xent_fwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
         b.N = rest.columns;
         b.e.col0 = v0;
         b.e.part = (float2*)(ws + p.o_part) + tiles * a.M;
-        TSM_TRY((x_product<XE_STATS, X_ROWS, X_ROWS, F32>(p.size, b, 1, "xent_stats", s)));
+        TSM_TRY((x_product<XE_STATS, X_ROWS, X_ROWS, F32 ? 3 : 1>(p.size, b, 1, "xent_stats", s)));
         tiles += (b.N + x_tile(p.size) - 1) / x_tile(p.size);
         if (b.N < n) {
             x_columns<T>(p, b, b.N, n, x, (const T*)w + v0 * D, D);
             b.e.part = (float2*)(ws + p.o_part) + tiles * a.M;
-            TSM_TRY((x_product<XE_STATS, X_ROWS, X_ROWS, F32>(rest.size, b, 1, "xent_stats_rest", s)));
+            TSM_TRY((x_product<XE_STATS, X_ROWS, X_ROWS, F32 ? 3 : 1>(rest.size, b, 1, "xent_stats_rest", s)));
             tiles += (b.N + x_tile(rest.size) - 1) / x_tile(rest.size);
         }
     }
@@ -1456,7 +1473,7 @@ static int xent_fwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
     return check_launch("xent_finish");
 }
 
-template <typename T>
+template <typename T, int GP>
 static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, const void* w, const float* bias, const int32_t* labels,
                     const float* lse, const float* dloss, void* dx, void* dw, float* dbias, char* ws, hipStream_t s) {
     constexpr bool F32 = sizeof(T) == 4;
@@ -1466,7 +1483,7 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
     float *acc = F32 && p.zdx == 1 ? (float*)dx : (float*)(ws + p.o_acc), *dwp = (float*)(ws + p.o_dw), *dbp = (float*)(ws + p.o_dbias);
     uint64_t* mask = (uint64_t*)(ws + p.o_mask);
     const float* scale = nullptr;
-    if (!F32 && R > X_SCALE_ROWS) {
+    if (GP == 1 && R > X_SCALE_ROWS) {
         scale = (const float*)(ws + p.o_scale);
         xent_scale_kernel<<<dim3(1), dim3(1024), 0, s>>>(dloss, labels, d->rows, V, (float*)(ws + p.o_scale));
         TSM_TRY(check_launch("xent_scale"));
@@ -1500,7 +1517,7 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
                 // one row tile: its sums are the result
                 a.e.dbias_part = mtiles == 1 ? dbias + a.e.col0 : dbp;
                 a.e.lddb = p.lddb;
-                TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, F32, true>(size, a, 1, part ? "xent_grad_rest" : "xent_grad", s)));
+                TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, GP, true>(size, a, 1, part ? "xent_grad_rest" : "xent_grad", s)));
                 if (mtiles > 1 && both && rest.columns == n) {
                     sums = XColumns{dbp, mtiles, p.lddb, n, dbias + v0};
                 } else if (mtiles > 1) {
@@ -1508,7 +1525,7 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
                     TSM_TRY(check_launch("xent_dbias"));
                 }
             } else {
-                TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, F32>(size, a, 1, part ? "xent_grad_rest" : "xent_grad", s)));
+                TSM_TRY((x_product<XE_GRAD, X_ROWS, X_ROWS, GP>(size, a, 1, part ? "xent_grad_rest" : "xent_grad", s)));
             }
         }
         XentArgs gx{}, gw{};
@@ -1545,10 +1562,10 @@ static int xent_bwd(const tsm_xent_desc* d, const XentPlan& p, const void* x, co
             else gw.e.out = (bf16_t*)out;
         }
         if (both) {
-            TSM_TRY((x_both<F32>(gx, p.zdx, gw, p.zdw, sums, "xent_dx_dw", s)));
+            TSM_TRY((x_both<GP>(gx, p.zdx, gw, p.zdw, sums, "xent_dx_dw", s)));
         } else {
-            if (dx) TSM_TRY((x_product<XE_OUT, X_GROWS, X_COLS, F32>(p.sizedx, gx, p.zdx, "xent_dx", s)));
-            if (dw) TSM_TRY((x_product<XE_OUT, X_GCOLS, X_COLS, F32>(p.sizedw, gw, p.zdw, "xent_dw", s)));
+            if (dx) TSM_TRY((x_product<XE_OUT, X_GROWS, X_COLS, GP>(p.sizedx, gx, p.zdx, "xent_dx", s)));
+            if (dw) TSM_TRY((x_product<XE_OUT, X_GCOLS, X_COLS, GP>(p.sizedw, gw, p.zdw, "xent_dw", s)));
         }
         if (dx && p.zdx > 1 && c + 1 == p.pieces) TSM_TRY(xent_join<T>(acc, p.zdx, R * D, dx, "xent_dx_join", s));      // (each has added up its pieces)
         if (dw && p.zdw > 1) TSM_TRY(xent_join<T>(dwp, p.zdw, n * D, out, "xent_dw_join", s));
@@ -1601,8 +1618,8 @@ int tsm_xent_bwd(const tsm_xent_desc* d, const void* x, const void* w, const flo
     const Span out[] = {{dx, xb, "dx"}, {dw, wb, "dw"}, {dbias, bb, "dbias"}, {ws, need, "the workspace"}};
     TSM_TRY(check_spans(who, in, 6, out, 4));
     const hipStream_t s = (hipStream_t)stream;
-    return d->dtype == TSM_BF16 ? xent_bwd<bf16_t>(d, p, x, w, bias, labels, lse, dloss, dx, dw, dbias, (char*)ws, s)
-                                : xent_bwd<float>(d, p, x, w, bias, labels, lse, dloss, dx, dw, dbias, (char*)ws, s);
+    const auto run = d->dtype == TSM_F32 ? xent_bwd<float, 3> : p.gparts == 2 ? xent_bwd<bf16_t, 2> : xent_bwd<bf16_t, 1>;
+    return run(d, p, x, w, bias, labels, lse, dloss, dx, dw, dbias, (char*)ws, s);
 }
 
 }  // extern "C"

@@ -389,3 +389,45 @@ def test_bias_gradient_of_very_many_rows(dtype):
     want = np.array([0.5, -0.5]) * R * float(up[0])
     within(db.double().cpu().numpy(), want, (212 + 16) * U * np.abs(want), "dbias")
     within(loss[::4097].double().cpu().numpy(), np.full(R // 4097 + 1, np.log(2.0)), 16 * U, "loss")
+
+
+@pytest.mark.parametrize("shape", [(1, 76, 3), (1, 8, 2), (2, 437, 3871), (3, 875, 6), (1, 3108, 133), (2, 6, 64), (17, 520, 1000), (64, 2048, 400),
+                                   (64, 72, 20000), (300, 96, 2), (1000, 33, 13), (5000, 264, 64), (9000, 40, 50), (12, 136, 60000)])
+@pytest.mark.parametrize("biased,ignored", [(False, False), (True, True)])
+def test_few_rows_or_classes_keep_their_gradients(shape, biased, ignored):
+    """Up to 64 rows or classes a bf16 gradient is made of few entries of G, whose roundings would not average out: G is in two parts there,
+    each rounded by at most 2^-8 of itself, and off by 2^-16 of itself.  The bounds are those of the module otherwise."""
+    R, D, V = shape
+    labels = _labels(R, V, 4, ignored)
+    (x, w, b, up), (loss, lse, dx, dw, db) = _run(R, D, V, "bf16", values((V,), 2, "f32") if biased else None, labels)
+    used = ((labels >= 0) & (labels < V))[:, None]
+    S = (np.abs(x) @ np.abs(w).T).max(1) + (0 if b is None else np.abs(b).max())
+    d = (4 * np.sqrt(D) + 16) * U * S
+    el = d + (4 * np.sqrt(V) + 32) * U + 16 * U * S
+    _, rlse = H.xent_fwd(x, w, b, labels)
+    G = H.xent_grad(x, w, b, labels, up)
+    p = np.where(used, np.abs(up)[:, None] * np.exp(x @ w.T + (0 if b is None else b) - rlse[:, None]), 0)
+    eG = 2.0 ** -126 + p * (2 * (d + el)[:, None] + 8 * U) + np.abs(G) * (2.0 ** -16 + 4 * U)
+    rdx, rdw, _ = H.xent_bwd(x, w, b, labels, up)
+    aw, ax, half = np.abs(w), np.where(used, np.abs(x), 0), HALF["bf16"]
+    within(dx, rdx, eG @ aw + (4 * np.sqrt(V) + 16) * U * (np.abs(G) @ aw) + half * np.abs(rdx) + 2.0 ** -126, "dx")
+    within(dw, rdw, eG.T @ ax + (4 * np.sqrt(R) + 16) * U * (np.abs(G).T @ ax) + half * np.abs(rdw) + 2.0 ** -126, "dw")
+
+
+def test_infinities_and_nan_of_dloss_with_few_rows():
+    """One row's dloss is infinite, another's NaN: what is infinite or NaN is in those rows of dx alone."""
+    R, D, V = 20, 64, 30
+    labels = torch.arange(R, dtype=torch.int32, device="cuda")
+    d = B.XentDesc(rows=R, features=D, classes=V, dtype=B.TSM_BF16)
+    x, _ = values((R, D), 0, "bf16")
+    w, _ = values((V, D), 1, "bf16", scale=0.1)
+    ws = scratch(B.tsm_xent_workspace_bytes(d))
+    loss, lse, up = torch.empty(R, device="cuda"), torch.empty(R, device="cuda"), torch.ones(R, device="cuda")
+    B.tsm_xent_fwd(d, x, w, None, labels, loss, lse, ws)
+    clean, dx = torch.empty_like(x), torch.empty_like(x)
+    B.tsm_xent_bwd(d, x, w, None, labels, lse, up, clean, None, None, ws)
+    up[3], up[7] = float("inf"), float("nan")
+    B.tsm_xent_bwd(d, x, w, None, labels, lse, up, dx, None, None, ws)
+    ok = torch.ones(R, dtype=torch.bool, device="cuda")
+    ok[3] = ok[7] = False
+    assert torch.equal(dx[ok], clean[ok]) and not bool(dx[~ok].isfinite().any())
