@@ -334,13 +334,15 @@ __global__ void __launch_bounds__(1024) ln_join_kernel(const float* __restrict__
 }
 
 // ---- host --------------------------------------------------------------------------------
-// Blocks keep gamma and beta over their rows (200704 x 256 bf16: 512 52, 1024 37, 2048 36, 4096 48, 8192 67 us).
+// Blocks keep gamma and beta over their rows (200704 x 256 bf16: 512 52, 1024 37, 2048 36, 4096 48, 8192 67 us; inputs
+// from HBM, 1024, 2048, 4096: 43, 38, 38, 400000 x 64 34, 30, 29, 25088 x 2048 42, 38, 38, 6000 x 8192 36, 37, 41).
 static constexpr int LN_FWD_BLOCKS = 2048;
 // Rows that a thread adds up in turn for dgamma and dbeta, at most; of more rows there are more blocks and partial rows.  (512 blocks for all: 2^26
 // rows of 8 channels, 8192 in turn, lose 1.2e-4 of a sum of one sign, and twice that of twice the rows.)
 static constexpr int64_t LN_CHAIN = 512;
 static constexpr long LN_JOIN_BLOCKS = 1 << 16;      // (2^32 threads are more than a launch has: 2 x 2^27 columns in one turn)
-static constexpr int LN_BLOCKS = 512;     // of the backward pass: two per CU, each writes one partial row (25088 x 2048 bf16: 256 73, 512 56, 1024 63 us)
+static constexpr int LN_BLOCKS = 512;     // of the backward pass: two per CU, each writes one partial row (25088 x 2048 bf16: 256 73, 512 56, 1024 63 us; both
+                                          // passes of 6000 x 4096 76, 67, 75, of 200704 x 256 153, 111, 97, of 400000 x 64 144, 98, 76)
 
 // Lanes and vectors per lane of a row; 0 lanes: the row exceeds a block's registers.  Few vectors per lane keep many rows in
 // flight, up to four they cost no barrier.

@@ -561,7 +561,8 @@ struct RecurPlan {
 // half a block).  us in turn and side by
 // side, bf16, 2048 columns per clip: 4 clips of 300 frames (3 tiles) forward 10.5, 11.3, backward 13.7, 13.1; of 512 12.7, 11.3 and
 // 17.7, 13.7; of 1024 22.6, 14.3 and 35.3, 23.2; 8 clips of 1024 25.8, 23.7 and 42.7, 38.4; 16 clips 36.6, 38.6 and 58.4, 67.3.  fp32 forward,
-// which has registers for fewer tiles at a time: 4 clips of 512 13.5, 15.5, 8 clips of 1024 34.0, 41.7.
+// which has registers for fewer tiles at a time: 4 clips of 512 13.5, 15.5, 8 clips of 1024 34.0, 41.7.  Three tiles, both passes, in turn, the backward pass side by side, both: 1 clip
+// of 300 bf16 23.6, 23.5, 25.8, 2 clips 23.7, 22.8, 25.0, 4 clips 25.4, 24.8, 25.0, fp32 22.7, 22.4, 27.7, 25.0, 23.2, 24.9, 26.1, 26.8, 28.8.
 static RecurPlan recur_plan(const tsm_recur_desc* d, bool bwd) {
     RecurPlan p;
     const long M = (long)d->C * d->H * d->W;

@@ -1262,7 +1262,9 @@ static int x_size(long M, long N, long K, bool split, bool parts) {
 
 // The columns of s that fill whole rounds of tiles, and the tiles of the rest: where the last round would be at most half full, smaller
 // ones that need one round of their own.  (A round of large, middle, small tiles at 1000 features: 36, 21, 9 us; in fp32 at 1024 41 for the
-// middle ones, 18 for deep ones.)
+// middle ones, 18 for deep ones.  At fewer features there is less to win than the second launch costs, us of a pass without and with it:
+// bf16 1777 x 128 x 32003 179, 182, x 256 254, 264, x 384 276, 274, 1030 x 128 x 14000 83, 85, x 256 128, 121, x 384 156, 143; fp32 512 x 128 x 8500
+// 97, 98, x 256 127, 125, x 384 156, 147; from 512 on 1030 x 520 x 14000 172, 153.)
 struct XRest {
     long columns;
     int size;
