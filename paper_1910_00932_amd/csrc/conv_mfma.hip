@@ -2375,6 +2375,9 @@ __global__ void __launch_bounds__(512) pw_dgrad_kernel(IgemmArgs a) {
             };
             // lane: pixel r, channels 32*j + 8*q + 4*hi + {0..3}
             auto stage = [&]() {
+                // 12 states between the last product and the first read of its result, whatever lies in between: behind the branch around
+                // load_a, which the last slab takes, the compiler leaves 7
+                asm volatile("s_nop 11" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     bf16_t* dstp = Cst + r * LDC + j * 32 + 4 * hi;
