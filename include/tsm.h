@@ -436,8 +436,7 @@ int tsm_layernorm_bwd(const tsm_layernorm_desc* d, const void* x, const void* dy
  * 2^-9.  Up to 64 rows or classes G keeps 16 bits, and in TSM_F32, which is how to have it in full, all of them
  * (dbias is summed before that rounding), everything else is fp32.  In
  * TSM_F32 a product is the sum of six products of bf16 parts, good to 2^-24 of it for operands of 2^-110 and more; an
- * infinite operand makes the sums it enters NaN; logits lean to lower values over many features (lse by 2e-7 of itself at
- * 2^16 of them, 6e-6 at 2^21).
+ * infinite operand makes the sums it enters NaN.
  * Logits of minus infinity (a bias that takes a class out) are classes without weight; where no class of a row is left
  * its lse is minus infinity, and its loss and gradients are NaN.  No output may overlap an input or another output.
  * Workspace of both calls: tsm_xent_workspace_bytes(desc).  At most 2^21 features.

@@ -516,7 +516,7 @@ struct XStage {
     static constexpr int BK = WOUT ? 32 : C::BK, APARTS = WOUT ? 3 : C::PARTS, BPARTS = C::PARTS, BROWS = WOUT ? 2 * C::BN : C::BN;
     static constexpr int NS = WOUT ? 3 : C::NS;
     static constexpr int BYTES = (C::BM * APARTS + BROWS * BPARTS) * BK * 2;
-    static constexpr int STAGES = C::DIRECT ? (C::KG - 1) * C::BM * C::BN * 4 : C::KG * NS * BYTES;      // (direct: the groups' sums)
+    static constexpr int STAGES = C::DIRECT ? C::KG * C::BM * C::BN * 4 : C::KG * NS * BYTES;      // (direct: the groups' sums)
     static constexpr int SMEM = STAGES + C::WN * C::BM * 8 + C::BN * 4;       // stages, row statistics, biases
 };
 static constexpr int X_LAUNCH = 1 << 22;   // blocks of one launch, at most
@@ -636,6 +636,30 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
 #pragma unroll
         for (int k = 0; k < 6; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[PB[k]], fa[PA[k]], acc[0][0], 0, 0, 0);
     };
+    // fp32 logits: every 8 steps what the matrix cores have added up is added to a sum outside of them, which rounds to the nearest.  Theirs
+    // lean to minus infinity, each addition by a little: of 2^21 features lse by 6e-6 of itself, of 65536 by 2e-7, now 4e-7 and 0.9e-7 (us of a pass of
+    // 192 x 1024 x 30000 437 and 442, 512 x 1024 x 10007 322 and 323).
+    constexpr bool SETTLE = SPLIT && MODE != XE_OUT;
+    constexpr int CHAIN = 8;
+    x_f32x16 settled[SETTLE && !C::DIRECT ? MI : 1][NJ];
+    if constexpr (SETTLE && !C::DIRECT) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) settled[i][0] = acc[i][0];
+    }
+    auto settle = [&](int n, bool last) {                       // behind the n-th step
+        if constexpr (SETTLE && !C::DIRECT) {
+            if (!last && n % CHAIN != CHAIN - 1) return;
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                asm volatile("s_nop 11" : "+v"(acc[i][0]));     // (12 states between a product and what reads it: behind this branch the compiler leaves 3)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    settled[i][0][r] += acc[i][0][r];
+                    acc[i][0][r] = last ? settled[i][0][r] : 0.f;
+                }
+            }
+        }
+    };
     auto join_groups = [&]() {                                  // the sums of all groups, in the first one
         float4* sums = (float4*)smem;                           // [KG - 1][4][NT]
         if (group > 0) {
@@ -733,16 +757,43 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) multiply_parts(XCut::of(fa[f][2 * ks], fa[f][2 * ks + 1]).part, XCut::of(fb[f][2 * ks], fb[f][2 * ks + 1]).part);
         };
+        // (no registers are left for another sum: it lies in LDS, where the groups' meet)
+        float4* sums = (float4*)smem;                           // [KG][4][NT]
+        auto put = [&](bool first) {
+            asm volatile("s_nop 11" : "+v"(acc[0][0]));         // (as above)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float4* at = sums + (group * 4 + r) * NT + tid;
+                const float4 o = first ? make_float4(0.f, 0.f, 0.f, 0.f) : *at;
+                *at = make_float4(o.x + acc[0][0][4 * r], o.y + acc[0][0][4 * r + 1], o.z + acc[0][0][4 * r + 2], o.w + acc[0][0][4 * r + 3]);
+                acc[0][0][4 * r] = acc[0][0][4 * r + 1] = acc[0][0][4 * r + 2] = acc[0][0][4 * r + 3] = 0.f;
+            }
+        };
+        bool first = true;
         if (group < steps) fetch(group, 0);
-        for (int s = group; s < steps; s += 2 * KG) {
+        for (int s = group, n = 0; s < steps; s += 2 * KG, n += 2) {
             if (s + KG < steps) fetch(s + KG, 1);
             take(0);
             if (s + KG < steps) {
                 if (s + 2 * KG < steps) fetch(s + 2 * KG, 0);
                 take(1);
             }
+            if (n % CHAIN == CHAIN - 2) {
+                put(first);
+                first = false;
+            }
         }
-        join_groups();
+        if (group > 0 || !first) put(first);
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll 3
+            for (int g = first ? 1 : 0; g < KG; ++g)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float4 o = sums[(g * 4 + r) * NT + tid];
+                    acc[0][0][4 * r] += o.x; acc[0][0][4 * r + 1] += o.y; acc[0][0][4 * r + 2] += o.z; acc[0][0][4 * r + 3] += o.w;
+                }
+        }
     } else if constexpr (KG > 1) {
         kc = group - KG;
         if (group < steps) next_step(0);
@@ -764,7 +815,9 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
                     for (int k = 0; k < 4; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k], fa[k], acc[0][0], 0, 0, 0);
                 }
             }
+            settle(s / KG, false);
         }
+        settle(0, true);
         x_wait<0>();
         x_barrier();
         join_groups();
@@ -797,7 +850,9 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
             };
             slice(std::integral_constant<int, 0>{});
             slice(std::integral_constant<int, 1>{});
+            settle(s, false);
         }
+        settle(0, true);
     } else {
         // One barrier per step: in front of it every wavefront waits for its loads of this step, behind it the stage of the step
         // before is free.
@@ -805,40 +860,44 @@ __device__ __forceinline__ void xent_tile(const XentArgs& a, int block, int njob
         if (NS > 3 && steps > 2) next_step(2);
         if constexpr (SCALE && MODE == XE_OUT) factor = scale.get(a.e, a.e.rows);
         int stage = 0;
-        for (int s = 0; s < steps; ++s) {
-            if (s + NS - 2 < steps) x_wait<(NS - 2) * NP>();
-            else x_wait<0>();
-            x_barrier();
-            if (s + NS - 1 < steps) next_step(stage == 0 ? NS - 1 : stage - 1);
-            const uint32_t so = stage * STAGE;
-            if constexpr (WOUT) {
-                const uint32_t b[4] = {bat[0] + so, bat[1] + so, bat[2] + so, bat[3] + so};
-                auto slice = [&](auto number) {
-                    constexpr int ks = decltype(number)::value;
-                    x_bf16x8 fa[3];
-                    float fb[8];
-                    if constexpr (OpA::KC) read_whole<ks>(aat[ks] + so, b, fa, fb);
-                    else read_whole_tr<ks>(aat[0] + so, b, fa, fb);
-                    multiply_parts(fa, XCut(fb).part);
-                };
-                slice(std::integral_constant<int, 0>{});
-                slice(std::integral_constant<int, 1>{});
-            } else {
-                x_bf16x8 fa[4], fb[4];
-                const uint32_t q[4] = {aat[0] + so, aat[OpA::KC ? 1 : 0] + so, aat[OpA::KC ? 2 : 0] + so, aat[OpA::KC ? 3 : 0] + so};
-                const uint32_t b[4] = {bat[0] + so, bat[OpB::KC ? 1 : 0] + so, bat[OpB::KC ? 2 : 0] + so, bat[OpB::KC ? 3 : 0] + so};
-                if constexpr (OpA::KC && OpB::KC) read_step(q, b, fa, fb);
-                else if constexpr (OpA::KC) read_step(q, b[0], fa, fb);
-                else read_step(q[0], b[0], fa, fb);
-                if constexpr (WHOLE) {
-#pragma unroll
-                    for (int ks = 0; ks < 2; ++ks) multiply_parts(XCut::of(fa[2 * ks], fa[2 * ks + 1]).part, XCut::of(fb[2 * ks], fb[2 * ks + 1]).part);
+        for (int s = 0; s < steps;) {                           // (a chain at a time: a branch in every step costs 3 % of 192 x 1024 x 30000)
+            const int to = SETTLE && steps - s > CHAIN ? s + CHAIN : steps;
+            for (; s < to; ++s) {
+                if (s + NS - 2 < steps) x_wait<(NS - 2) * NP>();
+                else x_wait<0>();
+                x_barrier();
+                if (s + NS - 1 < steps) next_step(stage == 0 ? NS - 1 : stage - 1);
+                const uint32_t so = stage * STAGE;
+                if constexpr (WOUT) {
+                    const uint32_t b[4] = {bat[0] + so, bat[1] + so, bat[2] + so, bat[3] + so};
+                    auto slice = [&](auto number) {
+                        constexpr int ks = decltype(number)::value;
+                        x_bf16x8 fa[3];
+                        float fb[8];
+                        if constexpr (OpA::KC) read_whole<ks>(aat[ks] + so, b, fa, fb);
+                        else read_whole_tr<ks>(aat[0] + so, b, fa, fb);
+                        multiply_parts(fa, XCut(fb).part);
+                    };
+                    slice(std::integral_constant<int, 0>{});
+                    slice(std::integral_constant<int, 1>{});
                 } else {
+                    x_bf16x8 fa[4], fb[4];
+                    const uint32_t q[4] = {aat[0] + so, aat[OpA::KC ? 1 : 0] + so, aat[OpA::KC ? 2 : 0] + so, aat[OpA::KC ? 3 : 0] + so};
+                    const uint32_t b[4] = {bat[0] + so, bat[OpB::KC ? 1 : 0] + so, bat[OpB::KC ? 2 : 0] + so, bat[OpB::KC ? 3 : 0] + so};
+                    if constexpr (OpA::KC && OpB::KC) read_step(q, b, fa, fb);
+                    else if constexpr (OpA::KC) read_step(q, b[0], fa, fb);
+                    else read_step(q[0], b[0], fa, fb);
+                    if constexpr (WHOLE) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k], fa[k], acc[0][0], 0, 0, 0);
+                        for (int ks = 0; ks < 2; ++ks) multiply_parts(XCut::of(fa[2 * ks], fa[2 * ks + 1]).part, XCut::of(fb[2 * ks], fb[2 * ks + 1]).part);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k], fa[k], acc[0][0], 0, 0, 0);
+                    }
                 }
+                stage = stage + 1 == NS ? 0 : stage + 1;
             }
-            stage = stage + 1 == NS ? 0 : stage + 1;
+            settle(CHAIN - 1, to == steps);
         }
     }
 

@@ -431,3 +431,24 @@ def test_infinities_and_nan_of_dloss_with_few_rows():
     ok = torch.ones(R, dtype=torch.bool, device="cuda")
     ok[3] = ok[7] = False
     assert torch.equal(dx[ok], clean[ok]) and not bool(dx[~ok].isfinite().any())
+
+
+def test_logits_of_very_many_features_do_not_lean():
+    """fp32, 2^21 features.  Were the matrix cores' additions rounded to the nearest: a logit (2 in size, 10 at most) is the sum of 16 groups',
+    of 512 chains each, of 96 additions each.  An addition is off by 0.3 units of 2^-24 of what has been added up, up to 0.1 in a chain, 2 in
+    a group, 10 in the end: sqrt(8192 96) 0.1, sqrt(512 16) 2 and sqrt(16) 10 times 0.3 2^-24, together 3.6e-6, four of which are allowed;
+    lse is a mean of the logits' errors.  They round down instead, which costs 3.6e-5 in one chain per group."""
+    R, D, V = 8, 1 << 21, 100
+    d = B.XentDesc(rows=R, features=D, classes=V, dtype=B.TSM_F32)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(R, D, device="cuda", generator=gen)
+    w = torch.randn(V, D, device="cuda", generator=gen) * (2 / D ** 0.5)
+    lab = torch.arange(R, dtype=torch.int32, device="cuda")
+    ws = scratch(B.tsm_xent_workspace_bytes(d))
+    loss, lse = Guarded((R,), torch.float32), Guarded((R,), torch.float32)
+    B.tsm_xent_fwd(d, x, w, None, lab, loss.t, lse.t, ws)
+    s = sum(a.double() @ b.double().t() for a, b in zip(x.split(1 << 18, 1), w.split(1 << 18, 1)))
+    assert float(s.abs().max()) < 10
+    want = torch.logsumexp(s, 1)
+    within(lse.np(), want.cpu().numpy(), 1.5e-5, "lse")
+    within(loss.np(), (want - s[torch.arange(R, device="cuda"), lab.long()]).cpu().numpy(), 3e-5, "loss")
