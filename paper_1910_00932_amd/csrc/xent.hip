@@ -1345,7 +1345,8 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     const long R = d->rows, D = d->features, V = d->classes;
     const int parts = d->dtype == TSM_F32 ? 3 : 1;
     p.gparts = parts == 3 ? 3 : std::min(R, V) <= X_GTWO ? 2 : 1;
-    long piece = (long)(XENT_G_BYTES / (2 * p.gparts)) / R / 1024 * 1024;
+    const long grows = (R + X_GTILE - 1) / X_GTILE * X_GTILE;   // of G, whole blocks
+    long piece = (long)(XENT_G_BYTES / (2 * p.gparts)) / grows / 1024 * 1024;
     if (piece < 1024) piece = 1024;
     if (piece > V) piece = V;
     p.piece = piece;
@@ -1369,7 +1370,7 @@ static XentPlan xent_plan(const tsm_xent_desc* d) {
     p.xplane = R * p.Cp;
     p.wplane = piece * p.Cp;
     p.ldg = (piece + std::max(t, 64L) - 1) / std::max(t, 64L) * std::max(t, 64L) * X_GTILE;
-    p.gplane = (R + X_GTILE - 1) / X_GTILE * p.ldg;
+    p.gplane = grows / X_GTILE * p.ldg;
     p.lddb = (piece + 7) / 8 * 8;
     Arena f(nullptr, 0);
     p.o_x = f.used; f.take(p.cut ? (size_t)copies * p.xplane * 2 : 0);

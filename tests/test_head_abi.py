@@ -106,3 +106,13 @@ def test_tensors_that_are_not_contiguous_are_refused():
     t = torch.zeros(4, 6).t()
     with pytest.raises(ValueError):
         B.tsm_layernorm_fwd(_ln(), t, t, t, t, None, None)
+
+
+@pytest.mark.parametrize("dtype", [B.TSM_BF16, B.TSM_F32])
+@pytest.mark.parametrize("rows", [1, 5, 64, 65, 255, 300, 5000])
+def test_xent_workspace_does_not_grow_with_the_classes(rows, dtype):
+    """A piece of G has 512 MB at most, rounded-up rows included, so that from some number of classes on the workspace grows by the
+    forward pass's 8 bytes per row and tile of classes alone."""
+    few, many = (B.tsm_xent_workspace_bytes(_xe(rows=rows, features=8, classes=n, dtype=dtype)) for n in (3000000, 300000000))
+    tiles = rows * 8 * (300000000 // 32 + 1000)
+    assert few < (1 << 30) + (1 << 29) and many < (1 << 30) + (1 << 29) + tiles, (few, many)
